@@ -285,6 +285,99 @@ int mtnlg_colsum_static(int dtype, int64_t T, int64_t C, const void *in, void *o
 int mtnlg_bias_residual(int dtype, int64_t T, int64_t h, const void *res, const void *partial,
                         const void *bias, void *out, void *stream);
 
+/* --- operators of decoder layers on packed batches: root-mean-square norms in LayerNorm's place, rotary positions in that of the
+ *     learned ones, and attention over sequences of different lengths whose query heads share heads of keys and values.  They go
+ *     with the products above as mtnlg_layernorm_fwd / _bwd and mtnlg_attention_fwd / _bwd do. ------------------------------------ */
+
+/* s = x [+ residual] (stored to xsum, rounded; norms are of what is stored), rstd[t] = 1 / sqrt(mean over h of s^2 + eps),
+ * out = s * rstd * gamma.  residual NULL: s is x, and xsum is not written.  x, residual, xsum, out [T,h], gamma [h] in the storage type;
+ * xsum may be x or residual.  h a multiple of 8, <= 32768. */
+int mtnlg_rmsnorm_fwd(int dtype, int64_t T, int64_t h, const void *x, const void *residual, const void *gamma, float eps,
+                      void *xsum, void *out, float *rstd, void *stream);
+/* The same with the result in 8 bits: out [T,h] holds e4m3 codes (bias 7, no infinities, 448 the largest) of s * rstd * gamma / scale,
+ * rounded to nearest even; scale[t][i] = the largest magnitude of the row's i-th `columns` columns / 448 (the last may be fewer; 1 where
+ * all are zeros), float [T][ceil(h / columns)].  columns: a power of two from 8 to 512, or 0: one scale to a row.  A NaN gives the
+ * code of NaN.  out 8-byte aligned. */
+int mtnlg_rmsnorm_fwd_e4m3(int dtype, int64_t T, int64_t h, const void *x, const void *residual, const void *gamma, float eps,
+                           int32_t columns, void *xsum, void *out, float *scale, float *rstd, void *stream);
+/* Adjoint: x is what was normalised (xsum, or x without a residual).  dx [T,h] = dres (nullable: the gradient that reaches the sum by
+ * another way) + the norm's; it is the gradient of x and of the residual.  dx may be dout or dres.  dgamma [h], float when grad_f32,
+ * else the storage type, overwritten or (accumulate) added to.  Sums over rows in a fixed order. */
+size_t mtnlg_rmsnorm_bwd_workspace(int64_t T, int64_t h);
+int mtnlg_rmsnorm_bwd(int dtype, int64_t T, int64_t h, const void *x, const void *gamma, const float *rstd, const void *dout,
+                      const void *dres, void *dx, void *dgamma, int grad_f32, int accumulate, void *workspace,
+                      size_t workspace_bytes, void *stream);
+
+/* A matrix of heads: element c of head i of group j of token t at data[t * token + j * group + i * head + c], strides in elements.
+ * Groups are the heads of keys, a group's heads the query heads that share it (matrices of keys and values have one to a group: head is
+ * not looked at).  So q may be [token][head][c], a part of one projection's result [token][head][q|k|v][c] or
+ * [token][group][q .. q|k|v][c], or [head][token][c].  data and all strides are multiples of 16 bytes, no element lies on another
+ * (a stride of 0 is refused), and token is at most 2^25 bytes.  Strides of a dimension of one are not looked at. */
+typedef struct {
+  void *data;
+  int64_t token, group, head;
+} mtnlg_heads;
+
+enum mtnlg_rotary_layout { MTNLG_ROTARY_HALF = 0, MTNLG_ROTARY_INTERLEAVED = 1 };
+enum mtnlg_rotary_scaling { MTNLG_ROTARY_UNSCALED = 0, MTNLG_ROTARY_LINEAR = 1, MTNLG_ROTARY_BASE = 2, MTNLG_ROTARY_PARTS = 3 };
+typedef struct {
+  int32_t dtype;                       /* MTNLG_F32 or MTNLG_BF16                                             */
+  int32_t heads, kv_heads, head_dim;   /* heads a multiple of kv_heads; head_dim of 8, <= 256                   */
+  int32_t rotary_dim;                  /* n: the first n columns of a head turn (even), the others stay as they are */
+  int32_t layout;                      /* pairs: columns (i, n/2 + i) or (2 i, 2 i + 1)                         */
+  int32_t scaling;                     /* mtnlg_rotary_scaling                                                */
+  int32_t original_positions;          /* MTNLG_ROTARY_PARTS: length of the context that the model was trained on */
+  int64_t tokens;
+  double base;                         /* pair i turns by position * base^(-2 i / n) radians                    */
+  double factor;                       /* >= 1, scaled only                                                   */
+  double slow, fast;                   /* MTNLG_ROTARY_PARTS: turns in the original context, slow < fast        */
+  double amplitude;                    /* what cosines and sines are multiplied with; 0: 1, and 0.1 log(factor) + 1 of MTNLG_ROTARY_PARTS */
+} mtnlg_rotary_desc;
+
+/* q_out, k_out = the heads of q and k turned by their tokens' positions (int32 [tokens], device; NULL: token t is at position t).
+ * Rows of a negative position (padding) are neither read nor written.  MTNLG_ROTARY_LINEAR: frequencies divided by factor;
+ * _BASE: base * factor^(n / (n - 2)); _PARTS: of a pair that makes fewer than `slow` turns in the original context divided by factor, of one of
+ * more than `fast` left, in between by their share.  Angles are worked out in 64 bits.  An output may be its input (same
+ * strides); k and k_out may both be NULL. */
+int mtnlg_rotary_fwd(const mtnlg_rotary_desc *desc, const mtnlg_heads *q, const mtnlg_heads *k, const mtnlg_heads *q_out,
+                     const mtnlg_heads *k_out, const int32_t *positions, void *stream);
+/* Adjoint: gradients of q_out and k_out in, of q and k out (the heads turned back, with the same amplitude). */
+int mtnlg_rotary_bwd(const mtnlg_rotary_desc *desc, const mtnlg_heads *dq_out, const mtnlg_heads *dk_out, const mtnlg_heads *dq,
+                     const mtnlg_heads *dk, const int32_t *positions, void *stream);
+
+typedef struct {
+  int32_t dtype;                       /* MTNLG_F32 or MTNLG_BF16                                          */
+  int32_t heads, kv_heads, head_dim;   /* heads a multiple of kv_heads; head_dim of 8, <= 256                */
+  int32_t sequences;                   /* <= 2^20                                                          */
+  int32_t max_q, max_k;                /* no sequence has more queries, keys; what lies beyond is unspecified */
+  int64_t q_tokens, k_tokens;          /* rows of q, a, da, dq; of k, v, dk, dv; times their heads < 2^31    */
+  float scale;                         /* 0 => 1/sqrt(head_dim)                                            */
+} mtnlg_packed_desc;
+/* Sequence i has the rows offsets[i] .. offsets[i + 1] - 1, or the first lengths[i] of them (lengths nullable: a cache whose regions
+ * are not full, a padded batch).  Device arrays of sequences + 1 and sequences int32; offsets do not fall.  Lengths may be 0.  Values that lie
+ * outside the matrices are taken for the nearest inside; offsets that fall leave results unspecified. */
+typedef struct {
+  const int32_t *q_offsets, *k_offsets, *q_lengths, *k_lengths;
+} mtnlg_packed_sequences;
+
+/* Causal attention within each sequence: query t of lq sees the keys 0 .. t + lk - lq of lk, so that the last query sees all (lq = lk: a
+ * prompt or a document; lq < lk: a prompt continued, a single token; lq > lk: the first queries see none).  a = softmax(scale q k^T) v,
+ * lse [heads][q_tokens] float = log sum exp; a query that sees no key: a = 0, lse = -infinity.  Rows of no sequence are neither read nor
+ * written; what a query does not see, infinities and NaN included, does not reach its results.
+ * workspace (nullable, 16-byte aligned): mtnlg_packed_attention_fwd_workspace() bytes of scratch that lets calls of few queries cut long sequences
+ * of keys; 0 for calls that have no use for it. */
+size_t mtnlg_packed_attention_fwd_workspace(const mtnlg_packed_desc *desc);
+int mtnlg_packed_attention_fwd(const mtnlg_packed_desc *desc, const mtnlg_packed_sequences *where, const mtnlg_heads *q,
+                               const mtnlg_heads *k, const mtnlg_heads *v, const mtnlg_heads *a, float *lse, void *workspace,
+                               size_t workspace_bytes, void *stream);
+/* Adjoint: dq, and dk, dv summed over the heads of a group, from da and forward's a and lse.  Keys that no query sees get zeros.  dq, dk, dv
+ * are none of the inputs.  Run-to-run identical.  workspace >= mtnlg_packed_attention_bwd_workspace() bytes, 16-byte aligned. */
+size_t mtnlg_packed_attention_bwd_workspace(const mtnlg_packed_desc *desc);
+int mtnlg_packed_attention_bwd(const mtnlg_packed_desc *desc, const mtnlg_packed_sequences *where, const mtnlg_heads *q,
+                               const mtnlg_heads *k, const mtnlg_heads *v, const mtnlg_heads *a, const float *lse,
+                               const mtnlg_heads *da, const mtnlg_heads *dq, const mtnlg_heads *dk, const mtnlg_heads *dv,
+                               void *workspace, size_t workspace_bytes, void *stream);
+
 /* --- first and last pipeline stage's extras (the paper names the GPT-2 decoder, Section 3.2, and
  *     prints none of this: token embedding E [V,h] with learned positions P [s,h], final LayerNorm,
  *     output projection tied to E, next-token cross-entropy).  Under the tensor slicing of

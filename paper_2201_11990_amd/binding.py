@@ -20,6 +20,8 @@ GELU_TANH, GELU_ERF = 0, 1
 RECOMPUTE, ACCUMULATE_WGRAD, WGRAD_FP32 = 1, 2, 4
 GEMM_NT, GEMM_NN, GEMM_TN = 0, 1, 2
 EPI_BIAS, EPI_GELU, EPI_RESIDUAL, EPI_ACCUMULATE, EPI_OUT_F32, EPI_GELU_ERF, EPI_GELU_GRAD = 1, 2, 4, 8, 16, 32, 64
+ROTARY_HALF, ROTARY_INTERLEAVED = 0, 1
+ROTARY_UNSCALED, ROTARY_LINEAR, ROTARY_BASE, ROTARY_PARTS = 0, 1, 2, 3
 KERNEL_CLASSES = ("gemm_nt", "gemm_nn", "gemm_tn", "attn_fwd", "attn_bwd", "ln_fwd", "ln_bwd",
                   "gelu", "colsum", "elementwise")
 
@@ -49,6 +51,28 @@ class HeadDesc(ctypes.Structure):
     _fields_ = [("hidden", ctypes.c_int32), ("vocab_local", ctypes.c_int32), ("vocab_start", ctypes.c_int32),
                 ("seq", ctypes.c_int32), ("micro_batch", ctypes.c_int32), ("dtype", ctypes.c_int32),
                 ("ln_eps", ctypes.c_float)]
+
+
+class Heads(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("token", ctypes.c_int64), ("group", ctypes.c_int64), ("head", ctypes.c_int64)]
+
+
+class RotaryDesc(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("rotary_dim", ctypes.c_int32), ("layout", ctypes.c_int32), ("scaling", ctypes.c_int32),
+                ("original_positions", ctypes.c_int32), ("tokens", ctypes.c_int64), ("base", ctypes.c_double),
+                ("factor", ctypes.c_double), ("slow", ctypes.c_double), ("fast", ctypes.c_double), ("amplitude", ctypes.c_double)]
+
+
+class PackedDesc(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("sequences", ctypes.c_int32), ("max_q", ctypes.c_int32), ("max_k", ctypes.c_int32),
+                ("q_tokens", ctypes.c_int64), ("k_tokens", ctypes.c_int64), ("scale", ctypes.c_float)]
+
+
+class PackedSequences(ctypes.Structure):
+    _fields_ = [("q_offsets", ctypes.c_void_p), ("k_offsets", ctypes.c_void_p), ("q_lengths", ctypes.c_void_p),
+                ("k_lengths", ctypes.c_void_p)]
 
 
 REDUCE_OP_FN = ctypes.CFUNCTYPE(ctypes.c_int, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int, ctypes.c_int,
@@ -82,6 +106,7 @@ def lib():
                                       ctypes.c_uint32, ctypes.c_float)
         dp = ctypes.POINTER(LayerDesc)
         pp = ctypes.POINTER(_Ptrs12)
+        hp = ctypes.POINTER(Heads)
         sigs = {
             "mtnlg_version": (ctypes.c_int, []),
             "mtnlg_status_string": (ctypes.c_char_p, [ctypes.c_int]),
@@ -120,6 +145,19 @@ def lib():
             "mtnlg_colsum_static_max_columns": (i64, []),
             "mtnlg_colsum_static": (ctypes.c_int, [ctypes.c_int, i64, i64, vp, vp, ctypes.c_int, ctypes.c_int, vp]),
             "mtnlg_bias_residual": (ctypes.c_int, [ctypes.c_int, i64, i64, vp, vp, vp, vp, vp]),
+            "mtnlg_rmsnorm_fwd": (ctypes.c_int, [ctypes.c_int, i64, i64, vp, vp, vp, f32, vp, vp, vp, vp]),
+            "mtnlg_rmsnorm_fwd_e4m3": (ctypes.c_int, [ctypes.c_int, i64, i64, vp, vp, vp, f32, i32, vp, vp, vp, vp, vp]),
+            "mtnlg_rmsnorm_bwd_workspace": (sz, [i64, i64]),
+            "mtnlg_rmsnorm_bwd": (ctypes.c_int, [ctypes.c_int, i64, i64, vp, vp, vp, vp, vp, vp, vp, ctypes.c_int, ctypes.c_int,
+                                                 vp, sz, vp]),
+            "mtnlg_rotary_fwd": (ctypes.c_int, [ctypes.POINTER(RotaryDesc), hp, hp, hp, hp, vp, vp]),
+            "mtnlg_rotary_bwd": (ctypes.c_int, [ctypes.POINTER(RotaryDesc), hp, hp, hp, hp, vp, vp]),
+            "mtnlg_packed_attention_fwd_workspace": (sz, [ctypes.POINTER(PackedDesc)]),
+            "mtnlg_packed_attention_fwd": (ctypes.c_int, [ctypes.POINTER(PackedDesc), ctypes.POINTER(PackedSequences), hp, hp, hp, hp,
+                                                          vp, vp, sz, vp]),
+            "mtnlg_packed_attention_bwd_workspace": (sz, [ctypes.POINTER(PackedDesc)]),
+            "mtnlg_packed_attention_bwd": (ctypes.c_int, [ctypes.POINTER(PackedDesc), ctypes.POINTER(PackedSequences), hp, hp, hp, hp,
+                                                          vp, hp, hp, hp, hp, vp, sz, vp]),
             "mtnlg_calibrate_mfma_operand_bytes": (sz, [ctypes.c_int]),
             "mtnlg_calibrate_mfma_flops": (i64, [ctypes.c_int, ctypes.c_int]),
             "mtnlg_calibrate_mfma": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, vp, vp, vp]),
@@ -143,6 +181,9 @@ EXPORTED = ("mtnlg_version", "mtnlg_status_string", "mtnlg_layer_desc_check", "m
             "mtnlg_colsum_workspace", "mtnlg_colsum", "mtnlg_colsum_static_max_columns", "mtnlg_colsum_static",
             "mtnlg_bias_residual", "mtnlg_grad_sqnorm_workspace", "mtnlg_grad_sqnorm", "mtnlg_adam_step",
             "mtnlg_lm_head_workspace", "mtnlg_embedding_fwd", "mtnlg_embedding_bwd", "mtnlg_lm_head_step",
+            "mtnlg_rmsnorm_fwd", "mtnlg_rmsnorm_fwd_e4m3", "mtnlg_rmsnorm_bwd_workspace", "mtnlg_rmsnorm_bwd",
+            "mtnlg_rotary_fwd", "mtnlg_rotary_bwd", "mtnlg_packed_attention_fwd_workspace", "mtnlg_packed_attention_fwd",
+            "mtnlg_packed_attention_bwd_workspace", "mtnlg_packed_attention_bwd",
             "mtnlg_calibrate_mfma_operand_bytes", "mtnlg_calibrate_mfma_flops", "mtnlg_calibrate_mfma",
             "mtnlg_calibrate_copy", "mtnlg_profile_enable", "mtnlg_profile_pause", "mtnlg_profile_read")
 
@@ -424,6 +465,181 @@ def mtnlg_lm_head_step(desc, x, ln_g, ln_b, emb, targets, dloss, loss, dx, d_ln_
     _check(lib().mtnlg_lm_head_step(ctypes.byref(desc), _p(x), _p(ln_g), _p(ln_b), _p(emb), _p(targets), _p(dloss),
                                     _p(loss), _p(dx), _p(d_ln_g), _p(d_ln_b), _p(demb), _p(workspace),
                                     _nbytes(workspace), _op_hook(reduce), None, _stream()), "mtnlg_lm_head_step")
+
+
+def _here(*tensors):
+    """The tensors (None aside) are on the current device, whose current stream the call goes to."""
+    device = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and not (t.is_cuda and t.device.index == device):
+            raise ValueError("tensors handed to the library must be on the current device")
+
+
+def _like(t, dtype, shape, what):
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what}: expected {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+
+
+def _heads(t, kv_heads):
+    """A matrix of heads [tokens, heads, head_dim] or [tokens, kv_heads, heads of a group, head_dim], any strides but the last's."""
+    if t is None:
+        return None
+    if t.dim() not in (3, 4) or t.shape[-1] == 0 or (t.shape[-1] > 1 and t.stride(-1) != 1):
+        raise ValueError("heads: [tokens, heads, head_dim] or [tokens, kv_heads, group, head_dim] with dense rows")
+    if t.dim() == 4:
+        return Heads(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2))
+    return Heads(t.data_ptr(), t.stride(0), t.stride(1) * (t.shape[1] // kv_heads), t.stride(1))
+
+
+def _ref(h):
+    return None if h is None else ctypes.byref(h)
+
+
+def _counts(q, k):
+    """heads, kv_heads, head_dim of a matrix of query heads beside one of key heads."""
+    heads = q.shape[1] if q.dim() == 3 else q.shape[1] * q.shape[2]
+    kv_heads = k.shape[1] if k is not None else q.shape[1]
+    if k is not None and (k.dim() != 3 or k.shape[2] != q.shape[-1] or k.dtype != q.dtype):
+        raise ValueError("keys and values: [tokens, kv_heads, head_dim] of the queries' type and head size")
+    if kv_heads == 0 or heads % kv_heads or (q.dim() == 4 and q.shape[1] != kv_heads):
+        raise ValueError("the number of query heads is a multiple of that of key heads")
+    return heads, kv_heads, q.shape[-1]
+
+
+def mtnlg_rmsnorm_fwd(x, gamma, eps, out, rstd, residual=None, xsum=None):
+    """x, residual, xsum, out: [T, h] (contiguous); rstd: fp32 [T]."""
+    T, h = x.shape
+    _here(x, gamma, out, rstd, residual, xsum)
+    _like(out, x.dtype, (T, h), "out")
+    _like(gamma, x.dtype, (h,), "gamma")
+    _like(rstd, torch.float32, (T,), "rstd")
+    for t, what in ((residual, "residual"), (xsum, "xsum")):
+        if t is not None:
+            _like(t, x.dtype, (T, h), what)
+    _check(lib().mtnlg_rmsnorm_fwd(_dtype_code(x), T, h, _p(x), _p(residual), _p(gamma), eps, _p(xsum), _p(out), _p(rstd), _stream()),
+           "mtnlg_rmsnorm_fwd")
+
+
+def mtnlg_rmsnorm_fwd_e4m3(x, gamma, eps, out, scale, rstd, columns=0, residual=None, xsum=None):
+    """out: e4m3 [T, h]; scale: fp32 [T, number of groups of `columns` columns] (columns 0: one to a row)."""
+    T, h = x.shape
+    _here(x, gamma, out, scale, rstd, residual, xsum)
+    _like(out, torch.float8_e4m3fn, (T, h), "out")
+    _like(gamma, x.dtype, (h,), "gamma")
+    _like(scale, torch.float32, (T, -(-h // columns) if columns > 0 else 1), "scale")
+    _like(rstd, torch.float32, (T,), "rstd")
+    for t, what in ((residual, "residual"), (xsum, "xsum")):
+        if t is not None:
+            _like(t, x.dtype, (T, h), what)
+    _check(lib().mtnlg_rmsnorm_fwd_e4m3(_dtype_code(x), T, h, _p(x), _p(residual), _p(gamma), eps, columns, _p(xsum), _p(out), _p(scale),
+                                        _p(rstd), _stream()), "mtnlg_rmsnorm_fwd_e4m3")
+
+
+def mtnlg_rmsnorm_bwd_workspace(T, h):
+    return lib().mtnlg_rmsnorm_bwd_workspace(T, h)
+
+
+def mtnlg_rmsnorm_bwd(x, gamma, rstd, dout, dx, dgamma, workspace, dres=None, accumulate=False):
+    """x: what was normalised; dgamma: [h], fp32 or x's type."""
+    T, h = x.shape
+    _here(x, gamma, rstd, dout, dx, dgamma, workspace, dres)
+    for t, what in ((dout, "dout"), (dx, "dx"), (dres, "dres")):
+        if t is not None:
+            _like(t, x.dtype, (T, h), what)
+    _like(gamma, x.dtype, (h,), "gamma")
+    _like(rstd, torch.float32, (T,), "rstd")
+    _like(dgamma, torch.float32 if dgamma.dtype == torch.float32 else x.dtype, (h,), "dgamma")
+    _check(lib().mtnlg_rmsnorm_bwd(_dtype_code(x), T, h, _p(x), _p(gamma), _p(rstd), _p(dout), _p(dres), _p(dx), _p(dgamma),
+                                   int(dgamma.dtype == torch.float32), int(accumulate), _p(workspace), _nbytes(workspace), _stream()),
+           "mtnlg_rmsnorm_bwd")
+
+
+def rotary_desc(rotary_dim, layout=ROTARY_HALF, base=10000.0, scaling=ROTARY_UNSCALED, factor=1.0, original_positions=0, slow=1.0,
+                fast=32.0, amplitude=0.0):
+    """How heads turn; their number, size and type come from the tensors of the call."""
+    return RotaryDesc(0, 0, 0, 0, rotary_dim, layout, scaling, original_positions, 0, base, factor, slow, fast, amplitude)
+
+
+def _rotary(name, desc, q, k, q_out, k_out, positions):
+    if q.dim() not in (3, 4):
+        raise ValueError("heads: [tokens, heads, head_dim] or [tokens, kv_heads, group, head_dim]")
+    heads, kv_heads, d = _counts(q, k)
+    _here(q, k, q_out, k_out, positions)
+    if (k is None) != (k_out is None):
+        raise ValueError("keys go with an output of theirs")
+    _like(q_out, q.dtype, q.shape, "the output of the queries")
+    if k is not None:
+        if k.shape[0] != q.shape[0]:
+            raise ValueError("queries and keys of the same tokens")
+        _like(k_out, k.dtype, k.shape, "the output of the keys")
+    if positions is not None:
+        _like(positions, torch.int32, (q.shape[0],), "positions")
+    full = RotaryDesc(_dtype_code(q), heads, kv_heads, d, desc.rotary_dim, desc.layout, desc.scaling, desc.original_positions,
+                      q.shape[0], desc.base, desc.factor, desc.slow, desc.fast, desc.amplitude)
+    _check(getattr(lib(), name)(ctypes.byref(full), _ref(_heads(q, kv_heads)), _ref(_heads(k, kv_heads)), _ref(_heads(q_out, kv_heads)),
+                                _ref(_heads(k_out, kv_heads)), _p(positions), _stream()), name)
+
+
+def mtnlg_rotary_fwd(desc, q, k, q_out, k_out, positions=None):
+    """q: [tokens, heads, head_dim] or [tokens, kv_heads, group, head_dim], k (nullable): [tokens, kv_heads, head_dim]; positions: int32 [tokens]."""
+    _rotary("mtnlg_rotary_fwd", desc, q, k, q_out, k_out, positions)
+
+
+def mtnlg_rotary_bwd(desc, dq_out, dk_out, dq, dk, positions=None):
+    _rotary("mtnlg_rotary_bwd", desc, dq_out, dk_out, dq, dk, positions)
+
+
+def packed_desc(q, k, sequences, max_q, max_k, scale=0.0):
+    """Sizes of calls of attention over packed sequences: q [tokens, heads, head_dim] or [tokens, kv_heads, group, head_dim], k [tokens, kv_heads, head_dim]."""
+    heads, kv_heads, d = _counts(q, k)
+    return PackedDesc(_dtype_code(q), heads, kv_heads, d, sequences, max_q, max_k, q.shape[0], k.shape[0], scale)
+
+
+def mtnlg_packed_attention_fwd_workspace(desc):
+    return lib().mtnlg_packed_attention_fwd_workspace(ctypes.byref(desc))
+
+
+def mtnlg_packed_attention_bwd_workspace(desc):
+    return lib().mtnlg_packed_attention_bwd_workspace(ctypes.byref(desc))
+
+
+def _packed(q, k, v, a, lse, q_offsets, k_offsets, max_q, max_k, scale, q_lengths, k_lengths):
+    if q.dim() not in (3, 4) or k is None:
+        raise ValueError("heads: [tokens, heads, head_dim] or [tokens, kv_heads, group, head_dim]")
+    desc = packed_desc(q, k, q_offsets.shape[0] - 1, max_q, max_k, scale)
+    _here(q, k, v, a, lse, q_offsets, k_offsets, q_lengths, k_lengths)
+    _like(v, k.dtype, k.shape, "v")
+    _like(a, q.dtype, q.shape, "a")
+    _like(lse, torch.float32, (desc.heads, q.shape[0]), "lse")
+    for t, n, what in ((q_offsets, desc.sequences + 1, "q_offsets"), (k_offsets, desc.sequences + 1, "k_offsets"),
+                       (q_lengths, desc.sequences, "q_lengths"), (k_lengths, desc.sequences, "k_lengths")):
+        if t is not None:
+            _like(t, torch.int32, (n,), what)
+    return desc, PackedSequences(_p(q_offsets), _p(k_offsets), _p(q_lengths), _p(k_lengths))
+
+
+def mtnlg_packed_attention_fwd(q, k, v, a, lse, q_offsets, k_offsets, max_q, max_k, scale=0.0, q_lengths=None, k_lengths=None,
+                               workspace=None):
+    """q, a: [tokens, heads, head_dim] or [tokens, kv_heads, group, head_dim]; k, v: [tokens, kv_heads, head_dim]; lse: fp32 [heads, tokens];
+    offsets: int32 [sequences + 1] on the device, lengths (nullable) [sequences]; max_q, max_k: no sequence is longer."""
+    desc, where = _packed(q, k, v, a, lse, q_offsets, k_offsets, max_q, max_k, scale, q_lengths, k_lengths)
+    _here(workspace)
+    n = desc.kv_heads
+    _check(lib().mtnlg_packed_attention_fwd(ctypes.byref(desc), ctypes.byref(where), _ref(_heads(q, n)), _ref(_heads(k, n)), _ref(_heads(v, n)),
+                                            _ref(_heads(a, n)), _p(lse), _p(workspace), _nbytes(workspace) if workspace is not None else 0,
+                                            _stream()), "mtnlg_packed_attention_fwd")
+
+
+def mtnlg_packed_attention_bwd(q, k, v, a, lse, da, dq, dk, dv, q_offsets, k_offsets, max_q, max_k, workspace, scale=0.0, q_lengths=None,
+                               k_lengths=None):
+    desc, where = _packed(q, k, v, a, lse, q_offsets, k_offsets, max_q, max_k, scale, q_lengths, k_lengths)
+    _here(da, dq, dk, dv, workspace)
+    for t, like, what in ((da, q, "da"), (dq, q, "dq"), (dk, k, "dk"), (dv, k, "dv")):
+        _like(t, like.dtype, like.shape, what)
+    n = desc.kv_heads
+    _check(lib().mtnlg_packed_attention_bwd(ctypes.byref(desc), ctypes.byref(where), _ref(_heads(q, n)), _ref(_heads(k, n)), _ref(_heads(v, n)),
+                                            _ref(_heads(a, n)), _p(lse), _ref(_heads(da, n)), _ref(_heads(dq, n)), _ref(_heads(dk, n)),
+                                            _ref(_heads(dv, n)), _p(workspace), _nbytes(workspace), _stream()), "mtnlg_packed_attention_bwd")
 
 
 def mtnlg_grad_sqnorm_workspace():

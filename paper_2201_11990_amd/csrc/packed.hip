@@ -1,0 +1,247 @@
+// Attention over packed sequences with grouped heads: how calls are cut into workgroups, the kernels that join what was cut, and the entry points.
+#include "packed.h"
+
+namespace mtnlg {
+
+namespace {
+
+// A row's results from those of its chunks: a wave to a row, four columns to a lane.
+template <typename E>
+__global__ __launch_bounds__(256) void packed_join_kernel(PackedFwdArgs w) {
+  const int lane = threadIdx.x & 63, r = w.group, d = w.d, j = blockIdx.x % w.kv_heads;
+  Span s;
+  unsigned at;
+  if (!find_piece(w.where, blockIdx.x / w.kv_heads, [&](const Span &s) { return (unsigned)((s.lq * r + 3) / 4); }, s, at)) return;
+  const int row = at * 4 + (threadIdx.x >> 6);
+  if (row >= s.lq * r) return;
+  const int tok = row / r, g = row - tok * r, head = j * r + g, limit = min(tok + s.lk - s.lq, s.lk - 1);
+  const int nc = min(limit < 0 ? 0 : limit / w.chunk + 1, w.chunks);
+  const int64_t all = (int64_t)w.where.q_tokens * w.kv_heads * r, id = (int64_t)(s.q0 + tok) * ((int64_t)w.kv_heads * r) + head;
+  float m = -INFINITY, l = 0.0f;
+  if (lane < nc) {
+    const float2 t = *reinterpret_cast<const float2 *>(w.stat + 2 * (lane * all + id));
+    m = t.x;
+    l = t.y;
+  }
+  const float most = wave_max(m), ref = most == -INFINITY ? 0.0f : most;
+  const float mul = sizeof(E) == 4 ? exact_exp(product_of(m, w.scale) - product_of(ref, w.scale)) : fast_exp2((m - ref) * (w.scale * kLog2e));
+  const float total = wave_sum(l * mul);
+  f32x4 o = {};
+  const float *from = w.part + id * d + (lane * 4 < d ? lane * 4 : 0);   // lanes past the columns go along: the others take the chunks' factors from them
+  for (int i = 0; i < nc; ++i) o += *reinterpret_cast<const f32x4 *>(from + i * all * d) * __shfl(mul, i, 64);
+  if (lane * 4 < d) put4(row_at<E>(w.a, s.q0 + tok, j, g) + lane * 4, o * (nc ? 1.0f / total : 0.0f));
+  if (lane == 0) w.lse[(int64_t)head * w.where.q_tokens + s.q0 + tok] = nc ? plus_log(product_of(most, w.scale), total) : -INFINITY;
+}
+
+// The parts of a group added up: a wave to a key, four columns of dv (lower half of the lanes' columns) and dk to a lane in turn.
+template <typename E>
+__global__ __launch_bounds__(256) void packed_dkv_join_kernel(PackedBwdArgs w) {
+  const int lane = threadIdx.x & 63, d = w.d, j = blockIdx.x % w.kv_heads;
+  Span s;
+  unsigned at;
+  if (!find_piece(w.where, blockIdx.x / w.kv_heads, [&](const Span &s) { return (unsigned)((s.lk + 15) / 16); }, s, at)) return;
+  const int64_t all = (int64_t)w.where.k_tokens * w.kv_heads * (2 * d);
+  for (int i = threadIdx.x >> 6; i < 16; i += 4) {
+    const int key = at * 16 + i;
+    if (key >= s.lk) return;
+    const float *from = w.part + ((int64_t)(s.k0 + key) * w.kv_heads + j) * (2 * d);
+    for (int col = lane * 4; col < 2 * d; col += 256) {
+      f32x4 v = *reinterpret_cast<const f32x4 *>(from + col);
+      for (int p = 1; p < w.splits; ++p) v += *reinterpret_cast<const f32x4 *>(from + p * all + col);
+      put4(col < d ? row_at<E>(w.dv, s.k0 + key, j, 0) + col : row_at<E>(w.dk, s.k0 + key, j, 0) + (col - d), v);
+    }
+  }
+}
+
+// How the keys are cut where the rows alone leave most of the chip idle.
+struct FwdPlan {
+  int owned;
+  int64_t pieces;   // workgroups of a head of keys at most, without cuts
+  int chunk, chunks;
+  size_t part_bytes, bytes;
+};
+FwdPlan fwd_plan(const PackedShape &S) {
+  FwdPlan p{};
+  const int64_t rows = (int64_t)S.where.q_tokens * S.group, most = (int64_t)S.max_q * S.group;
+  p.owned = 128;
+  p.pieces = pieces_bound(rows, most, S.where.count, p.owned);
+  if (S.dtype == MTNLG_BF16 && p.pieces * S.kv_heads < 1024) {
+    p.owned = 64;
+    p.pieces = pieces_bound(rows, most, S.where.count, p.owned);
+  }
+  p.chunks = 1;
+  const int64_t wide = p.pieces * S.kv_heads;
+  if (wide < 256 && S.max_k > 512) {
+    int64_t chunk = (int64_t)S.max_k * wide / 1024;   // about four to a unit
+    chunk = chunk < 256 ? 256 : chunk;
+    if (chunk * 64 < S.max_k) chunk = (S.max_k + 63) / 64;
+    chunk = (chunk + 63) / 64 * 64;
+    p.chunk = (int)chunk;
+    p.chunks = (int)((S.max_k + chunk - 1) / chunk);
+    const size_t all = (size_t)S.where.q_tokens * S.heads;
+    p.part_bytes = align_up(p.chunks * all * S.d * sizeof(float), 256);
+    p.bytes = p.part_bytes + align_up(p.chunks * all * 2 * sizeof(float), 256);
+    if (p.chunks == 1) p.chunk = 0, p.bytes = 0;
+  }
+  return p;
+}
+
+bool unaligned(const mtnlg_packed_sequences *w) {
+  return (((uintptr_t)w->q_offsets | (uintptr_t)w->k_offsets | (uintptr_t)w->q_lengths | (uintptr_t)w->k_lengths) & 3) != 0;
+}
+
+struct BwdPlan {
+  int owned, splits;         // rows of a dq workgroup; parts of a group
+  int64_t pieces, key_pieces;
+  size_t d_bytes, bytes;
+};
+BwdPlan bwd_plan(const PackedShape &S) {
+  BwdPlan p{};
+  const int64_t rows = (int64_t)S.where.q_tokens * S.group, most = (int64_t)S.max_q * S.group;
+  p.owned = 128;
+  p.pieces = pieces_bound(rows, most, S.where.count, p.owned);
+  if (S.dtype == MTNLG_BF16 && p.pieces * S.kv_heads < 1024) {
+    p.owned = 64;
+    p.pieces = pieces_bound(rows, most, S.where.count, p.owned);
+  }
+  p.key_pieces = pieces_bound(S.where.k_tokens, S.max_k, S.where.count, packed_dkv_owned(S.dtype, S.d));
+  const int64_t wide = p.key_pieces * S.kv_heads, splits = (512 + wide - 1) / wide;
+  p.splits = (int)(splits < S.group ? splits : S.group);
+  p.d_bytes = align_up((size_t)S.where.q_tokens * S.heads * sizeof(float), 256);
+  p.bytes = p.d_bytes + (p.splits > 1 ? (size_t)p.splits * S.where.k_tokens * S.kv_heads * 2 * S.d * sizeof(float) : 0);
+  return p;
+}
+
+}  // namespace
+
+int packed_shape(const mtnlg_packed_desc *D, PackedShape *S) {
+  if (!D) return MTNLG_NULL_POINTER;
+  if (D->dtype != MTNLG_F32 && D->dtype != MTNLG_BF16) return MTNLG_INVALID_ARG;
+  if (D->heads <= 0 || D->kv_heads <= 0 || D->heads % D->kv_heads || D->head_dim <= 0 || D->sequences <= 0) return MTNLG_INVALID_ARG;
+  if (D->q_tokens <= 0 || D->k_tokens <= 0 || D->max_q <= 0 || D->max_k <= 0) return MTNLG_INVALID_ARG;
+  if (!(D->scale >= 0.0f && D->scale < INFINITY)) return MTNLG_INVALID_ARG;
+  if (D->head_dim % 8 || D->head_dim > 256 || D->heads > 65535 || D->sequences > 1 << 20) return MTNLG_UNSUPPORTED_SHAPE;
+  if (D->q_tokens > 0x7FFFFFFF || D->k_tokens > 0x7FFFFFFF) return MTNLG_UNSUPPORTED_SHAPE;
+  if (D->q_tokens * D->heads > 0x7FFFFFFF || D->k_tokens * D->kv_heads > 0x7FFFFFFF) return MTNLG_UNSUPPORTED_SHAPE;   // rows are counted in 32 bits
+  *S = PackedShape{D->dtype, D->heads, D->kv_heads, D->heads / D->kv_heads, D->head_dim, D->scale > 0.0f ? D->scale : 1.0f / sqrtf((float)D->head_dim),
+                   Sequences{nullptr, nullptr, nullptr, nullptr, D->sequences, (int)D->q_tokens, (int)D->k_tokens}, D->max_q, D->max_k};
+  // no sequence is longer than the matrix
+  if (S->max_q > S->where.q_tokens) S->max_q = S->where.q_tokens;
+  if (S->max_k > S->where.k_tokens) S->max_k = S->where.k_tokens;
+  return MTNLG_OK;
+}
+
+}  // namespace mtnlg
+
+using namespace mtnlg;
+
+extern "C" {
+
+size_t mtnlg_packed_attention_fwd_workspace(const mtnlg_packed_desc *desc) {
+  PackedShape S;
+  return packed_shape(desc, &S) == MTNLG_OK ? fwd_plan(S).bytes : 0;
+}
+
+int mtnlg_packed_attention_fwd(const mtnlg_packed_desc *desc, const mtnlg_packed_sequences *where, const mtnlg_heads *q, const mtnlg_heads *k,
+                               const mtnlg_heads *v, const mtnlg_heads *a, float *lse, void *workspace, size_t workspace_bytes, void *stream) {
+  if (!where || !where->q_offsets || !where->k_offsets || !q || !k || !v || !a || !q->data || !k->data || !v->data || !a->data || !lse) return MTNLG_NULL_POINTER;
+  PackedShape S;
+  MTNLG_TRY(packed_shape(desc, &S));
+  MTNLG_TRY(heads_check(q, S.where.q_tokens, S.kv_heads, S.group, S.d, S.dtype));
+  MTNLG_TRY(heads_check(a, S.where.q_tokens, S.kv_heads, S.group, S.d, S.dtype));
+  MTNLG_TRY(heads_check(k, S.where.k_tokens, S.kv_heads, 1, S.d, S.dtype));
+  MTNLG_TRY(heads_check(v, S.where.k_tokens, S.kv_heads, 1, S.d, S.dtype));
+  if (a->data == q->data || a->data == k->data || a->data == v->data) return MTNLG_INVALID_ARG;
+  if (((uintptr_t)lse & 3) || ((uintptr_t)workspace & 15) || unaligned(where)) return MTNLG_INVALID_ARG;
+  FwdPlan plan = fwd_plan(S);
+  if (!workspace || plan.bytes == 0) {   // without scratch: no cuts
+    plan.chunk = 0;
+    plan.chunks = 1;
+  } else if (workspace_bytes < plan.bytes) {
+    return MTNLG_WORKSPACE_TOO_SMALL;
+  }
+  PackedFwdArgs w{};
+  w.where = Sequences{where->q_offsets, where->k_offsets, where->q_lengths, where->k_lengths, S.where.count, S.where.q_tokens, S.where.k_tokens};
+  w.kv_heads = S.kv_heads;
+  w.group = S.group;
+  w.d = S.d;
+  w.chunk = plan.chunk;
+  w.chunks = plan.chunks;
+  w.scale = S.scale;
+  w.q = heads_of(q, S.where.q_tokens, S.d);
+  w.k = heads_of(k, S.where.k_tokens, S.d);
+  w.v = heads_of(v, S.where.k_tokens, S.d);
+  w.a = heads_of(a, S.where.q_tokens, S.d);
+  w.lse = lse;
+  w.part = (float *)workspace;
+  w.stat = (float *)((char *)workspace + plan.part_bytes);
+  int64_t pieces = plan.pieces;
+  if (plan.chunks > 1) {   // all keys in chunks and the last ones of each sequence, for every block that a sequence can have
+    const int64_t blocks_of = ((int64_t)S.max_q * S.group + plan.owned - 1) / plan.owned, by_keys = blocks_of * (S.where.k_tokens / plan.chunk + S.where.count);
+    pieces = pieces * plan.chunks < by_keys ? pieces * plan.chunks : by_keys;
+  }
+  const int64_t blocks = pieces * S.kv_heads;
+  if (blocks > 0x7FFFFFFF) return MTNLG_UNSUPPORTED_SHAPE;
+  const hipStream_t st = (hipStream_t)stream;
+  LaunchScope scope(MTNLG_K_ATTN_FWD, st);
+  MTNLG_TRY(S.dtype == MTNLG_F32 ? packed_fwd_f32(w, blocks, st) : packed_fwd_bf16(w, plan.owned, blocks, st));
+  if (plan.chunks == 1) return MTNLG_OK;
+  const unsigned joins = (unsigned)(pieces_bound((int64_t)S.where.q_tokens * S.group, (int64_t)S.max_q * S.group, S.where.count, 4) * S.kv_heads);
+  if (S.dtype == MTNLG_F32) packed_join_kernel<float><<<joins, 256, 0, st>>>(w);
+  else packed_join_kernel<bf16><<<joins, 256, 0, st>>>(w);
+  return check_launch();
+}
+
+
+size_t mtnlg_packed_attention_bwd_workspace(const mtnlg_packed_desc *desc) {
+  PackedShape S;
+  return packed_shape(desc, &S) == MTNLG_OK ? bwd_plan(S).bytes : 0;
+}
+
+int mtnlg_packed_attention_bwd(const mtnlg_packed_desc *desc, const mtnlg_packed_sequences *where, const mtnlg_heads *q, const mtnlg_heads *k,
+                               const mtnlg_heads *v, const mtnlg_heads *a, const float *lse, const mtnlg_heads *da, const mtnlg_heads *dq,
+                               const mtnlg_heads *dk, const mtnlg_heads *dv, void *workspace, size_t workspace_bytes, void *stream) {
+  if (!where || !where->q_offsets || !where->k_offsets || !lse || !workspace) return MTNLG_NULL_POINTER;
+  for (const mtnlg_heads *m : {q, k, v, a, da, dq, dk, dv})
+    if (!m || !m->data) return MTNLG_NULL_POINTER;
+  PackedShape S;
+  MTNLG_TRY(packed_shape(desc, &S));
+  for (const mtnlg_heads *m : {q, a, da, dq}) MTNLG_TRY(heads_check(m, S.where.q_tokens, S.kv_heads, S.group, S.d, S.dtype));
+  for (const mtnlg_heads *m : {k, v, dk, dv}) MTNLG_TRY(heads_check(m, S.where.k_tokens, S.kv_heads, 1, S.d, S.dtype));
+  for (const mtnlg_heads *m : {dq, dk, dv})
+    for (const mtnlg_heads *in : {q, k, v, a, da})
+      if (m->data == in->data) return MTNLG_INVALID_ARG;
+  if (dq->data == dk->data || dq->data == dv->data || dk->data == dv->data) return MTNLG_INVALID_ARG;
+  if (((uintptr_t)lse & 3) || ((uintptr_t)workspace & 15) || unaligned(where)) return MTNLG_INVALID_ARG;
+  const BwdPlan plan = bwd_plan(S);
+  if (workspace_bytes < plan.bytes) return MTNLG_WORKSPACE_TOO_SMALL;
+  if (plan.pieces * S.kv_heads > 0x7FFFFFFF || plan.key_pieces * plan.splits * S.kv_heads > 0x7FFFFFFF) return MTNLG_UNSUPPORTED_SHAPE;
+  PackedBwdArgs w{};
+  w.where = Sequences{where->q_offsets, where->k_offsets, where->q_lengths, where->k_lengths, S.where.count, S.where.q_tokens, S.where.k_tokens};
+  w.kv_heads = S.kv_heads;
+  w.group = S.group;
+  w.d = S.d;
+  w.splits = plan.splits;
+  w.scale = S.scale;
+  w.q = heads_of(q, S.where.q_tokens, S.d);
+  w.k = heads_of(k, S.where.k_tokens, S.d);
+  w.v = heads_of(v, S.where.k_tokens, S.d);
+  w.a = heads_of(a, S.where.q_tokens, S.d);
+  w.da = heads_of(da, S.where.q_tokens, S.d);
+  w.dq = heads_of(dq, S.where.q_tokens, S.d);
+  w.dk = heads_of(dk, S.where.k_tokens, S.d);
+  w.dv = heads_of(dv, S.where.k_tokens, S.d);
+  w.lse = lse;
+  w.D = (float *)workspace;
+  w.part = (float *)((char *)workspace + plan.d_bytes);
+  const hipStream_t st = (hipStream_t)stream;
+  LaunchScope scope(MTNLG_K_ATTN_BWD, st);
+  MTNLG_TRY(S.dtype == MTNLG_F32 ? packed_bwd_f32(w, plan.pieces, plan.key_pieces, st) : packed_bwd_bf16(w, plan.owned, plan.pieces, plan.key_pieces, st));
+  if (plan.splits == 1) return MTNLG_OK;
+  const unsigned joins = (unsigned)(pieces_bound(S.where.k_tokens, S.max_k, S.where.count, 16) * S.kv_heads);
+  if (S.dtype == MTNLG_F32) packed_dkv_join_kernel<float><<<joins, 256, 0, st>>>(w);
+  else packed_dkv_join_kernel<bf16><<<joins, 256, 0, st>>>(w);
+  return check_launch();
+}
+
+}  // extern "C"

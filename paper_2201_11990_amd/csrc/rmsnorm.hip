@@ -1,0 +1,374 @@
+// Root-mean-square norm (Zhang and Sennrich, "Root mean square layer normalization", 2019) with the residual's addition before it:
+//   s = x [+ residual] (stored, in the storage type),  r = 1 / sqrt(mean(s^2) + eps),  out = s r gamma,
+// the same with the result in 8 bits (e4m3) and a scale to every row or every so many columns, and the backward pass
+//   dn = dout gamma,  n = s r,  dx = dres + r (dn - n mean(dn n)),  dgamma = sum over rows of dout n.
+// All bound by memory: every matrix is read or written once, a row stays in registers between its reduction and its result.
+#include "common.h"
+
+namespace mtnlg {
+
+namespace {
+
+constexpr int MAX_COLUMNS = 32768;
+constexpr float E4M3_MOST = 448.0f;
+
+// How a row is shared out: W waves to a row (1, 4 or 16), NV pieces of 8 columns to a lane.  One wave needs no barrier and keeps up to eight
+// loads of a row in flight, so it takes rows up to 2048 columns.
+template <int W> constexpr int threads_of() { return W < 4 ? 256 : 64 * W; }
+
+// Sum over the W waves of a row; the same in every lane.
+template <int W>
+__device__ __forceinline__ float row_sum(float v, float *lds) {
+  v = wave_sum(v);
+  if constexpr (W > 1) {
+    __syncthreads();   // lds may still be read from the last time
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = 0.0f;
+#pragma unroll
+    for (int i = 0; i < W; ++i) v += lds[i];
+  }
+  return v;
+}
+template <int W>
+__device__ __forceinline__ float row_max(float v, float *lds) {
+  v = wave_max(v);
+  if constexpr (W > 1) {
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = lds[0];
+#pragma unroll
+    for (int i = 1; i < W; ++i) v = fmaxf(v, lds[i]);
+  }
+  return v;
+}
+
+struct NormArgs {
+  int64_t rows;
+  int h;
+  const void *x, *residual, *gamma;
+  void *xsum, *out;
+  float eps;
+  float *rstd, *scale;
+  int columns, scales;   // 8 bits: columns that share a scale (0: the row), scales of a row
+};
+
+// y to the nearest value of e4m3, beyond 448 to 448 (NaN stays NaN).  The instruction rounds to nearest even.
+__device__ __forceinline__ unsigned e4m3_of4(float a, float b, float c, float d) {
+  auto within = [](float y) { return y > E4M3_MOST ? E4M3_MOST : y < -E4M3_MOST ? -E4M3_MOST : y; };
+  int w = __builtin_amdgcn_cvt_pk_fp8_f32(within(a), within(b), 0, false);
+  return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(within(c), within(d), w, true);
+}
+
+template <typename E, int W, int NV, bool E4M3>
+__global__ __launch_bounds__(threads_of<W>()) void rmsnorm_fwd_kernel(NormArgs a) {
+  __shared__ float red[16];
+  constexpr int LANES = 64 * W, ROWS = threads_of<W>() / LANES;
+  const int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / LANES;
+  if (ROWS > 1 && row >= a.rows) return;   // whole waves
+  const int at = threadIdx.x % LANES, nvec = a.h / 8;
+  const E *x = static_cast<const E *>(a.x) + row * a.h, *res = static_cast<const E *>(a.residual) + row * a.h;
+  Raw8<E> xv[NV], rv[NV];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int j = at + i * LANES;
+    if (j < nvec) {
+      xv[i].load(x + 8 * j);
+      if (a.residual) rv[i].load(res + 8 * j);
+    }
+  }
+  float v[NV][8], sum = 0.0f;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int j = at + i * LANES;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[i][e] = j < nvec ? xv[i][e] : 0.0f;
+    if (j < nvec && a.residual) {
+      // what is normalised is the sum as it is stored, which the backward pass is given
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[i][e] = to_f32(from_f32<E>(v[i][e] + rv[i][e]));
+      store8(static_cast<E *>(a.xsum) + row * a.h + 8 * j, v[i]);
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum += v[i][e] * v[i][e];
+  }
+  const float r = 1.0f / sqrtf(row_sum<W>(sum, red) / (float)a.h + a.eps);
+  if (at == 0) a.rstd[row] = r;
+  const E *gamma = static_cast<const E *>(a.gamma);
+  float most = 0.0f;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int j = at + i * LANES;
+    if (j < nvec) {
+      float g[8];
+      load8(gamma + 8 * j, g);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        v[i][e] = v[i][e] * r * g[e];
+        most = fmaxf(most, fabsf(v[i][e]));
+      }
+      if constexpr (!E4M3) store8(static_cast<E *>(a.out) + row * a.h + 8 * j, v[i]);
+    }
+  }
+  if constexpr (E4M3) {
+    if (a.columns == 0) most = row_max<W>(most, red);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int j = at + i * LANES;
+      float m = most;
+      if (a.columns != 0) {   // columns is 8 times a power of two up to 64: lanes that share a scale lie side by side
+        m = 0.0f;
+        if (j < nvec) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(v[i][e]));
+        }
+        for (int off = 1; off < a.columns / 8; off *= 2) m = fmaxf(m, __shfl_xor(m, off, 64));
+      }
+      if (j >= nvec) continue;
+      const float scale = m > 0.0f ? m / E4M3_MOST : 1.0f;
+      const int first = a.columns ? 8 * j % a.columns : j;
+      if (first == 0) a.scale[row * a.scales + (a.columns ? 8 * j / a.columns : 0)] = scale;
+      float y[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] = v[i][e] / scale;
+      *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(a.out) + row * a.h + 8 * j) =
+          uint2{e4m3_of4(y[0], y[1], y[2], y[3]), e4m3_of4(y[4], y[5], y[6], y[7])};
+    }
+  }
+}
+
+template <typename E, bool E4M3>
+int fwd_launch(const NormArgs &a, hipStream_t st) {
+  const int nvec = a.h / 8;
+  LaunchScope scope(MTNLG_K_LN_FWD, st);
+#define RMS(W, NV) \
+  rmsnorm_fwd_kernel<E, W, NV, E4M3><<<(unsigned)((a.rows + threads_of<W>() / (64 * W) - 1) / (threads_of<W>() / (64 * W))), threads_of<W>(), 0, st>>>(a)
+  if (nvec <= 64) RMS(1, 1);
+  else if (nvec <= 128) RMS(1, 2);
+  else if (nvec <= 256) RMS(1, 4);
+  else if (nvec <= 512) RMS(4, 2);
+  else if (nvec <= 1024) RMS(4, 4);
+  else if (nvec <= 2048) RMS(16, 2);
+  else if (nvec <= 3072) RMS(16, 3);
+  else RMS(16, 4);
+#undef RMS
+  return check_launch();
+}
+
+// ------------------------------------------------------------------ backward
+struct NormBwdArgs {
+  int64_t rows;
+  int h;
+  const void *x, *gamma, *dout, *dres;
+  const float *rstd;
+  void *dx;
+  float *partial;   // [workgroups][h]: the workgroup's rows of dgamma
+};
+
+// A workgroup takes every gridDim.x-th row (of each of its ROWS groups of waves) and sums its share of dgamma in registers.  bf16: the next row is
+// requested before the present one is reduced, so the loads of a row travel behind the barriers of the other; a row of fp32 has no registers for that.
+template <typename E, int W, int NV>
+__global__ __launch_bounds__(threads_of<W>()) void rmsnorm_bwd_kernel(NormBwdArgs a) {
+  constexpr int LANES = 64 * W, ROWS = threads_of<W>() / LANES;
+  constexpr bool AHEAD = sizeof(E) == 2;
+  __shared__ float red[16];
+  __shared__ __attribute__((aligned(16))) float side[ROWS > 1 ? (ROWS - 1) * LANES * NV * 8 : 1];
+  const int at = threadIdx.x % LANES, group = threadIdx.x / LANES, nvec = a.h / 8;
+  const int64_t step = (int64_t)gridDim.x * ROWS;
+  struct Row { Raw8<E> x[NV], dout[NV]; };
+  float dg[NV][8] = {};
+  auto request = [&](int64_t row, Row &to) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int j = at + i * LANES;
+      if (j < nvec && row < a.rows) {
+        to.x[i].load(static_cast<const E *>(a.x) + row * a.h + 8 * j);
+        to.dout[i].load(static_cast<const E *>(a.dout) + row * a.h + 8 * j);
+      }
+    }
+  };
+  int64_t row = (int64_t)blockIdx.x * ROWS + group;
+  Row next;
+  if constexpr (AHEAD) request(row, next);
+  const E *gamma = static_cast<const E *>(a.gamma);
+  // the same number of turns for all waves of a row's group; a group without a row left has none
+  for (; row < a.rows; row += step) {
+    const float r = a.rstd[row];
+    asm volatile("" : "+s"(gamma));   // read again for every row, from the caches: its values in registers would leave none for a row ahead
+    Row now;
+    if constexpr (AHEAD) {
+      now = next;
+      request(row + step, next);
+    } else {
+      request(row, now);
+    }
+    Raw8<E> dres[NV];
+    if (AHEAD && a.dres) {   // fp32: after the reduction, where the registers of the products are free
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+        if (at + i * LANES < nvec) dres[i].load(static_cast<const E *>(a.dres) + row * a.h + 8 * (at + i * LANES));
+    }
+    float dot = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int j = at + i * LANES;
+      if (j < nvec) {
+        float g[8];
+        load8(gamma + 8 * j, g);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float n = now.x[i][e] * r;
+          dot += now.dout[i][e] * g[e] * n;
+          dg[i][e] += now.dout[i][e] * n;
+        }
+      }
+    }
+    const float mean = row_sum<W>(dot, red) / (float)a.h;
+    asm volatile("" : "+s"(gamma));
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int j = at + i * LANES;
+      if (j < nvec) {
+        float g[8], o[8];
+        load8(gamma + 8 * j, g);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          o[e] = r * (now.dout[i][e] * g[e] - now.x[i][e] * r * mean);
+        }
+        if (a.dres) {
+          if constexpr (!AHEAD) dres[i].load(static_cast<const E *>(a.dres) + row * a.h + 8 * j);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) o[e] += dres[i][e];
+        }
+        store8(static_cast<E *>(a.dx) + row * a.h + 8 * j, o);
+      }
+    }
+  }
+  if constexpr (ROWS > 1) {   // the groups' sums, in their order
+    if (group > 0) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; e += 4)
+          *reinterpret_cast<f32x4 *>(side + (((group - 1) * NV + i) * 2 + e / 4) * LANES * 4 + at * 4) = f32x4{dg[i][e], dg[i][e + 1], dg[i][e + 2], dg[i][e + 3]};
+    }
+    __syncthreads();
+    if (group > 0) return;
+#pragma unroll
+    for (int s = 0; s < ROWS - 1; ++s)
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) dg[i][e] += side[((s * NV + i) * 2 + e / 4) * LANES * 4 + at * 4 + e % 4];
+  }
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+    if (at + i * LANES < nvec) store8(a.partial + (int64_t)blockIdx.x * a.h + 8 * (at + i * LANES), dg[i]);
+}
+
+// dgamma from the workgroups' sums: 32 columns to a workgroup, 8 lanes across them, 32 down; a fixed order
+template <typename O>
+__global__ __launch_bounds__(256) void rmsnorm_dgamma_kernel(int rows, int h, const float *__restrict__ partial, O *__restrict__ dgamma, int accumulate) {
+  __shared__ f32x4 side[32][8];
+  const int lane = threadIdx.x % 8, down = threadIdx.x / 8, col = blockIdx.x * 32 + lane * 4;
+  f32x4 s = {};
+  if (col < h) {
+#pragma unroll 4
+    for (int i = down; i < rows; i += 32) s += *reinterpret_cast<const f32x4 *>(partial + (int64_t)i * h + col);
+  }
+  side[down][lane] = s;
+  __syncthreads();
+  if (down > 0 || col >= h) return;
+  for (int i = 1; i < 32; ++i) s += side[i][lane];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) dgamma[col + e] = from_f32<O>(accumulate ? to_f32(dgamma[col + e]) + s[e] : s[e]);
+}
+
+// Workgroups of the row kernel: as many as run at once.
+int waves_of(int h) { return h <= 2048 ? 1 : h <= 8192 ? 4 : 16; }
+int64_t bwd_groups(int64_t rows, int h) {
+  const int w = waves_of(h);
+  const int64_t most = w == 16 ? 256 : 1024, each = w == 1 ? 4 : 1, want = (rows + each - 1) / each;
+  return want < most ? want : most;
+}
+
+template <typename E>
+int bwd_launch(const NormBwdArgs &a, void *dgamma, int grad_f32, int accumulate, hipStream_t st) {
+  const int nvec = a.h / 8;
+  const unsigned groups = (unsigned)bwd_groups(a.rows, a.h);
+  LaunchScope scope(MTNLG_K_LN_BWD, st);
+#define RMS(W, NV) rmsnorm_bwd_kernel<E, W, NV><<<groups, threads_of<W>(), 0, st>>>(a)
+  if (nvec <= 64) RMS(1, 1);
+  else if (nvec <= 128) RMS(1, 2);
+  else if (nvec <= 256) RMS(1, 4);
+  else if (nvec <= 512) RMS(4, 2);
+  else if (nvec <= 1024) RMS(4, 4);
+  else if (nvec <= 2048) RMS(16, 2);
+  else if (nvec <= 3072) RMS(16, 3);
+  else RMS(16, 4);
+#undef RMS
+  MTNLG_TRY(check_launch());
+  const unsigned blocks = (a.h + 31) / 32;
+  if (grad_f32) rmsnorm_dgamma_kernel<float><<<blocks, 256, 0, st>>>((int)groups, a.h, a.partial, (float *)dgamma, accumulate);
+  else rmsnorm_dgamma_kernel<E><<<blocks, 256, 0, st>>>((int)groups, a.h, a.partial, (E *)dgamma, accumulate);
+  return check_launch();
+}
+
+int check_norm(int dtype, int64_t T, int64_t h) {
+  if (dtype != MTNLG_F32 && dtype != MTNLG_BF16) return MTNLG_INVALID_ARG;
+  if (T <= 0 || h <= 0) return MTNLG_INVALID_ARG;
+  if (h % 8 || h > MAX_COLUMNS || T > 0x7FFFFFFF) return MTNLG_UNSUPPORTED_SHAPE;
+  return MTNLG_OK;
+}
+bool unaligned(std::initializer_list<const void *> ps) {
+  for (const void *p : ps)
+    if ((uintptr_t)p & 15) return true;
+  return false;
+}
+
+}  // namespace
+
+}  // namespace mtnlg
+
+using namespace mtnlg;
+
+extern "C" {
+
+int mtnlg_rmsnorm_fwd(int dtype, int64_t T, int64_t h, const void *x, const void *residual, const void *gamma, float eps, void *xsum, void *out,
+                      float *rstd, void *stream) {
+  if (!x || !gamma || !out || !rstd || (residual && !xsum)) return MTNLG_NULL_POINTER;
+  MTNLG_TRY(check_norm(dtype, T, h));
+  if (!(eps >= 0.0f && eps < INFINITY) || unaligned({x, residual, gamma, xsum, out}) || ((uintptr_t)rstd & 3)) return MTNLG_INVALID_ARG;
+  const NormArgs a{T, (int)h, x, residual, gamma, xsum, out, eps, rstd, nullptr, 0, 0};
+  return dtype == MTNLG_F32 ? fwd_launch<float, false>(a, (hipStream_t)stream) : fwd_launch<bf16, false>(a, (hipStream_t)stream);
+}
+
+int mtnlg_rmsnorm_fwd_e4m3(int dtype, int64_t T, int64_t h, const void *x, const void *residual, const void *gamma, float eps, int32_t columns,
+                           void *xsum, void *out, float *scale, float *rstd, void *stream) {
+  if (!x || !gamma || !out || !rstd || !scale || (residual && !xsum)) return MTNLG_NULL_POINTER;
+  MTNLG_TRY(check_norm(dtype, T, h));
+  if (!(eps >= 0.0f && eps < INFINITY) || unaligned({x, residual, gamma, xsum}) || ((uintptr_t)out & 7) || (((uintptr_t)rstd | (uintptr_t)scale) & 3))
+    return MTNLG_INVALID_ARG;
+  if (columns != 0 && (columns < 8 || columns > 512 || (columns & (columns - 1)))) return MTNLG_INVALID_ARG;
+  const NormArgs a{T, (int)h, x, residual, gamma, xsum, out, eps, rstd, scale, columns, columns ? (int)((h + columns - 1) / columns) : 1};
+  return dtype == MTNLG_F32 ? fwd_launch<float, true>(a, (hipStream_t)stream) : fwd_launch<bf16, true>(a, (hipStream_t)stream);
+}
+
+size_t mtnlg_rmsnorm_bwd_workspace(int64_t T, int64_t h) {
+  if (check_norm(MTNLG_F32, T, h) != MTNLG_OK) return 0;
+  return (size_t)bwd_groups(T, (int)h) * h * sizeof(float);
+}
+
+int mtnlg_rmsnorm_bwd(int dtype, int64_t T, int64_t h, const void *x, const void *gamma, const float *rstd, const void *dout, const void *dres,
+                      void *dx, void *dgamma, int grad_f32, int accumulate, void *workspace, size_t workspace_bytes, void *stream) {
+  if (!x || !gamma || !rstd || !dout || !dx || !dgamma || !workspace) return MTNLG_NULL_POINTER;
+  MTNLG_TRY(check_norm(dtype, T, h));
+  if (unaligned({x, gamma, dout, dres, dx, dgamma, workspace}) || ((uintptr_t)rstd & 3)) return MTNLG_INVALID_ARG;
+  if (workspace_bytes < mtnlg_rmsnorm_bwd_workspace(T, h)) return MTNLG_WORKSPACE_TOO_SMALL;
+  const NormBwdArgs a{T, (int)h, x, gamma, dout, dres, rstd, dx, (float *)workspace};
+  return dtype == MTNLG_F32 ? bwd_launch<float>(a, dgamma, grad_f32, accumulate ? 1 : 0, (hipStream_t)stream)
+                            : bwd_launch<bf16>(a, dgamma, grad_f32, accumulate ? 1 : 0, (hipStream_t)stream);
+}
+
+}  // extern "C"

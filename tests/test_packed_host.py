@@ -1,0 +1,170 @@
+"""Host-side checks of attention over packed sequences, rotary positions and RMS norms that need no GPU: arguments are refused before any
+launch, size queries answer."""
+import ctypes
+
+import pytest
+import torch
+
+import paper_2201_11990_amd as M
+from paper_2201_11990_amd import binding as B
+
+ONE, TWO, THREE = (ctypes.c_void_p(n << 20) for n in (1, 2, 3))   # never dereferenced: argument checks come first
+I64, F32 = ctypes.c_int64, ctypes.c_float
+INVALID, NULL, SHAPE, SMALL = -1, -2, -3, -4
+
+
+def heads(data, token=256, group=128, head=64):
+    return B.Heads(data, token, group, head)
+
+
+def packed(**kw):
+    d = dict(dtype=B.BF16, heads=4, kv_heads=2, head_dim=64, sequences=3, max_q=50, max_k=50, q_tokens=100, k_tokens=100, scale=0.0)
+    d.update(kw)
+    return B.PackedDesc(*d.values())
+
+
+def attention(desc=None, where=None, backward=False, ws=1 << 40, **kw):
+    """status of a call whose matrices lie apart, `kw` put in their places"""
+    m = {n: heads((i + 1) << 30) if n in ("q", "a", "da", "dq") else heads((i + 1) << 30, 128, 64, 0)
+         for i, n in enumerate(("q", "k", "v", "a", "da", "dq", "dk", "dv"))}
+    m.update(kw)
+    where = where or B.PackedSequences(4096, 8192, None, None)
+    desc = desc or packed()
+    ref = lambda n: None if m[n] is None else ctypes.byref(m[n])   # noqa: E731
+    stat = m.get("lse", ONE)
+    if backward:
+        return B.lib().mtnlg_packed_attention_bwd(ctypes.byref(desc), ctypes.byref(where), *(ref(n) for n in ("q", "k", "v", "a")), stat,
+                                                  *(ref(n) for n in ("da", "dq", "dk", "dv")), m.get("workspace", TWO), ws, None)
+    return B.lib().mtnlg_packed_attention_fwd(ctypes.byref(desc), ctypes.byref(where), *(ref(n) for n in ("q", "k", "v", "a")), stat,
+                                              m.get("workspace", None), ws, None)
+
+
+BAD_DESC = [(dict(dtype=2), INVALID), (dict(heads=0), INVALID), (dict(kv_heads=0), INVALID), (dict(kv_heads=3), INVALID), (dict(head_dim=0), INVALID),
+            (dict(head_dim=60), SHAPE), (dict(head_dim=264), SHAPE), (dict(sequences=0), INVALID), (dict(sequences=(1 << 20) + 1), SHAPE),
+            (dict(max_q=0), INVALID), (dict(max_k=-1), INVALID), (dict(q_tokens=0), INVALID), (dict(k_tokens=0), INVALID),
+            (dict(q_tokens=1 << 31), SHAPE), (dict(k_tokens=1 << 30), SHAPE), (dict(scale=-1.0), INVALID), (dict(scale=float("nan")), INVALID),
+            (dict(scale=float("inf")), INVALID)]
+
+
+@pytest.mark.parametrize("backward", [False, True])
+@pytest.mark.parametrize("bad,status", BAD_DESC)
+def test_descriptors_that_are_refused(bad, status, backward):
+    desc = packed(**bad)
+    assert attention(desc, backward=backward) == status
+    size = M.mtnlg_packed_attention_bwd_workspace if backward else M.mtnlg_packed_attention_fwd_workspace
+    assert size(desc) == 0
+
+
+@pytest.mark.parametrize("backward", [False, True])
+def test_null_pointers_and_workspaces_that_are_too_small(backward):
+    for n in ("q", "k", "v", "a") + (("da", "dq", "dk", "dv") if backward else ()):
+        assert attention(backward=backward, **{n: None}) == NULL
+        assert attention(backward=backward, **{n: heads(None)}) == NULL
+    assert attention(backward=backward, lse=None) == NULL
+    assert attention(backward=backward, where=B.PackedSequences(None, 4096, None, None)) == NULL
+    assert attention(backward=backward, where=B.PackedSequences(4096, None, None, None)) == NULL
+    assert attention(backward=backward, where=B.PackedSequences(4098, 4096, None, None)) == INVALID
+    assert attention(backward=backward, where=B.PackedSequences(4096, 4096, 4097, None)) == INVALID
+    if backward:
+        assert attention(backward=True, workspace=None) == NULL
+        assert attention(backward=True, ws=M.mtnlg_packed_attention_bwd_workspace(packed()) - 1) == SMALL
+    else:
+        long = packed(max_k=50000, k_tokens=100000)
+        size = M.mtnlg_packed_attention_fwd_workspace(long)
+        assert size > 0 and attention(long, workspace=TWO, ws=size - 1) == SMALL
+    assert attention(backward=backward, workspace=ctypes.c_void_p(8)) == INVALID
+
+
+# (strides of q, status): too small, not of 16 bytes, negative, of a broadcast, overlapping, too wide
+@pytest.mark.parametrize("strides,status", [((248, 128, 64), INVALID), ((260, 128, 64), INVALID), ((-256, 128, 64), INVALID), ((0, 128, 64), INVALID),
+                                            ((256, 0, 64), INVALID), ((256, 64, 64), INVALID), ((256, 128, 0), INVALID), ((256, 128, 56), INVALID),
+                                            ((128, 64 * 100, 64), INVALID), (((1 << 24) + 8, 128, 64), SHAPE)])
+@pytest.mark.parametrize("which", ["q", "a", "da", "dq"])
+def test_strides_that_are_refused(which, strides, status):
+    backward = which in ("da", "dq")
+    assert attention(backward=backward, **{which: heads(1 << 36, *strides)}) == status
+    assert attention(backward=backward, **{which: heads((1 << 36) + 8)}) == INVALID   # alignment
+
+
+def test_outputs_that_are_inputs_are_refused():
+    for n, i in (("q", 1), ("k", 2), ("v", 3)):
+        assert attention(a=heads(i << 30)) == INVALID, n
+    for n in ("dq", "dk", "dv"):
+        m = heads if n == "dq" else lambda p: heads(p, 128, 64, 0)
+        for i in range(1, 6):
+            assert attention(backward=True, **{n: m(i << 30)}) == INVALID, (n, i)
+    assert attention(backward=True, dk=heads(8 << 30, 128, 64, 0)) == INVALID   # dv's
+
+
+def test_workspace_sizes():
+    # few queries over long keys: room for the parts; whole prompts that fill the chip: none
+    assert M.mtnlg_packed_attention_fwd_workspace(packed(heads=32, kv_heads=4, head_dim=128, sequences=8, max_q=1, max_k=16384, q_tokens=8,
+                                                         k_tokens=1 << 17)) > 0
+    assert M.mtnlg_packed_attention_fwd_workspace(packed(heads=32, kv_heads=8, q_tokens=16384, k_tokens=16384, max_q=8192, max_k=8192)) == 0
+    bwd = M.mtnlg_packed_attention_bwd_workspace
+    assert bwd(packed()) >= 4 * 100 * 4
+    assert bwd(packed(heads=8, kv_heads=8, q_tokens=1 << 20, k_tokens=1 << 20, max_q=1 << 20, max_k=1 << 20)) >= 8 * (1 << 20) * 4
+
+
+def rotary(q=None, k=None, qo=None, ko=None, positions=None, backward=False, **kw):
+    d = dict(dtype=B.BF16, heads=4, kv_heads=2, head_dim=64, rotary_dim=64, layout=0, scaling=0, original_positions=0, tokens=10, base=1e4, factor=1.0,
+             slow=1.0, fast=32.0, amplitude=0.0)
+    d.update(kw)
+    desc = B.RotaryDesc(*d.values())
+    fn = B.lib().mtnlg_rotary_bwd if backward else B.lib().mtnlg_rotary_fwd
+    ref = lambda m, other: ctypes.byref(m or other) if m is not False else None   # noqa: E731
+    return fn(ctypes.byref(desc), ref(q, heads(1 << 30)), ref(k, heads(2 << 30, 128, 64, 0)), ref(qo, heads(3 << 30)), ref(ko, heads(4 << 30, 128, 64, 0)),
+              positions, None)
+
+
+@pytest.mark.parametrize("backward", [False, True])
+@pytest.mark.parametrize("bad,status", [
+    (dict(dtype=5), INVALID), (dict(heads=3), INVALID), (dict(tokens=0), INVALID), (dict(head_dim=60, rotary_dim=60), SHAPE),
+    (dict(head_dim=264), SHAPE), (dict(rotary_dim=0), INVALID), (dict(rotary_dim=7), INVALID), (dict(rotary_dim=66), INVALID), (dict(layout=2), INVALID),
+    (dict(scaling=4), INVALID), (dict(base=0.0), INVALID), (dict(base=float("nan")), INVALID), (dict(base=float("inf")), INVALID),
+    (dict(scaling=1, factor=0.5), INVALID), (dict(scaling=1, factor=float("nan")), INVALID), (dict(scaling=3, factor=2.0), INVALID),
+    (dict(scaling=3, factor=2.0, original_positions=100, slow=3.0, fast=3.0), INVALID), (dict(amplitude=-1.0), INVALID),
+    (dict(q=False), NULL), (dict(qo=False), NULL), (dict(k=False), NULL), (dict(ko=False), NULL), (dict(q=heads(None)), NULL),
+    (dict(qo=heads(1 << 30, 512, 128, 64)), INVALID),   # the input's address with other strides
+    (dict(q=heads(1 << 30, 0, 128, 64)), INVALID), (dict(ko=heads((4 << 30) + 2, 128, 64, 0)), INVALID),
+    (dict(positions=ctypes.c_void_p(4097)), INVALID)])
+def test_rotary_calls_that_are_refused(bad, status, backward):
+    assert rotary(backward=backward, **bad) == status
+
+
+def test_norms_that_are_refused():
+    L = B.lib()
+    fwd = lambda dtype=1, T=4, h=16, x=ONE, res=None, gamma=ONE, eps=1e-5, xsum=None, out=TWO, rstd=ONE: L.mtnlg_rmsnorm_fwd(   # noqa: E731
+        dtype, I64(T), I64(h), x, res, gamma, F32(eps), xsum, out, rstd, None)
+    for kw, status in ((dict(dtype=3), INVALID), (dict(T=0), INVALID), (dict(h=0), INVALID), (dict(h=12), SHAPE), (dict(h=32776), SHAPE),
+                       (dict(T=1 << 31), SHAPE), (dict(x=None), NULL), (dict(gamma=None), NULL), (dict(out=None), NULL), (dict(rstd=None), NULL),
+                       (dict(res=ONE), NULL), (dict(eps=-1.0), INVALID), (dict(eps=float("nan")), INVALID), (dict(out=ctypes.c_void_p(8)), INVALID)):
+        assert fwd(**kw) == status, kw
+    eight = lambda columns=0, scale=ONE, out=TWO: L.mtnlg_rmsnorm_fwd_e4m3(1, I64(4), I64(16), ONE, None, ONE, F32(1e-5), columns, None, out, scale, ONE, None)   # noqa: E731
+    for columns in (-8, 4, 12, 1024):
+        assert eight(columns) == INVALID
+    assert eight(scale=None) == NULL and eight(out=ctypes.c_void_p(4)) == INVALID
+    size = M.mtnlg_rmsnorm_bwd_workspace(100, 2048)
+    assert size > 0 and M.mtnlg_rmsnorm_bwd_workspace(0, 2048) == 0 and M.mtnlg_rmsnorm_bwd_workspace(4, 12) == 0
+    bwd = lambda T=100, h=2048, dres=None, ws=ONE, n=size, dx=TWO: L.mtnlg_rmsnorm_bwd(1, I64(T), I64(h), ONE, ONE, ONE, ONE, dres, dx, TWO, 1, 0, ws, n, None)   # noqa: E731
+    assert bwd(n=size - 1) == SMALL and bwd(ws=None) == NULL and bwd(T=0) == INVALID and bwd(h=20) == SHAPE and bwd(dx=ctypes.c_void_p(2)) == INVALID
+
+
+def test_the_binding_refuses_what_it_can_see():
+    q, k = torch.zeros(5, 4, 64), torch.zeros(5, 2, 64)
+    with pytest.raises(ValueError):
+        M.packed_desc(q, torch.zeros(5, 3, 64), 1, 5, 5)
+    with pytest.raises(ValueError):
+        M.packed_desc(q, torch.zeros(5, 2, 32), 1, 5, 5)
+    with pytest.raises(ValueError):
+        M.packed_desc(q, k.bfloat16(), 1, 5, 5)
+    with pytest.raises(ValueError):
+        M.packed_desc(torch.zeros(5, 4, 1, 64), k, 1, 5, 5)
+    with pytest.raises(TypeError):
+        M.packed_desc(q.double(), k.double(), 1, 5, 5)
+    with pytest.raises(ValueError):
+        B._heads(torch.zeros(5, 4, 64).transpose(1, 2), 2)   # rows that are not dense
+    with pytest.raises(ValueError):
+        B._heads(torch.zeros(5, 64), 2)
+    h = B._heads(torch.zeros(5, 2, 4, 64)[:, :, :2], 2)
+    assert (h.token, h.group, h.head) == (512, 256, 64)
