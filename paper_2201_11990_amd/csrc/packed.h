@@ -40,12 +40,16 @@ struct PackedBwdArgs {
   float *D, *part;
 };
 
-// kernels of either type (packed_bf16.hip, packed_f32.hip); pieces: workgroups of a head of keys
-int packed_fwd_bf16(const PackedFwdArgs &w, int owned, int64_t blocks, hipStream_t st);
-int packed_fwd_f32(const PackedFwdArgs &w, int64_t blocks, hipStream_t st);
-int packed_bwd_bf16(const PackedBwdArgs &w, int owned, int64_t pieces, int64_t key_pieces, hipStream_t st);
-int packed_bwd_f32(const PackedBwdArgs &w, int64_t pieces, int64_t key_pieces, hipStream_t st);
-int packed_dkv_owned(int dtype, int d);   // keys of a workgroup
+// Head sizes up to which bf16 has kernels of its own (packed_fwd.hip, packed_bwd.hip); others and fp32: packed_plain.hip.
+constexpr int PACKED_TUNED = 192;
+inline bool packed_tuned(int dtype, int d) { return dtype == MTNLG_BF16 && d <= PACKED_TUNED; }
+// owned: rows of a workgroup (plain: 128); blocks, pieces: workgroups, of all heads of keys and of one
+int packed_fwd_tuned(const PackedFwdArgs &w, int owned, int64_t blocks, hipStream_t st);
+int packed_fwd_plain(int dtype, const PackedFwdArgs &w, int64_t blocks, hipStream_t st);
+int packed_bwd_tuned(const PackedBwdArgs &w, int owned, int64_t pieces, int key_owned, int64_t key_pieces, hipStream_t st);
+int packed_bwd_plain(int dtype, const PackedBwdArgs &w, int64_t pieces, int64_t key_pieces, hipStream_t st);
+int packed_dkv_plain_owned(int dtype, int d);   // keys of a workgroup of dk / dv
+int packed_dkv_least(int d);                    // ... of the tuned kernels: this many or 128
 
 namespace {
 
@@ -120,6 +124,31 @@ struct RowStream {
   }
 };
 
+// The same as a walk from tile to tile in scalar registers (the compiler clamps and multiplies on the vector unit).
+struct RowWalk {
+  uint64_t base;
+  int rows;
+  uint32_t pitch, step;   // bytes of a row, of a tile
+  __device__ __forceinline__ RowWalk(const void *first, int n, uint32_t pitch_, int tile_rows) {
+    const uint64_t a = (uint64_t)first;
+    base = ((uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(a >> 32)) << 32) | (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)a);
+    rows = __builtin_amdgcn_readfirstlane(n);
+    pitch = __builtin_amdgcn_readfirstlane(pitch_);
+    step = pitch * (uint32_t)tile_rows;
+  }
+  template <int TR>
+  __device__ __forceinline__ dma_rsrc_t tile() const {
+    uint32_t records;
+    asm("s_max_i32 %0, %1, 0\n\ts_min_i32 %0, %0, %2\n\ts_mul_i32 %0, %0, %3" : "=&s"(records) : "s"(rows), "n"(TR), "s"(pitch) : "scc");
+    return dma_rsrc((const void *)base, records);
+  }
+  template <int TR>
+  __device__ __forceinline__ void advance() {
+    base += step;
+    rows -= TR;
+  }
+};
+
 // ------------------------------------------------------------------ element types
 // Tiles hold rows as in memory, d columns filled up with zeros to D, 16-byte units permuted by row.  A step of a first product (contracting over columns) is one
 // 16-byte piece of a row: 16 columns of bf16 (one MFMA), 8 of fp32 (four).  A step of a second product (contracting over 16 rows of the tile) is a 32-column block: one MFMA
@@ -151,13 +180,8 @@ struct Elem<bf16, D> {
     return load4(reinterpret_cast<const bf16 *>(t + T::off(row, 4 * cb + q) + 8 * h));
   }
   static __device__ __forceinline__ float not_finite(const Unit &u, float z) {   // NaN if any is an infinity or NaN
-    typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
-    const u32x4 w = __builtin_bit_cast(u32x4, u);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const unsigned t = w[i];
-      z = fmaf(__builtin_bit_cast(float, t & 0xFFFF0000u), 0.0f, fmaf(__builtin_bit_cast(float, t << 16), 0.0f, z));
-    }
+    for (int i = 0; i < 8; i += 2) z = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{u[i], u[i + 1]}, bf16x2{(bf16)0.0f, (bf16)0.0f}, z, false);
     return z;
   }
   static __device__ __forceinline__ float dot(const Unit &a, const Unit &b, float s) {
@@ -253,10 +277,14 @@ __device__ __forceinline__ float weight_of(float s, float f, float shift) { retu
 // Whether 32 rows of a tile hold an infinity or NaN: asked where a mask hides some of them from some of the wave's rows, whose weights there are zeros
 // (0 x inf would be NaN in rows that do not depend on it).
 template <typename E, int D>
-__device__ __forceinline__ bool rows_not_finite(const char *t, const typename Elem<E, D>::Lane &ln) {
+__device__ __forceinline__ bool rows_not_finite(const char *t, typename Elem<E, D>::Lane ln) {
   float z = 0.0f;
+  ln.here();   // (as above: not for every tile)
 #pragma unroll
-  for (int kk = 0; kk < Elem<E, D>::K1; ++kk) z = Elem<E, D>::not_finite(Elem<E, D>::unit(t, ln, kk), z);
+  for (int kk = 0; kk < Elem<E, D>::K1; ++kk) {
+    z = Elem<E, D>::not_finite(Elem<E, D>::unit(t, ln, kk), z);
+    if (kk % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+  }
   return __builtin_amdgcn_ballot_w64(z != 0.0f) != 0;
 }
 // Then the product with 32 rows of the tile is taken row by row, from the weights w of those rows R that the own row sees.
@@ -278,7 +306,39 @@ __device__ __forceinline__ void add_seen_rows(f32x16 (&acc)[D / 32], const f32x1
         const f32x4 v = Elem<E, D>::row4(t, row, cb, q, h);
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[cb][4 * q + e] = fmaf(p, v[e], acc[cb][4 * q + e]);
+        __builtin_amdgcn_sched_barrier(0);   // no registers for more reads at once
       }
+  }
+}
+
+// The two kinds of product of 32 rows of a tile, fragments a few steps ahead of their MFMAs (bf16: in fenced steps, the compiler otherwise reads all
+// fragments first, into registers that the kernels do not have).
+template <typename E, int D>
+__device__ __forceinline__ void products_with_units(const char *t, const typename Elem<E, D>::Lane &ln, const typename Elem<E, D>::Unit (&own)[Elem<E, D>::K1], f32x16 &v) {
+  using P = Elem<E, D>;
+  if constexpr (sizeof(E) == 2) {
+    typename P::Unit fr[4];
+    pipelined<P::K1, 3>([&](int i) { fr[i & 3] = P::unit(t, ln, i); }, [&](int i) { v = P::mma(fr[i & 3], own[i], v); }, [](int) {});
+  } else {
+#pragma unroll
+    for (int kk = 0; kk < P::K1; ++kk) v = P::mma(P::unit(t, ln, kk), own[kk], v);
+  }
+}
+template <typename E, int D>
+__device__ __forceinline__ void products_with_rows(f32x16 (&acc)[D / 32], const f32x16 &v, const char *t, const typename Elem<E, D>::Lane &ln) {
+  using P = Elem<E, D>;
+  if constexpr (sizeof(E) == 2) {
+    const typename P::Weights x[2] = {P::weights(v, 0), P::weights(v, 1)};
+    typename P::Column fr[4];
+    pipelined<P::K1, 3>([&](int i) { fr[i & 3] = P::column(t, ln, i / 2, i % 2); }, [&](int i) { acc[i / 2] = P::mma_rows(fr[i & 3], x[i % 2], acc[i / 2]); },
+                        [](int) {});
+  } else {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const typename P::Weights x = P::weights(v, u);
+#pragma unroll
+      for (int cb = 0; cb < D / 32; ++cb) acc[cb] = P::mma_rows(P::column(t, ln, cb, u), x, acc[cb]);
+    }
   }
 }
 
@@ -300,13 +360,16 @@ inline int64_t pieces_bound(int64_t total, int64_t most, int count, int rows) {
 }
 
 template <typename F>
-int packed_by_size(int d, F &&f) {   // head sizes in tiles of the next multiple of 32 columns that there are kernels for
+int packed_tuned_by_size(int d, F &&f) {
   if (d <= 64) return f(std::integral_constant<int, 64>{});
   if (d <= 96) return f(std::integral_constant<int, 96>{});
   if (d <= 128) return f(std::integral_constant<int, 128>{});
   if (d <= 160) return f(std::integral_constant<int, 160>{});
-  if (d <= 192) return f(std::integral_constant<int, 192>{});
-  return f(std::integral_constant<int, 256>{});
+  return f(std::integral_constant<int, 192>{});
+}
+template <typename F>
+int packed_by_size(int d, F &&f) {   // head sizes in tiles of the next multiple of 32 columns that there are kernels for
+  return d <= PACKED_TUNED ? packed_tuned_by_size(d, f) : f(std::integral_constant<int, 256>{});
 }
 
 }  // namespace

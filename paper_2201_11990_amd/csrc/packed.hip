@@ -65,7 +65,7 @@ FwdPlan fwd_plan(const PackedShape &S) {
   const int64_t rows = (int64_t)S.where.q_tokens * S.group, most = (int64_t)S.max_q * S.group;
   p.owned = 128;
   p.pieces = pieces_bound(rows, most, S.where.count, p.owned);
-  if (S.dtype == MTNLG_BF16 && p.pieces * S.kv_heads < 1024) {
+  if (packed_tuned(S.dtype, S.d) && p.pieces * S.kv_heads < 1024) {
     p.owned = 64;
     p.pieces = pieces_bound(rows, most, S.where.count, p.owned);
   }
@@ -91,7 +91,7 @@ bool unaligned(const mtnlg_packed_sequences *w) {
 }
 
 struct BwdPlan {
-  int owned, splits;         // rows of a dq workgroup; parts of a group
+  int owned, key_owned, splits;   // rows of a dq workgroup, keys of one of dk / dv; parts of a group
   int64_t pieces, key_pieces;
   size_t d_bytes, bytes;
 };
@@ -100,11 +100,16 @@ BwdPlan bwd_plan(const PackedShape &S) {
   const int64_t rows = (int64_t)S.where.q_tokens * S.group, most = (int64_t)S.max_q * S.group;
   p.owned = 128;
   p.pieces = pieces_bound(rows, most, S.where.count, p.owned);
-  if (S.dtype == MTNLG_BF16 && p.pieces * S.kv_heads < 1024) {
+  if (packed_tuned(S.dtype, S.d) && p.pieces * S.kv_heads < 1024) {
     p.owned = 64;
     p.pieces = pieces_bound(rows, most, S.where.count, p.owned);
   }
-  p.key_pieces = pieces_bound(S.where.k_tokens, S.max_k, S.where.count, packed_dkv_owned(S.dtype, S.d));
+  p.key_owned = packed_tuned(S.dtype, S.d) ? 128 : packed_dkv_plain_owned(S.dtype, S.d);
+  p.key_pieces = pieces_bound(S.where.k_tokens, S.max_k, S.where.count, p.key_owned);
+  if (packed_tuned(S.dtype, S.d) && p.key_pieces * S.heads < 512) {
+    p.key_owned = packed_dkv_least(S.d);
+    p.key_pieces = pieces_bound(S.where.k_tokens, S.max_k, S.where.count, p.key_owned);
+  }
   const int64_t wide = p.key_pieces * S.kv_heads, splits = (512 + wide - 1) / wide;
   p.splits = (int)(splits < S.group ? splits : S.group);
   p.d_bytes = align_up((size_t)S.where.q_tokens * S.heads * sizeof(float), 256);
@@ -184,7 +189,7 @@ int mtnlg_packed_attention_fwd(const mtnlg_packed_desc *desc, const mtnlg_packed
   if (blocks > 0x7FFFFFFF) return MTNLG_UNSUPPORTED_SHAPE;
   const hipStream_t st = (hipStream_t)stream;
   LaunchScope scope(MTNLG_K_ATTN_FWD, st);
-  MTNLG_TRY(S.dtype == MTNLG_F32 ? packed_fwd_f32(w, blocks, st) : packed_fwd_bf16(w, plan.owned, blocks, st));
+  MTNLG_TRY(packed_tuned(S.dtype, S.d) ? packed_fwd_tuned(w, plan.owned, blocks, st) : packed_fwd_plain(S.dtype, w, blocks, st));
   if (plan.chunks == 1) return MTNLG_OK;
   const unsigned joins = (unsigned)(pieces_bound((int64_t)S.where.q_tokens * S.group, (int64_t)S.max_q * S.group, S.where.count, 4) * S.kv_heads);
   if (S.dtype == MTNLG_F32) packed_join_kernel<float><<<joins, 256, 0, st>>>(w);
@@ -236,7 +241,8 @@ int mtnlg_packed_attention_bwd(const mtnlg_packed_desc *desc, const mtnlg_packed
   w.part = (float *)((char *)workspace + plan.d_bytes);
   const hipStream_t st = (hipStream_t)stream;
   LaunchScope scope(MTNLG_K_ATTN_BWD, st);
-  MTNLG_TRY(S.dtype == MTNLG_F32 ? packed_bwd_f32(w, plan.pieces, plan.key_pieces, st) : packed_bwd_bf16(w, plan.owned, plan.pieces, plan.key_pieces, st));
+  MTNLG_TRY(packed_tuned(S.dtype, S.d) ? packed_bwd_tuned(w, plan.owned, plan.pieces, plan.key_owned, plan.key_pieces, st)
+                                       : packed_bwd_plain(S.dtype, w, plan.pieces, plan.key_pieces, st));
   if (plan.splits == 1) return MTNLG_OK;
   const unsigned joins = (unsigned)(pieces_bound(S.where.k_tokens, S.max_k, S.where.count, 16) * S.kv_heads);
   if (S.dtype == MTNLG_F32) packed_dkv_join_kernel<float><<<joins, 256, 0, st>>>(w);

@@ -1,30 +1,181 @@
-// Attention over packed sequences with grouped heads, backward (packed_fwd.hip: forward).
-//
-//   D = da . a (of a row):  dP = da v^T,  dS = P o (dP - D),  dq = scale dS k;  of a head of keys, summed over the query heads that share it:
-//   dk = scale sum dS^T q,  dv = sum P^T da
-//
-// Two kernels: dq (and D), which owns rows (token, head of the group) as the forward kernel does and streams K and V, and dk / dv, which owns keys and streams Q and dO of
-// one head after the other.  No atomics: where a head's keys leave units idle, the heads of the group are dealt out over workgroups, whose sums a third kernel adds up in their
-// order.  Keys that no query sees get zeros, rows of no sequence are left as they are.
-#pragma once
+// Attention over packed sequences in the order of its formulas, without a schedule of its own: fp32 on v_mfma_f32_32x32x2_f32 with P and dS in fp32, and bf16
+// of head sizes above 192 (packed_fwd.hip, packed_bwd.hip: the others).
 #include "packed.h"
 
 namespace mtnlg {
 
 namespace {
 
+// ------------------------------------------------------------------ forward
+// rows of a tile: what 160 KB of LDS hold twice of K and V, and two workgroups of each
+template <typename E> constexpr int tile_rows() { return sizeof(E) == 2 ? 64 : 32; }
+template <typename E, int D> constexpr int fwd_stage() { return 2 * tile_rows<E>() * D * (int)sizeof(E); }
+template <typename E, int D> constexpr int fwd_per_unit() { return 2 * 2 * fwd_stage<E, D>() <= 160 * 1024 ? 2 : 1; }
+
+template <typename E, int D>
+__global__ __launch_bounds__(256, (fwd_per_unit<E, D>())) void plain_fwd_kernel(PackedFwdArgs w) {
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  using P = Elem<E, D>;
+  constexpr int TR = tile_rows<E>(), K1 = P::K1, CB = D / 32, MATRIX = TR * D * (int)sizeof(E), STAGE = 2 * MATRIX, SUB = 2 * P::BAND;
+  constexpr int OWNED = 128, SUBS = TR / 32;
+  const int lane = threadIdx.x & 63, h = lane >> 5, r = w.group, d = w.d;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int j = blockIdx.x % w.kv_heads;
+  const bool chunked = w.chunk > 0;
+  auto chunks_of = [&](const Span &s) { return chunked ? min((max(s.lk, 1) + w.chunk - 1) / w.chunk, w.chunks) : 1; };
+  Span s;
+  unsigned at;
+  if (!find_piece(w.where, blockIdx.x / w.kv_heads, [&](const Span &s) { return (unsigned)((s.lq * r + OWNED - 1) / OWNED * chunks_of(s)); }, s, at)) return;
+  const int nc = chunks_of(s), count = (s.lq * r + OWNED - 1) / OWNED, shift = s.lk - s.lq;
+  const int chunk = at % nc, block = count - 1 - at / nc;   // falling work
+  const int rows = s.lq * r, block0 = block * OWNED;
+  const int last_row = min(block0 + OWNED, rows) - 1;
+  const int begin = chunk * w.chunk;
+  int end = min(s.lk, last_row / r + shift + 1);   // keys that the block sees
+  if (chunked && chunk + 1 < nc) end = min(end, begin + w.chunk);
+  if (chunked && end <= begin && chunk > 0) return;
+  const int ntiles = end > begin ? (end - begin + TR - 1) / TR : 0;
+
+  const int own0 = block0 + wave * 32, mine = own0 + (lane & 31), row = min(mine, rows - 1);
+  const int tok = row / r, g = row - tok * r;
+  const int limit = min(tok + shift, end - 1);   // the last key here that the row sees
+  // uniform over the wave: the least and the most of its rows, -1 if it has none
+  const int least = __builtin_amdgcn_readfirstlane(limit), most = own0 < rows ? __builtin_amdgcn_readlane(limit, 31) : -1;
+
+  const RowStream ks{reinterpret_cast<const char *>(row_at<E>(w.k, s.k0 + begin, j, 0)), end - begin, (uint32_t)(w.k.token * sizeof(E))};
+  const RowStream vs{reinterpret_cast<const char *>(row_at<E>(w.v, s.k0 + begin, j, 0)), end - begin, (uint32_t)(w.v.token * sizeof(E))};
+  // waves 0, 1 bring K, waves 2, 3 V
+  constexpr int IPW = TR / 32 * P::NI;
+  const int half = wave >> 1, band = (wave & 1) * (TR / 32);
+  const uint32_t pitch = half ? vs.pitch : ks.pitch;
+  uint32_t dma_off[IPW];
+#pragma unroll
+  for (int i = 0; i < IPW; ++i) dma_off[i] = P::dma_offset(pitch, band + i / P::NI, lane, i % P::NI, d);
+  const uint32_t dst0 = lds_address(smem) + half * MATRIX + band * P::BAND;
+  auto issue = [&](int t) {
+    const dma_rsrc_t rs = half ? vs.tile<TR>(t) : ks.tile<TR>(t);
+#pragma unroll
+    for (int i = 0; i < IPW; ++i) dma16<Burst::value>(rs, dst0 + (t & 1) * STAGE + i * 1024, dma_off[i]);
+  };
+  if (ntiles > 0) issue(0);
+  typename P::Unit qf[K1];
+  const E *qrow = row_at<E>(w.q, s.q0 + tok, j, g);
+#pragma unroll
+  for (int kk = 0; kk < K1; ++kk) qf[kk] = row_unit<E, D>(qrow, kk, h, d);
+#pragma unroll
+  for (int kk = 0; kk < K1; ++kk) arrive(qf[kk]);
+
+  constexpr bool EXACT = sizeof(E) == 4;
+  const float c = w.scale * kLog2e, f = EXACT ? w.scale : c;
+  const typename P::Lane ln(lane);
+  f32x16 o[CB];
+#pragma unroll
+  for (int cb = 0; cb < CB; ++cb) o[cb] = f32x16{};
+  float m = -INFINITY, l = 0.0f;
+  for (int it = 0; it < ntiles; ++it) {
+    wait_and_barrier<0>();   // tile it landed everywhere, and the other stage is free
+    if (it + 1 < ntiles) issue(it + 1);
+#pragma unroll
+    for (int sub = 0; sub < SUBS; ++sub) {
+      const int key0 = begin + it * TR + 32 * sub;
+      if (key0 > most) continue;   // nothing that a row of the wave sees
+      const char *K = smem + (it & 1) * STAGE + sub * SUB, *V = K + MATRIX;
+      f32x16 sc = {};
+#pragma unroll
+      for (int kk = 0; kk < K1; ++kk) sc = P::mma(P::unit(K, ln, kk), qf[kk], sc);
+      const bool masked = key0 + 31 > least;
+      if (masked) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (key0 + 8 * (e / 4) + 4 * h + e % 4 > limit) sc[e] = -INFINITY;
+      }
+      // The reference maximum follows when the row maximum has outgrown it by more than 2^8: any reference gives the same sums, this one makes rescaling rare.
+      float mx = sc[0];
+#pragma unroll
+      for (int e = 1; e < 16; ++e) mx = fmaxf(mx, sc[e]);
+      mx = pair_max(mx);
+      const float m_new = mx * c > m * c + (it == 0 ? 0.0f : 8.0f) ? mx : m;
+      const float ref = m_new == -INFINITY ? 0.0f : m_new;
+      const float shifted = EXACT ? product_of(ref, w.scale) : ref * c;
+      float rs = 0.0f;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        sc[e] = weight_of<E>(sc[e], f, shifted);
+        rs += sc[e];
+      }
+      const float alpha = m == m_new ? 1.0f : EXACT ? exact_exp(product_of(m, w.scale) - shifted) : fast_exp2((m - m_new) * c);
+      l = l * alpha + rs;
+      m = m_new;
+      if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) o[cb] *= alpha;
+      }
+      if (masked && rows_not_finite<E, D>(V, ln)) {
+        add_seen_rows<E, D>(o, sc, V, [&](int row) { return key0 + row <= limit; });
+      } else {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const typename P::Weights x = P::weights(sc, t);
+#pragma unroll
+          for (int cb = 0; cb < CB; ++cb) o[cb] = P::mma_rows(P::column(V, ln, cb, t), x, o[cb]);
+        }
+      }
+    }
+  }
+  l += __shfl_xor(l, 32, 64);
+  if (mine >= rows) return;
+  const int head = j * r + g;
+  if (chunked) {
+    const int64_t id = (int64_t)(s.q0 + tok) * ((int64_t)w.kv_heads * r) + head, at = chunk * ((int64_t)w.where.q_tokens * w.kv_heads * r) + id;
+    float *const to = w.part + at * d;
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int col = 32 * cb + 8 * q + 4 * h;
+        if (col < d) *reinterpret_cast<f32x4 *>(to + col) = quarter_of(o[cb], q);
+      }
+    if (h == 0) *reinterpret_cast<float2 *>(w.stat + 2 * at) = float2{m, l};
+    return;
+  }
+  const bool none = tok + shift < 0;   // the row sees no key
+  const float inv = none ? 0.0f : 1.0f / l;
+  E *const to = row_at<E>(w.a, s.q0 + tok, j, g);
+#pragma unroll
+  for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int col = 32 * cb + 8 * q + 4 * h;
+      if (col < d) put4(to + col, quarter_of(o[cb], q) * inv);
+    }
+  if (h == 0) w.lse[(int64_t)head * w.where.q_tokens + s.q0 + tok] = none ? -INFINITY : plus_log(product_of(m, w.scale), l);
+}
+
+template <typename E, int D>
+int fwd_launch(const PackedFwdArgs &w, int64_t blocks, hipStream_t st) {
+  constexpr int smem = 2 * fwd_stage<E, D>();
+  static unsigned long long attr_done = 0;
+  int device;
+  if (!attr_is_set(attr_done, &device)) {
+    MTNLG_TRY(set_lds(plain_fwd_kernel<E, D>, smem));
+    attr_mark_set(attr_done, device);
+  }
+  plain_fwd_kernel<E, D><<<(unsigned)blocks, 256, smem, st>>>(w);
+  return check_launch();
+}
+
+// ------------------------------------------------------------------ backward: dq and D
 template <typename E> constexpr int dq_rows() { return sizeof(E) == 2 ? 64 : 32; }
 template <typename E, int D> constexpr int dq_stage() { return 2 * dq_rows<E>() * D * (int)sizeof(E); }
 // own rows of q and da, and results, take D * sizeof(E) / 2 + D / 2 registers and more
 template <typename E, int D> constexpr int dq_per_unit() { return 2 * 2 * dq_stage<E, D>() <= 160 * 1024 && D * (int)sizeof(E) <= 384 ? 2 : 1; }
 
-// ------------------------------------------------------------------ dq and D
-template <typename E, int D, int SPLIT>
-__global__ __launch_bounds__(256, (dq_per_unit<E, D>())) void packed_dq_kernel(PackedBwdArgs w) {
+template <typename E, int D>
+__global__ __launch_bounds__(256, (dq_per_unit<E, D>())) void plain_dq_kernel(PackedBwdArgs w) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
   using P = Elem<E, D>;
   constexpr int TR = dq_rows<E>(), K1 = P::K1, CB = D / 32, MATRIX = TR * D * (int)sizeof(E), STAGE = 2 * MATRIX, SUB = 2 * P::BAND;
-  constexpr int OWNED = 128 / SPLIT, SUBS = TR / 32 / SPLIT;
+  constexpr int OWNED = 128, SUBS = TR / 32;
   const int lane = threadIdx.x & 63, h = lane >> 5, r = w.group, d = w.d;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int j = blockIdx.x % w.kv_heads;
@@ -35,8 +186,7 @@ __global__ __launch_bounds__(256, (dq_per_unit<E, D>())) void packed_dq_kernel(P
   const int rows = s.lq * r, block0 = block * OWNED, last_row = min(block0 + OWNED, rows) - 1;
   const int end = max(0, min(s.lk, last_row / r + shift + 1)), ntiles = (end + TR - 1) / TR;
 
-  const int part = SPLIT == 2 ? wave >> 1 : 0, rows_of = SPLIT == 2 ? wave & 1 : wave;
-  const int own0 = block0 + rows_of * 32, mine = own0 + (lane & 31), row = min(mine, rows - 1);
+  const int own0 = block0 + wave * 32, mine = own0 + (lane & 31), row = min(mine, rows - 1);
   const int tok = row / r, g = row - tok * r, head = j * r + g;
   const int limit = min(tok + shift, s.lk - 1);
   const int least = __builtin_amdgcn_readfirstlane(limit), most = own0 < rows ? __builtin_amdgcn_readlane(limit, 31) : -1;
@@ -70,7 +220,7 @@ __global__ __launch_bounds__(256, (dq_per_unit<E, D>())) void packed_dq_kernel(P
   dsum += __shfl_xor(dsum, 32, 64);
   constexpr bool EXACT = sizeof(E) == 4;
   const int64_t stat = (int64_t)head * w.where.q_tokens + s.q0 + tok;
-  if (mine < rows && h == 0 && part == 0) w.D[stat] = dsum;
+  if (mine < rows && h == 0) w.D[stat] = dsum;
   float lse = w.lse[stat];
   lse = lse == -INFINITY ? INFINITY : EXACT ? lse : lse * kLog2e;   // a row that sees nothing: weights of 0
 #pragma unroll
@@ -90,9 +240,9 @@ __global__ __launch_bounds__(256, (dq_per_unit<E, D>())) void packed_dq_kernel(P
     if (it + 1 < ntiles) issue(it + 1);
 #pragma unroll
     for (int sub = 0; sub < SUBS; ++sub) {
-      const int key0 = it * TR + 32 * (part + sub);
+      const int key0 = it * TR + 32 * sub;
       if (key0 > most) continue;
-      const char *K = smem + (it & 1) * STAGE + (part + sub) * SUB, *V = K + MATRIX;
+      const char *K = smem + (it & 1) * STAGE + sub * SUB, *V = K + MATRIX;
       f32x16 sc = {}, pc = {};
 #pragma unroll
       for (int kk = 0; kk < K1; ++kk) sc = P::mma(P::unit(K, ln, kk), qf[kk], sc);
@@ -118,26 +268,6 @@ __global__ __launch_bounds__(256, (dq_per_unit<E, D>())) void packed_dq_kernel(P
       }
     }
   }
-  if constexpr (SPLIT == 2) {   // the two halves of the keys: each wave finishes half of the columns
-    f32x4 *slots = reinterpret_cast<f32x4 *>(smem) + lane;
-    __syncthreads();
-#pragma unroll
-    for (int cb = 0; cb < CB; ++cb)
-#pragma unroll
-      for (int q = 0; q < 2; ++q) slots[((wave * CB + cb) * 2 + q) * 64] = part ? quarter_of(acc[cb], q) : quarter_of(acc[cb], 2 + q);
-    __syncthreads();
-#pragma unroll
-    for (int cb = 0; cb < CB; ++cb)
-#pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        const f32x4 rest = slots[(((wave ^ 2) * CB + cb) * 2 + q) * 64];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          if (part) acc[cb][8 + 4 * q + e] += rest[e];
-          else acc[cb][4 * q + e] += rest[e];
-        }
-      }
-  }
   if (mine >= rows) return;
   E *const to = row_at<E>(w.dq, s.q0 + tok, j, g);
 #pragma unroll
@@ -145,7 +275,7 @@ __global__ __launch_bounds__(256, (dq_per_unit<E, D>())) void packed_dq_kernel(P
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const int col = 32 * cb + 8 * q + 4 * h;
-      if (col < d && (SPLIT == 1 || q / 2 == part)) put4(to + col, quarter_of(acc[cb], q) * w.scale);
+      if (col < d) put4(to + col, quarter_of(acc[cb], q) * w.scale);
     }
 }
 
@@ -159,7 +289,7 @@ template <typename E, int D> struct Dkv {
 };
 
 template <typename E, int D>
-__global__ __launch_bounds__((Dkv<E, D>::THREADS)) void packed_dkv_kernel(PackedBwdArgs w) {
+__global__ __launch_bounds__((Dkv<E, D>::THREADS)) void plain_dkv_kernel(PackedBwdArgs w) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
   using P = Elem<E, D>;
   using L = Dkv<E, D>;
@@ -309,28 +439,39 @@ __global__ __launch_bounds__((Dkv<E, D>::THREADS)) void packed_dkv_kernel(Packed
 }
 
 template <typename E, int D>
-int bwd_launch(const PackedBwdArgs &w, int owned, int64_t pieces, int64_t key_pieces, hipStream_t st) {
-  constexpr int CB = D / 32, ring = 2 * dq_stage<E, D>(), merge = 4 * CB * 2048, smem = ring > merge ? ring : merge;
+int bwd_launch(const PackedBwdArgs &w, int64_t pieces, int64_t key_pieces, hipStream_t st) {
+  constexpr int smem = 2 * dq_stage<E, D>();
   static unsigned long long attr_done = 0;
   int device;
   if (!attr_is_set(attr_done, &device)) {
-    MTNLG_TRY(set_lds(packed_dq_kernel<E, D, 1>, smem));
-    if constexpr (sizeof(E) == 2) MTNLG_TRY(set_lds(packed_dq_kernel<E, D, 2>, smem));
-    MTNLG_TRY(set_lds(packed_dkv_kernel<E, D>, Dkv<E, D>::LDS));
+    MTNLG_TRY(set_lds(plain_dq_kernel<E, D>, smem));
+    MTNLG_TRY(set_lds(plain_dkv_kernel<E, D>, Dkv<E, D>::LDS));
     attr_mark_set(attr_done, device);
   }
-  const unsigned blocks = (unsigned)(pieces * w.kv_heads);
-  if constexpr (sizeof(E) == 2) {
-    if (owned == 64) packed_dq_kernel<E, D, 2><<<blocks, 256, smem, st>>>(w);
-    else packed_dq_kernel<E, D, 1><<<blocks, 256, smem, st>>>(w);
-  } else {
-    packed_dq_kernel<E, D, 1><<<blocks, 256, smem, st>>>(w);
-  }
+  plain_dq_kernel<E, D><<<(unsigned)(pieces * w.kv_heads), 256, smem, st>>>(w);
   MTNLG_TRY(check_launch());
-  packed_dkv_kernel<E, D><<<(unsigned)(key_pieces * w.splits * w.kv_heads), Dkv<E, D>::THREADS, Dkv<E, D>::LDS, st>>>(w);
+  plain_dkv_kernel<E, D><<<(unsigned)(key_pieces * w.splits * w.kv_heads), Dkv<E, D>::THREADS, Dkv<E, D>::LDS, st>>>(w);
   return check_launch();
 }
 
+template <typename F>
+int by_size(int dtype, int d, F &&f) {
+  if (dtype == MTNLG_F32) return packed_by_size(d, [&](auto D) { return f(0.0f, D); });
+  return f((bf16)0.0f, std::integral_constant<int, 256>{});
+}
+
 }  // namespace
+
+int packed_fwd_plain(int dtype, const PackedFwdArgs &w, int64_t blocks, hipStream_t st) {
+  return by_size(dtype, w.d, [&](auto e, auto D) { return fwd_launch<decltype(e), decltype(D)::value>(w, blocks, st); });
+}
+
+int packed_bwd_plain(int dtype, const PackedBwdArgs &w, int64_t pieces, int64_t key_pieces, hipStream_t st) {
+  return by_size(dtype, w.d, [&](auto e, auto D) { return bwd_launch<decltype(e), decltype(D)::value>(w, pieces, key_pieces, st); });
+}
+
+int packed_dkv_plain_owned(int dtype, int d) {
+  return by_size(dtype, d, [&](auto e, auto D) { return Dkv<decltype(e), decltype(D)::value>::OWNED; });
+}
 
 }  // namespace mtnlg
