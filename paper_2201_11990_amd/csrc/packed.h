@@ -75,10 +75,32 @@ __device__ __forceinline__ Span span_of(const Sequences &s, int i) {
 }
 
 // Which sequence holds the place-th piece of work, and which of the sequence's pieces it is (at): count(span) says how many a sequence has.  Lengths are known
-// on the device only, so every wave looks for itself: a lane counts a few consecutive sequences, a sum over the lanes before it finds the lane, and again
-// inside that lane's sequences.  False: fewer pieces than places.
+// on the device only, so every wave looks for itself.  Up to 32 sequences, the ones with the most keys come first: what is left over at the end of a call are
+// the pieces of short ones.  More: a lane counts a few consecutive sequences, a sum over the lanes before it finds the lane, and again inside that lane's sequences.
+// False: fewer pieces than places.
 template <typename Count>
 __device__ __forceinline__ bool find_piece(const Sequences &s, unsigned place, Count &&count, Span &found, unsigned &at) {
+  if (s.count <= 32) {
+    const int i = threadIdx.x & 63;
+    unsigned mine = 0, before = 0;
+    int keys = -1;
+    if (i < s.count) {
+      const Span p = span_of(s, i);
+      mine = count(p);
+      keys = p.lk;
+    }
+    for (int o = 0; o < s.count; ++o) {
+      const int other = __builtin_amdgcn_readlane(keys, o);
+      const unsigned n = (unsigned)__builtin_amdgcn_readlane((int)mine, o);
+      before += other > keys || (other == keys && o < i) ? n : 0;
+    }
+    const uint64_t holds = __builtin_amdgcn_ballot_w64(place >= before && place - before < mine);
+    if (holds == 0) return false;
+    const int l = __builtin_ctzll(holds);
+    found = span_of(s, l);
+    at = place - (unsigned)__builtin_amdgcn_readlane((int)before, l);
+    return true;
+  }
   const int lane = threadIdx.x & 63;
   int first = 0, n = s.count;
   unsigned before = 0;
@@ -137,10 +159,10 @@ struct RowWalk {
     step = pitch * (uint32_t)tile_rows;
   }
   template <int TR>
-  __device__ __forceinline__ dma_rsrc_t tile() const {
+  __device__ __forceinline__ dma_rsrc_t tile(int row = 0) const {   // TR rows, from a row of the present tile on
     uint32_t records;
-    asm("s_max_i32 %0, %1, 0\n\ts_min_i32 %0, %0, %2\n\ts_mul_i32 %0, %0, %3" : "=&s"(records) : "s"(rows), "n"(TR), "s"(pitch) : "scc");
-    return dma_rsrc((const void *)base, records);
+    asm("s_max_i32 %0, %1, 0\n\ts_min_i32 %0, %0, %2\n\ts_mul_i32 %0, %0, %3" : "=&s"(records) : "s"(rows - row), "n"(TR), "s"(pitch) : "scc");
+    return dma_rsrc((const void *)(base + (uint32_t)row * pitch), records);
   }
   template <int TR>
   __device__ __forceinline__ void advance() {

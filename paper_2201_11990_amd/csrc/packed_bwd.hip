@@ -50,20 +50,21 @@ __global__ __launch_bounds__(DQ_THREADS, dq_per_unit<D>()) void packed_dq_kernel
   constexpr int IPW = 2 * T::NI;
   const int half = wave >> 1;   // waves 0, 1 bring 32 rows each of K, waves 2, 3 of V
   const Heads &mat = half ? w.v : w.k;
-  RowWalk stream(row_at<bf16>(mat, s.k0, j, 0), end, (uint32_t)(mat.token * 2), 64);
+  const int row0 = 32 * (wave & 1);
+  RowWalk stream(row_at<bf16>(mat, s.k0 + row0, j, 0), end - row0, (uint32_t)(mat.token * 2), 64);   // from the wave's rows on
   const uint32_t dst0 = smem_addr + half * T::BYTES + (wave & 1) * (2 * T::NI * 1024);
-  uint32_t dma_off[IPW];
+  uint32_t dma_off[T::NI];   // of 16 rows: the next 16 lie the same in a descriptor of their own
 #pragma unroll
-  for (int i = 0; i < IPW; ++i) dma_off[i] = T::dma_offset(stream.pitch, 2 * (wave & 1) + i / T::NI, lane, i % T::NI, d);
+  for (int i = 0; i < T::NI; ++i) dma_off[i] = T::dma_offset(stream.pitch, 0, lane, i, d);
   constexpr int ISSUE_STEPS = IPW / 2;   // (one tile ahead: it is waited for in the same iteration)
   auto issue_step = [&](int step, int st) {
 #pragma unroll
     for (int i = 0; i < IPW; ++i)
       if (i >= (step ? dma_by<IPW, ISSUE_STEPS>(step - 1) : 0) && i < dma_by<IPW, ISSUE_STEPS>(step))
-        dma16<Spread::value>(stream.tile<64>(), dst0 + st * STAGE + i * 1024, dma_off[i]);
+        dma16<Spread::value>(stream.tile<16>(16 * (i / T::NI)), dst0 + st * STAGE + i * 1024, dma_off[i % T::NI]);
   };
 #pragma unroll
-  for (int i = 0; i < IPW; ++i) dma16<Burst::value>(stream.tile<64>(), dst0 + i * 1024, dma_off[i]);
+  for (int i = 0; i < IPW; ++i) dma16<Burst::value>(stream.tile<16>(16 * (i / T::NI)), dst0 + i * 1024, dma_off[i % T::NI]);
   stream.advance<64>();
   bf16x8 of0[K1], of1[K1];   // own rows of q and da: columns 16 kk + 8 h .. + 7
   float dsum = 0.0f;
@@ -73,15 +74,19 @@ __global__ __launch_bounds__(DQ_THREADS, dq_per_unit<D>()) void packed_dq_kernel
 #pragma unroll
     for (int kk = 0; kk < K1; ++kk) {
       av[kk] = row_unit<bf16, D>(arow, kk, h, d);
-      of0[kk] = row_unit<bf16, D>(qrow, kk, h, d);
       of1[kk] = row_unit<bf16, D>(drow, kk, h, d);
+      of0[kk] = row_unit<bf16, D>(qrow, kk, h, d);
     }
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int kk = 0; kk < K1; ++kk) dsum = P::dot(av[kk], of1[kk], dsum);
+    for (int kk = 0; kk < K1; ++kk) {
+      dsum = P::dot(av[kk], of1[kk], dsum);
+      __builtin_amdgcn_sched_barrier(0);
+    }
   }
   dsum += __shfl_xor(dsum, 32, 64);
   const int64_t stat = (int64_t)head * w.where.q_tokens + s.q0 + tok;
-  if (mine < rows && h == 0 && part == 0) w.D[stat] = dsum;
+  if (mine < rows && h == 0 && part == 0) w.D[stat] = -dsum;   // as dP's accumulators start
   float lsf = w.lse[stat];
   lsf = lsf == -INFINITY ? INFINITY : lsf * kLog2e;   // a row that sees nothing: weights of 0
   float dneg = -dsum;
@@ -115,7 +120,7 @@ __global__ __launch_bounds__(DQ_THREADS, dq_per_unit<D>()) void packed_dq_kernel
   __builtin_amdgcn_sched_barrier(0);
 
   int cur = 0;
-  auto tile = [&](auto TAKEN, int it) __attribute__((always_inline)) {   // TAKEN: parts, SUBS or the first only
+  auto tile = [&](auto TAKEN, auto MASKED, int it) __attribute__((always_inline)) {   // TAKEN: parts, SUBS or the first only
     constexpr int N = decltype(TAKEN)::value * N1;
     ln.here();
     const int next = cur ^ 1;
@@ -137,9 +142,8 @@ __global__ __launch_bounds__(DQ_THREADS, dq_per_unit<D>()) void packed_dq_kernel
         if (r == 2 * K1) pc[e] *= sc[e];
       }
       if (r == 2 * K1) {
-        if (key0 + 31 > least) {   // wave-uniform: some rows do not see all of these keys
-          int seen = limit - key0 - 4 * h;
-          asm volatile("" : "+v"(seen));   // known here only: the compiler else does all this for every tile and drops the results
+        if constexpr (decltype(MASKED)::value) {
+          const int seen = limit - key0 - 4 * (lane_here() >> 5);
 #pragma unroll
           for (int e = 0; e < 16; ++e)
             if (8 * (e / 4) + e % 4 > seen) pc[e] = 0.0f;
@@ -164,15 +168,19 @@ __global__ __launch_bounds__(DQ_THREADS, dq_per_unit<D>()) void packed_dq_kernel
     stream.advance<64>();
     cur = next;
   };
-  const int all = most < 0 ? 0 : most / 32 + 1, visible = SPLIT == 2 ? (all + 1 - part) / 2 : all;   // 32-key parts with a key that a row sees; the rest is passed over
+  // 32-key parts with a key that a row of the wave sees, and of those the first ones, which all rows see whole: a loop without masks for them, which has fewer values
+  // to keep.  The parts after them are passed over.
+  auto parts_of = [&](int keys) { return SPLIT == 2 ? (keys / 32 + 1 - part) / 2 : keys / 32; };
+  const int visible = parts_of(most + 32), whole = parts_of(min(least, most) + 1) / SUBS;
   int it = 0;
-  for (; it < visible / SUBS; ++it) tile(std::integral_constant<int, SUBS>{}, it);
+  for (; it < whole; ++it) tile(std::integral_constant<int, SUBS>{}, std::false_type{}, it);
+  for (; it < visible / SUBS; ++it) tile(std::integral_constant<int, SUBS>{}, std::true_type{}, it);
   if constexpr (SUBS == 2) {
-    if (visible % 2) tile(std::integral_constant<int, 1>{}, it++);
+    if (visible % 2) tile(std::integral_constant<int, 1>{}, std::true_type{}, it++);
   }
   for (; it < ntiles; ++it) {   // passed over: its share of a later tile, and the barrier
 #pragma unroll
-    for (int i = 0; i < IPW; ++i) dma16<Burst::value>(stream.tile<64>(), dst0 + (cur ^ 1) * STAGE + i * 1024, dma_off[i]);
+    for (int i = 0; i < IPW; ++i) dma16<Burst::value>(stream.tile<16>(16 * (i / T::NI)), dst0 + (cur ^ 1) * STAGE + i * 1024, dma_off[i % T::NI]);
     wait_and_barrier<0>();
     stream.advance<64>();
     cur ^= 1;
@@ -180,7 +188,7 @@ __global__ __launch_bounds__(DQ_THREADS, dq_per_unit<D>()) void packed_dq_kernel
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");   // the look-ahead tiles, which nobody uses
 
   // SPLIT 2: the two waves with the same rows each hand over half of their column blocks' elements (q 0, 1 or 2, 3) and finish the other half
-  f32x4 *slots = reinterpret_cast<f32x4 *>(smem) + lane;
+  f32x4 *slots = reinterpret_cast<f32x4 *>(smem) + lane_here();
   if constexpr (SPLIT == 2) {
     int *const bad = reinterpret_cast<int *>(smem + 2 * 4 * CB * 1024);
     __syncthreads();   // the rings are no longer read
@@ -188,12 +196,14 @@ __global__ __launch_bounds__(DQ_THREADS, dq_per_unit<D>()) void packed_dq_kernel
     for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
       for (int q = 0; q < 2; ++q) slots[((wave * CB + cb) * 2 + q) * 64] = part ? quarter_of(acc[cb], q) : quarter_of(acc[cb], 2 + q);
-    if (lane == 0) bad[wave] = redo;
+    if (lane_here() == 0) bad[wave] = redo;
     __syncthreads();
     redo |= __builtin_amdgcn_readfirstlane(bad[wave ^ 2]) != 0;
   }
   if (own0 >= rows) return;
-  bf16 *const out = row_at<bf16>(w.dq, s.q0 + tok, j, g);
+  // where the row lies, worked out once more: registers less across the loop
+  const int last = own0 + (lane_here() & 31), out_row = min(last, rows - 1), out_tok = out_row / r, out_g = out_row - out_tok * r, out_h = lane_here() >> 5;
+  bf16 *const out = row_at<bf16>(w.dq, s.q0 + out_tok, j, out_g);
   if (redo) {   // key by key, without matrix instructions (packed_fwd.hip: why)
     if (part) return;
     float sum[K1][8];
@@ -201,40 +211,40 @@ __global__ __launch_bounds__(DQ_THREADS, dq_per_unit<D>()) void packed_dq_kernel
     for (int kk = 0; kk < K1; ++kk)
 #pragma unroll
       for (int e = 0; e < 8; ++e) sum[kk][e] = 0.0f;
-    const bf16 *qrow = row_at<bf16>(w.q, s.q0 + tok, j, g), *drow = row_at<bf16>(w.da, s.q0 + tok, j, g);
+    const bf16 *qrow = row_at<bf16>(w.q, s.q0 + out_tok, j, out_g), *drow = row_at<bf16>(w.da, s.q0 + out_tok, j, out_g);
 #pragma unroll 1
     for (int key = 0; key <= most; ++key) {
       const bf16 *kr = row_at<bf16>(w.k, s.k0 + key, j, 0), *vr = row_at<bf16>(w.v, s.k0 + key, j, 0);
       float sk = 0.0f, dp = 0.0f;
 #pragma unroll
       for (int kk = 0; kk < K1; ++kk) {
-        sk = P::dot(row_unit<bf16, D>(kr, kk, h, d), row_unit<bf16, D>(qrow, kk, h, d), sk);
-        dp = P::dot(row_unit<bf16, D>(vr, kk, h, d), row_unit<bf16, D>(drow, kk, h, d), dp);
+        sk = P::dot(row_unit<bf16, D>(kr, kk, out_h, d), row_unit<bf16, D>(qrow, kk, out_h, d), sk);
+        dp = P::dot(row_unit<bf16, D>(vr, kk, out_h, d), row_unit<bf16, D>(drow, kk, out_h, d), dp);
         __builtin_amdgcn_sched_barrier(0);   // few reads at once: no registers for more
       }
       sk += __shfl_xor(sk, 32, 64);
       dp += __shfl_xor(dp, 32, 64);
-      if (key > limit) continue;
+      if (key > out_tok + shift) continue;
       const float ds = fast_exp2(fmaf(sk, f, -lsf)) * (dp + dneg);
 #pragma unroll
       for (int kk = 0; kk < K1; ++kk) {
-        const bf16x8 k = row_unit<bf16, D>(kr, kk, h, d);
+        const bf16x8 k = row_unit<bf16, D>(kr, kk, out_h, d);
 #pragma unroll
         for (int e = 0; e < 8; ++e) sum[kk][e] = fmaf(ds, (float)k[e], sum[kk][e]);
         __builtin_amdgcn_sched_barrier(0);
       }
     }
-    if (mine >= rows) return;
+    if (last >= rows) return;
 #pragma unroll
     for (int kk = 0; kk < K1; ++kk)
 #pragma unroll
       for (int e = 0; e < 8; e += 4)
-        if (16 * kk + 8 * h < d) put4(out + 16 * kk + 8 * h + e, f32x4{sum[kk][e], sum[kk][e + 1], sum[kk][e + 2], sum[kk][e + 3]} * w.scale);
+        if (16 * kk + 8 * out_h < d) put4(out + 16 * kk + 8 * out_h + e, f32x4{sum[kk][e], sum[kk][e + 1], sum[kk][e + 2], sum[kk][e + 3]} * w.scale);
     return;
   }
-  if (mine >= rows) return;
+  if (last >= rows) return;
   auto put = [&](int cb, int q, f32x4 v) {   // columns 32 cb + 8 q + 4 h .. + 3
-    const int col = 32 * cb + 8 * q + 4 * h;
+    const int col = 32 * cb + 8 * q + 4 * out_h;
     if (col < d) put4(out + col, v * w.scale);
   };
 #pragma unroll
@@ -260,7 +270,7 @@ __global__ __launch_bounds__(DQ_THREADS, dq_per_unit<D>()) void packed_dq_kernel
 constexpr int DKV_THREADS = 512;
 template <int D, int OWNED> struct DkvLds {
   static constexpr int ROWS = OWNED == 128 ? 32 : 64, GROUPS = OWNED / 32, PARTS = ROWS / 32, PAIRS = GROUPS * PARTS;
-  static constexpr int MATRIX = ROWS * D * 2, STAGE = 2 * MATRIX + 512;   // Q tile, dO tile, 256 bytes each of lse and D
+  static constexpr int MATRIX = ROWS * D * 2, STAGE = 2 * MATRIX + 512;   // Q tile, dO tile, 256 bytes each of lse and -D
   static constexpr int XCHG = PAIRS * 4096;                               // P of a tile
   static constexpr int ROOM = 160 * 1024;
   static constexpr int RING = 4 * STAGE + 2 * XCHG <= ROOM ? 4 : 3, AHEAD = RING - 2;   // tiles in LDS, and fetched ahead
@@ -297,36 +307,35 @@ __global__ __launch_bounds__(DKV_THREADS) void packed_dkv_kernel(PackedBwdArgs w
   typename P::Lane ln(lane);
   const uint32_t smem_addr = lds_address(smem);
 
-  // The tile's instructions dealt out over the waves: matrices (Q, dO), bands of 16 rows, NI each; and its lse values (even waves) or D values (odd ones), several
-  // times over, so that every wave issues the same number of memory operations, which the counted waits rely on.
-  constexpr int ALL = 2 * (ROWS / 16) * T::NI, IPW = (ALL + 7) / 8, OPS = IPW + 1;
-  auto second_of = [&](int i) { return (wave + 8 * i) % ALL / (ALL / 2); };
-  auto in_of = [&](int i) { return (wave + 8 * i) % ALL % (ALL / 2); };
-  const uint32_t qp = (uint32_t)(w.q.token * 2), dp = (uint32_t)(w.da.token * 2);
+  // Waves 0-3 bring the Q tile, waves 4-7 the dO tile (bands of 16 rows, NI instructions each, dealt out over the four; what does not come out even is brought twice), and
+  // every wave the tile's lse values (even waves) or -D values (odd ones): all issue the same number of memory operations, which the counted waits rely on.
+  constexpr int ALL = ROWS / 16 * T::NI, IPW = (ALL + 3) / 4, OPS = IPW + 1;
+  const int half = wave >> 2;
+  const Heads &mat = half ? w.da : w.q;
+  const uint32_t pitch = (uint32_t)(mat.token * 2);
+  auto instruction = [&](int i) { return ((wave & 3) + 4 * i) % ALL; };
   uint32_t dma_off[IPW];
 #pragma unroll
-  for (int i = 0; i < IPW; ++i) dma_off[i] = T::dma_offset(second_of(i) ? dp : qp, in_of(i) / T::NI, lane, in_of(i) % T::NI, d);
-  const float *const stat_base = wave & 1 ? w.D : w.lse;
-  auto stat_at = [&](int g) { return stat_base + (int64_t)(j * r + g) * w.where.q_tokens + s.q0 + first; };
-  RowWalk qs(row_at<bf16>(w.q, s.q0 + first, j, g0), s.lq - first, qp, ROWS), ds(row_at<bf16>(w.da, s.q0 + first, j, g0), s.lq - first, dp, ROWS);
-  RowWalk stats(stat_at(g0), s.lq - first, 4, ROWS);
+  for (int i = 0; i < IPW; ++i) dma_off[i] = T::dma_offset(pitch, instruction(i) / T::NI, lane, instruction(i) % T::NI, d);
+  auto rows_at = [&](int g) { return RowWalk(row_at<bf16>(mat, s.q0 + first, j, g), s.lq - first, pitch, ROWS); };
+  auto stats_at = [&](int g) {
+    return RowWalk((wave & 1 ? w.D : w.lse) + ((int64_t)(j * r + g) * w.where.q_tokens + s.q0 + first), s.lq - first, 4, ROWS);
+  };
+  RowWalk stream = rows_at(g0), stats = stats_at(g0);
   int to_come = tiles, g_in = g0;   // tiles of the head g_in that have not been fetched
   auto issue_one = [&](auto tag, int st, int i) {   // i == IPW: the statistics (with tiles of 32 rows those of the next tile as well, unused)
     constexpr int TAG = decltype(tag)::value;
     const uint32_t stage = smem_addr + st * STAGE;
     if (i == IPW) dma4<TAG>(stats.tile<64>(), stage + 2 * L::MATRIX + (wave & 1) * 256, lane * 4);
-    else dma16<TAG>(second_of(i) ? ds.tile<ROWS>() : qs.tile<ROWS>(), stage + second_of(i) * L::MATRIX + in_of(i) * 1024, dma_off[i]);
+    else dma16<TAG>(stream.tile<ROWS>(), stage + half * L::MATRIX + instruction(i < IPW ? i : 0) * 1024, dma_off[i < IPW ? i : 0]);
   };
   auto advance = [&] {
-    qs.advance<ROWS>();
-    ds.advance<ROWS>();
+    stream.advance<ROWS>();
     stats.advance<ROWS>();
     if (--to_come == 0 && g_in + 1 < g1) {   // the next head of the group
-      ++g_in;
       to_come = tiles;
-      qs = RowWalk(row_at<bf16>(w.q, s.q0 + first, j, g_in), s.lq - first, qp, ROWS);
-      ds = RowWalk(row_at<bf16>(w.da, s.q0 + first, j, g_in), s.lq - first, dp, ROWS);
-      stats = RowWalk(stat_at(g_in), s.lq - first, 4, ROWS);
+      stream = rows_at(++g_in);
+      stats = stats_at(g_in);
     }
   };
   auto issue_tile = [&](int st) {
@@ -428,7 +437,7 @@ __global__ __launch_bounds__(DKV_THREADS) void packed_dkv_kernel(PackedBwdArgs w
         for (int q = 0; q < 4; ++q) {
           const f32x4 v = *reinterpret_cast<const f32x4 *>(stat + 64 + 8 * q);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) sc[4 * q + e] = -v[e];
+          for (int e = 0; e < 4; ++e) sc[4 * q + e] = v[e];
         }
       }
       auto step = [&](auto I) __attribute__((always_inline)) {
@@ -453,7 +462,7 @@ __global__ __launch_bounds__(DKV_THREADS) void packed_dkv_kernel(PackedBwdArgs w
           for (int e = 0; e < 16; ++e)
             if (r == 2 + e * (K1 - 2) / 16) prev[e] *= p[e];
           if (r == K1) {
-            if (it > 0 && masked(row_before)) {
+            if (masked(row_before)) {   // (before the first tile there is none: this looks at the first, which comes again)
               hide(row_before, prev);
               redo |= rows_not_finite<bf16, D>(before + SECOND_AT + part_rows, ln);
             }
@@ -561,7 +570,7 @@ __global__ __launch_bounds__(DKV_THREADS) void packed_dkv_kernel(PackedBwdArgs w
         if (q + shift < mine) continue;
         const int64_t stat = (int64_t)(j * r + g) * w.where.q_tokens + s.q0 + q;
         float weight = fast_exp2(fmaf(sk, f, -w.lse[stat] * kLog2e));
-        if (role) weight *= dpk - w.D[stat];
+        if (role) weight *= dpk + w.D[stat];
 #pragma unroll
         for (int kk = 0; kk < K1; ++kk) {
           const bf16x8 v = row_unit<bf16, D>(role ? qr : dr, kk, h, d);

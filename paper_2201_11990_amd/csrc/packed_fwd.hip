@@ -98,21 +98,21 @@ __global__ __launch_bounds__(64 * WAVES, per_unit<D>()) void packed_fwd_kernel(P
   constexpr int IPW = 2 * T::NI;
   const int half = wave >> 1, band = 2 * (wave & 1);
   const Heads &mat = half ? w.v : w.k;
-  RowWalk stream(row_at<bf16>(mat, s.k0 + begin, j, 0), end - begin, (uint32_t)(mat.token * 2), 64);
-  uint32_t dma_off[IPW];
+  RowWalk stream(row_at<bf16>(mat, s.k0 + begin + 16 * band, j, 0), end - begin - 16 * band, (uint32_t)(mat.token * 2), 64);   // from the wave's rows on
+  uint32_t dma_off[T::NI];   // of 16 rows: the next 16 lie the same in a descriptor of their own
 #pragma unroll
-  for (int i = 0; i < IPW; ++i) dma_off[i] = T::dma_offset(stream.pitch, band + i / T::NI, lane, i % T::NI, d);
+  for (int i = 0; i < T::NI; ++i) dma_off[i] = T::dma_offset(stream.pitch, 0, lane, i, d);
   const uint32_t dst0 = smem_addr + half * T::BYTES + band * (T::NI * 1024);
   constexpr int ISSUE_STEPS = IPW / 2;   // (one tile ahead: it is waited for in the same iteration)
   auto issue_step = [&](int step, int st) {
 #pragma unroll
     for (int i = 0; i < IPW; ++i)
       if (i >= (step ? dma_by<IPW, ISSUE_STEPS>(step - 1) : 0) && i < dma_by<IPW, ISSUE_STEPS>(step))
-        dma16<Spread::value>(stream.tile<64>(), dst0 + st * STAGE + i * 1024, dma_off[i]);
+        dma16<Spread::value>(stream.tile<16>(16 * (i / T::NI)), dst0 + st * STAGE + i * 1024, dma_off[i % T::NI]);
   };
   bf16x8 qf[K1];   // own rows: columns 16 kk + 8 h .. + 7
 #pragma unroll
-  for (int i = 0; i < IPW; ++i) dma16<Burst::value>(stream.tile<64>(), dst0 + i * 1024, dma_off[i]);
+  for (int i = 0; i < IPW; ++i) dma16<Burst::value>(stream.tile<16>(16 * (i / T::NI)), dst0 + i * 1024, dma_off[i % T::NI]);
   stream.advance<64>();
   {
     const bf16 *qrow = row_at<bf16>(w.q, s.q0 + tok, j, g);
@@ -143,7 +143,7 @@ __global__ __launch_bounds__(64 * WAVES, per_unit<D>()) void packed_fwd_kernel(P
   __builtin_amdgcn_sched_barrier(0);
 
   int cur = 0;
-  auto tile = [&](auto TAKEN, int it) __attribute__((always_inline)) {   // TAKEN: parts, SUBS or the first only
+  auto tile = [&](auto TAKEN, auto MASKED, int it) __attribute__((always_inline)) {   // TAKEN: parts, SUBS or the first only
     constexpr int N = decltype(TAKEN)::value * N1;
     ln.here();
     const int next = cur ^ 1;   // stage of tile it + 1
@@ -154,9 +154,8 @@ __global__ __launch_bounds__(64 * WAVES, per_unit<D>()) void packed_fwd_kernel(P
       if (r == 0) sc = f32x16{};
       if (r == K1) {
         // element e: key key0 + 8 (e / 4) + 4 h + e % 4
-        if (key0 + 31 > least) {  // wave-uniform: some rows do not see all of these keys
-          int seen = limit - key0 - 4 * h;
-          asm volatile("" : "+v"(seen));   // known here only: the compiler else does all this for every tile and drops the results
+        if constexpr (decltype(MASKED)::value) {
+          const int seen = limit - key0 - 4 * (lane_here() >> 5);
 #pragma unroll
           for (int e = 0; e < 16; ++e)
             if (8 * (e / 4) + e % 4 > seen) sc[e] = -INFINITY;
@@ -202,16 +201,19 @@ __global__ __launch_bounds__(64 * WAVES, per_unit<D>()) void packed_fwd_kernel(P
     stream.advance<64>();
     cur = next;
   };
-  // How many 32-key parts this wave takes: those with a key that one of its rows sees.  The rest, at the end, it passes over.
-  const int all = most < begin ? 0 : (most - begin) / 32 + 1, visible = SPLIT == 2 ? (all + 1 - part) / 2 : all;
+  // 32-key parts with a key that a row of the wave sees, and of those the first ones, which all rows see whole: a loop without masks for them, which has fewer values
+  // to keep.  The parts after them are passed over.
+  auto parts_of = [&](int keys) { return SPLIT == 2 ? (keys / 32 + 1 - part) / 2 : keys / 32; };
+  const int visible = parts_of(most - begin + 32), whole = parts_of(min(least, most) - begin + 1) / SUBS;
   int it = 0;
-  for (; it < visible / SUBS; ++it) tile(std::integral_constant<int, SUBS>{}, it);
+  for (; it < whole; ++it) tile(std::integral_constant<int, SUBS>{}, std::false_type{}, it);
+  for (; it < visible / SUBS; ++it) tile(std::integral_constant<int, SUBS>{}, std::true_type{}, it);
   if constexpr (SUBS == 2) {
-    if (visible % 2) tile(std::integral_constant<int, 1>{}, it++);
+    if (visible % 2) tile(std::integral_constant<int, 1>{}, std::true_type{}, it++);
   }
   for (; it < ntiles; ++it) {   // passed over: its share of the next tile, and the barrier
 #pragma unroll
-    for (int i = 0; i < IPW; ++i) dma16<Burst::value>(stream.tile<64>(), dst0 + (cur ^ 1) * STAGE + i * 1024, dma_off[i]);
+    for (int i = 0; i < IPW; ++i) dma16<Burst::value>(stream.tile<16>(16 * (i / T::NI)), dst0 + (cur ^ 1) * STAGE + i * 1024, dma_off[i % T::NI]);
     wait_and_barrier<0>();
     stream.advance<64>();
     cur ^= 1;
@@ -219,17 +221,19 @@ __global__ __launch_bounds__(64 * WAVES, per_unit<D>()) void packed_fwd_kernel(P
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");   // the look-ahead tiles, which nobody uses
 
   l += __shfl_xor(l, 32, 64);
+  // lane, own row and where it lies, worked out once more: registers less across the loop
+  const int out_lane = lane_here(), out_h = out_lane >> 5, last = own0 + (out_lane & 31), out_row = min(last, rows - 1), out_tok = out_row / r, out_g = out_row - out_tok * r;
   if constexpr (SPLIT == 2) {   // the part's results relative to the larger of the two maxima
-    f32x4 *slots = reinterpret_cast<f32x4 *>(smem) + lane;
+    f32x4 *slots = reinterpret_cast<f32x4 *>(smem) + out_lane;
     float *const stat = reinterpret_cast<float *>(smem + 2 * WAVES * CB * 1024);   // maximum and sum of each wave
     int *const bad = reinterpret_cast<int *>(stat + WAVES * 128);
     __syncthreads();   // the rings are no longer read
-    stat[wave * 128 + lane] = m;
-    stat[wave * 128 + 64 + lane] = l;
-    if (lane == 0) bad[wave] = redo;
+    stat[wave * 128 + out_lane] = m;
+    stat[wave * 128 + 64 + out_lane] = l;
+    if (out_lane == 0) bad[wave] = redo;
     __syncthreads();
     redo |= __builtin_amdgcn_readfirstlane(bad[other]) != 0;
-    const float mo = stat[other * 128 + lane], lo = stat[other * 128 + 64 + lane], both = fmaxf(m, mo), ref = both == -INFINITY ? 0.0f : both;
+    const float mo = stat[other * 128 + out_lane], lo = stat[other * 128 + 64 + out_lane], both = fmaxf(m, mo), ref = both == -INFINITY ? 0.0f : both;
     auto relative = [&](float x) { return fast_exp2((x - ref) * c); };
     const float mul = relative(m);
     l = part ? fmaf(l, mul, lo * relative(mo)) : fmaf(lo, relative(mo), l * mul);
@@ -244,11 +248,11 @@ __global__ __launch_bounds__(64 * WAVES, per_unit<D>()) void packed_fwd_kernel(P
     __syncthreads();
   }
   if (own0 >= rows) return;
-  const int head = j * r + g;
-  const int64_t id = (int64_t)(s.q0 + tok) * ((int64_t)w.kv_heads * r) + head, place = chunk * ((int64_t)w.where.q_tokens * w.kv_heads * r) + id;
-  bf16 *const out = row_at<bf16>(w.a, s.q0 + tok, j, g);
-  float *const to = w.part + place * d, *const out_lse = w.lse + (int64_t)head * w.where.q_tokens + s.q0 + tok;
-  const bool none = tok + shift < 0;   // the row sees no key
+  const int head = j * r + out_g;
+  const int64_t id = (int64_t)(s.q0 + out_tok) * ((int64_t)w.kv_heads * r) + head, place = chunk * ((int64_t)w.where.q_tokens * w.kv_heads * r) + id;
+  bf16 *const out = row_at<bf16>(w.a, s.q0 + out_tok, j, out_g);
+  float *const to = w.part + place * d, *const out_lse = w.lse + (int64_t)head * w.where.q_tokens + s.q0 + out_tok;
+  const bool none = out_tok + shift < 0;   // the row sees no key
   auto statistics = [&](float m, float l) {
     if (chunked) *reinterpret_cast<float2 *>(w.stat + 2 * place) = float2{m, l};
     else *out_lse = none ? -INFINITY : plus_log(product_of(m, w.scale), l);
@@ -256,12 +260,12 @@ __global__ __launch_bounds__(64 * WAVES, per_unit<D>()) void packed_fwd_kernel(P
   if (redo) {
     if (part) return;
     RowByRow<D> again;
-    again.run(w, s, j, row_at<bf16>(w.q, s.q0 + tok, j, g), begin, most, limit, h);
-    if (mine >= rows) return;
+    again.run(w, s, j, row_at<bf16>(w.q, s.q0 + out_tok, j, out_g), begin, most, min(out_tok + shift, end - 1), out_h);
+    if (last >= rows) return;
     const float inv = none ? 0.0f : 1.0f / again.l;
 #pragma unroll
     for (int kk = 0; kk < K1; ++kk) {
-      const int col = 16 * kk + 8 * h;
+      const int col = 16 * kk + 8 * out_h;
       if (col >= d) continue;
 #pragma unroll
       for (int e = 0; e < 8; e += 4) {
@@ -270,13 +274,13 @@ __global__ __launch_bounds__(64 * WAVES, per_unit<D>()) void packed_fwd_kernel(P
         else put4(out + col + e, v * inv);
       }
     }
-    if (h == 0) statistics(again.m, again.l);
+    if (out_h == 0) statistics(again.m, again.l);
     return;
   }
-  if (mine >= rows) return;
+  if (last >= rows) return;
   const float inv = none ? 0.0f : 1.0f / l;
-  auto put = [&](int cb, int q, f32x4 sum) {   // columns 32 cb + 8 q + 4 h .. + 3
-    const int col = 32 * cb + 8 * q + 4 * h;
+  auto put = [&](int cb, int q, f32x4 sum) {   // columns 32 cb + 8 q + 4 out_h .. + 3
+    const int col = 32 * cb + 8 * q + 4 * out_h;
     if (col >= d) return;
     if (chunked) *reinterpret_cast<f32x4 *>(to + col) = sum;
     else put4(out + col, sum * inv);
@@ -284,7 +288,7 @@ __global__ __launch_bounds__(64 * WAVES, per_unit<D>()) void packed_fwd_kernel(P
 #pragma unroll
   for (int cb = 0; cb < CB; ++cb) {
     if constexpr (SPLIT == 2) {
-      const f32x4 *slots = reinterpret_cast<const f32x4 *>(smem) + lane;
+      const f32x4 *slots = reinterpret_cast<const f32x4 *>(smem) + out_lane;
 #pragma unroll
       for (int q = 0; q < 2; ++q) {
         const f32x4 rest = slots[((other * CB + cb) * 2 + q) * 64];
@@ -296,7 +300,7 @@ __global__ __launch_bounds__(64 * WAVES, per_unit<D>()) void packed_fwd_kernel(P
       for (int q = 0; q < 4; ++q) put(cb, q, quarter_of(o[cb], q));
     }
   }
-  if (h == 0 && part == 0) statistics(m, l);
+  if (out_h == 0 && part == 0) statistics(m, l);
 }
 
 template <int D, int SPLIT>
