@@ -28,7 +28,16 @@ __global__ __launch_bounds__(256) void packed_join_kernel(PackedFwdArgs w) {
   const float total = wave_sum(l * mul);
   f32x4 o = {};
   const float *from = w.part + id * d + (lane * 4 < d ? lane * 4 : 0);   // lanes past the columns go along: the others take the chunks' factors from them
-  for (int i = 0; i < nc; ++i) o += *reinterpret_cast<const f32x4 *>(from + i * all * d) * __shfl(mul, i, 64);
+  for (int i = 0; i < nc; i += 4) {   // four reads in flight (of the last chunk again past the end, where the factors are 0)
+    f32x4 v[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) v[u] = *reinterpret_cast<const f32x4 *>(from + min(i + u, nc - 1) * all * d);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const float f = __shfl(mul, i + u, 64);
+      if (i + u < nc) o += v[u] * f;   // (an infinity there is read again: not times 0)
+    }
+  }
   if (lane * 4 < d) put4(row_at<E>(w.a, s.q0 + tok, j, g) + lane * 4, o * (nc ? 1.0f / total : 0.0f));
   if (lane == 0) w.lse[(int64_t)head * w.where.q_tokens + s.q0 + tok] = nc ? plus_log(product_of(most, w.scale), total) : -INFINITY;
 }
@@ -54,6 +63,15 @@ __global__ __launch_bounds__(256) void packed_dkv_join_kernel(PackedBwdArgs w) {
 }
 
 // How the keys are cut where the rows alone leave most of the chip idle.
+#ifndef CUT_INTO
+#define CUT_INTO 1024
+#endif
+#ifndef CUT_BELOW
+#define CUT_BELOW 512
+#endif
+#ifndef CUT_LEAST
+#define CUT_LEAST 256
+#endif
 struct FwdPlan {
   int owned;
   int64_t pieces;   // workgroups of a head of keys at most, without cuts
@@ -71,10 +89,10 @@ FwdPlan fwd_plan(const PackedShape &S) {
   }
   p.chunks = 1;
   const int64_t wide = p.pieces * S.kv_heads;
-  if (wide < 256 && S.max_k > 512) {
-    int64_t chunk = (int64_t)S.max_k * wide / 1024;   // about four to a unit
-    chunk = chunk < 256 ? 256 : chunk;
-    if (chunk * 64 < S.max_k) chunk = (S.max_k + 63) / 64;
+  if (wide < CUT_BELOW && S.max_k > 2 * CUT_LEAST) {
+    int64_t chunk = wide * (S.where.k_tokens / S.where.count) / CUT_INTO;
+    chunk = chunk < CUT_LEAST ? CUT_LEAST : chunk;
+    if (chunk * 64 < S.max_k) chunk = (S.max_k + 63) / 64;   // a lane of the joining wave to each
     chunk = (chunk + 63) / 64 * 64;
     p.chunk = (int)chunk;
     p.chunks = (int)((S.max_k + chunk - 1) / chunk);

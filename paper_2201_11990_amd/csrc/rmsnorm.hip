@@ -157,6 +157,18 @@ int fwd_launch(const NormArgs &a, hipStream_t st) {
 }
 
 // ------------------------------------------------------------------ backward
+// as loaded, not as eight floats (the compiler else widens them once, for all rows)
+__device__ __forceinline__ void keep(Raw8<bf16> &r) { asm volatile("" : "+v"(r.v)); }
+__device__ __forceinline__ void keep(Raw8<float> &) {}
+
+typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
+// the lane's number, worked out where it stands
+__device__ __forceinline__ int lane_of() {
+  int lane;
+  asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(lane));
+  return lane;
+}
+
 struct NormBwdArgs {
   int64_t rows;
   int h;
@@ -166,83 +178,71 @@ struct NormBwdArgs {
   float *partial;   // [workgroups][h]: the workgroup's rows of dgamma
 };
 
-// A workgroup takes every gridDim.x-th row (of each of its ROWS groups of waves) and sums its share of dgamma in registers.  bf16: the next row is
-// requested before the present one is reduced, so the loads of a row travel behind the barriers of the other; a row of fp32 has no registers for that.
+// A workgroup takes every gridDim.x-th row (of each of its ROWS groups of waves) and sums its share of dgamma in registers.  The next row is requested before the
+// present one is reduced, so that the loads of a row travel behind the barriers of the other.  Rows up to 8192 columns; longer ones have no registers for a row ahead.
 template <typename E, int W, int NV>
 __global__ __launch_bounds__(threads_of<W>()) void rmsnorm_bwd_kernel(NormBwdArgs a) {
   constexpr int LANES = 64 * W, ROWS = threads_of<W>() / LANES;
-  constexpr bool AHEAD = sizeof(E) == 2;
   __shared__ float red[16];
   __shared__ __attribute__((aligned(16))) float side[ROWS > 1 ? (ROWS - 1) * LANES * NV * 8 : 1];
-  const int at = threadIdx.x % LANES, group = threadIdx.x / LANES, nvec = a.h / 8;
+  const int at = threadIdx.x % LANES, group = ROWS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / LANES), nvec = a.h / 8;
   const int64_t step = (int64_t)gridDim.x * ROWS;
-  struct Row { Raw8<E> x[NV], dout[NV]; };
+  struct Row { Raw8<E> x[NV], dout[NV], dres[NV]; };
   float dg[NV][8] = {};
+  const bool with_dres = a.dres != nullptr;
   auto request = [&](int64_t row, Row &to) __attribute__((always_inline)) {
+    if (row >= a.rows) return;
+    const int64_t from = row * a.h + 8 * at;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int j = at + i * LANES;
-      if (j < nvec && row < a.rows) {
-        to.x[i].load(static_cast<const E *>(a.x) + row * a.h + 8 * j);
-        to.dout[i].load(static_cast<const E *>(a.dout) + row * a.h + 8 * j);
+      if (at + i * LANES < nvec) {
+        to.x[i].load(static_cast<const E *>(a.x) + from + 8 * LANES * i);
+        to.dout[i].load(static_cast<const E *>(a.dout) + from + 8 * LANES * i);
+        if (with_dres) to.dres[i].load(static_cast<const E *>(a.dres) + from + 8 * LANES * i);
       }
     }
   };
   int64_t row = (int64_t)blockIdx.x * ROWS + group;
   Row next;
-  if constexpr (AHEAD) request(row, next);
-  const E *gamma = static_cast<const E *>(a.gamma);
+  request(row, next);
+  // gamma stays in registers: a load of it behind the next row's would be waited for after them
+  Raw8<E> gamma[NV];
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+    if (at + i * LANES < nvec) gamma[i].load(static_cast<const E *>(a.gamma) + 8 * at + 8 * LANES * i);
   // the same number of turns for all waves of a row's group; a group without a row left has none
   for (; row < a.rows; row += step) {
     const float r = a.rstd[row];
-    asm volatile("" : "+s"(gamma));   // read again for every row, from the caches: its values in registers would leave none for a row ahead
-    Row now;
-    if constexpr (AHEAD) {
-      now = next;
-      request(row + step, next);
-    } else {
-      request(row, now);
-    }
-    Raw8<E> dres[NV];
-    if (AHEAD && a.dres) {   // fp32: after the reduction, where the registers of the products are free
-#pragma unroll
-      for (int i = 0; i < NV; ++i)
-        if (at + i * LANES < nvec) dres[i].load(static_cast<const E *>(a.dres) + row * a.h + 8 * (at + i * LANES));
-    }
+    const Row now = next;
+    request(row + step, next);
     float dot = 0.0f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int j = at + i * LANES;
-      if (j < nvec) {
-        float g[8];
-        load8(gamma + 8 * j, g);
+      if (at + i * LANES < nvec) {
+        keep(gamma[i]);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const float n = now.x[i][e] * r;
-          dot += now.dout[i][e] * g[e] * n;
+          dot += now.dout[i][e] * gamma[i][e] * n;
           dg[i][e] += now.dout[i][e] * n;
         }
       }
+      __builtin_amdgcn_sched_barrier(0);   // eight columns at a time: all of them in fp32 at once do not fit beside the next row
     }
     const float mean = row_sum<W>(dot, red) / (float)a.h;
-    asm volatile("" : "+s"(gamma));
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int j = at + i * LANES;
-      if (j < nvec) {
-        float g[8], o[8];
-        load8(gamma + 8 * j, g);
+      if (at + i * LANES < nvec) {
+        float o[8];
+        keep(gamma[i]);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          o[e] = r * (now.dout[i][e] * g[e] - now.x[i][e] * r * mean);
+          o[e] = r * (now.dout[i][e] * gamma[i][e] - now.x[i][e] * r * mean);
+          if (with_dres) o[e] += now.dres[i][e];
         }
-        if (a.dres) {
-          if constexpr (!AHEAD) dres[i].load(static_cast<const E *>(a.dres) + row * a.h + 8 * j);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) o[e] += dres[i][e];
-        }
-        store8(static_cast<E *>(a.dx) + row * a.h + 8 * j, o);
+        store8(static_cast<E *>(a.dx) + row * a.h + 8 * at + 8 * LANES * i, o);
       }
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
   if constexpr (ROWS > 1) {   // the groups' sums, in their order
@@ -265,6 +265,139 @@ __global__ __launch_bounds__(threads_of<W>()) void rmsnorm_bwd_kernel(NormBwdArg
 #pragma unroll
   for (int i = 0; i < NV; ++i)
     if (at + i * LANES < nvec) store8(a.partial + (int64_t)blockIdx.x * a.h + 8 * (at + i * LANES), dg[i]);
+}
+
+// Rows of more than 8192 columns, 16 waves to a row.  The next row comes into LDS by DMA while the present one is in registers: every wave brings what it reads itself, so that
+// no barrier stands between.  PRE: of x, dout and dres those that LDS has room for (the others are loaded with their row).  Where dres is not ahead its place is taken before the next
+// row's DMA goes out, since memory operations are waited for in their order; dx goes out by buffer stores, of which every wave has the same number (what lies past the
+// row is dropped), so that the next row can be waited for and they not.
+template <typename E, int NV, int PRE>
+__global__ __launch_bounds__(1024) void rmsnorm_bwd_wide_kernel(NormBwdArgs a) {
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  __shared__ float red[16];
+  constexpr int ES = sizeof(E), HALVES = ES / 2, SEG = 64 * 8 * ES, STORES = NV * HALVES;   // SEG: a wave's bytes of a piece
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), nvec = a.h / 8;
+  const bool with_dres = a.dres != nullptr;
+  const uint32_t bytes = (uint32_t)a.h * ES;
+  char *const mine = smem + wave * (PRE * NV * SEG);
+  const uint32_t lds0 = lds_address(mine);
+  const char *const from[3] = {static_cast<const char *>(a.x), static_cast<const char *>(a.dout), static_cast<const char *>(a.dres)};
+  auto fetch = [&](int64_t row) {
+    const uint32_t here = (uint32_t)(wave * SEG + lane_of() * 16);   // worked out where it stands: no registers for offsets across the loop
+#pragma unroll
+    for (int m = 0; m < PRE; ++m) {
+      if (m == 2 && !with_dres) continue;
+      const dma_rsrc_t rs = dma_rsrc(from[m] + row * bytes, __builtin_amdgcn_readfirstlane(bytes));
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int k = 0; k < HALVES; ++k) dma16(rs, lds0 + (m * NV + i) * SEG + k * 1024, here + i * 16 * SEG + k * 1024);
+    }
+  };
+  auto column = [&](int i) { return (i * 1024 + wave * 64 + lane) * 8; };
+  auto take = [&](int m, int i, int64_t row) {
+    Raw8<E> r{};
+    if (m < PRE) r.load(reinterpret_cast<const E *>(mine + (m * NV + i) * SEG) + lane * 8);
+    else if (column(i) < a.h) r.load(reinterpret_cast<const E *>(from[m]) + row * a.h + column(i));
+    return r;
+  };
+  auto sum_over = [&](float v) {   // of the row, without waiting for memory
+    v = wave_sum(v);
+    asm volatile("s_barrier" ::: "memory");   // read the last time
+    if (lane == 0) red[wave] = v;
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    v = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v += red[i];
+    return v;
+  };
+  Raw8<E> gamma[NV];
+  float dg[NV][8] = {};
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    gamma[i] = Raw8<E>{};
+    if (column(i) < a.h) gamma[i].load(static_cast<const E *>(a.gamma) + column(i));
+  }
+  int64_t row = blockIdx.x;
+  float r_next = a.rstd[row];
+  fetch(row);
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  for (; row < a.rows; row += gridDim.x) {
+    float r = r_next;
+    asm volatile("" : "+v"(r));   // here: a wait for it behind the next row's DMA would be one for that too
+    Raw8<E> x[NV], d[NV], res[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      x[i] = take(0, i, row);
+      d[i] = take(1, i, row);
+      if (with_dres) res[i] = take(2, i, row);
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {   // here, before the next row's go out
+      keep(x[i]);
+      keep(d[i]);
+      keep(res[i]);
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if (row + gridDim.x < a.rows) {
+      r_next = a.rstd[row + gridDim.x];
+      fetch(row + gridDim.x);
+    }
+    float dot = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      keep(gamma[i]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float n = x[i][e] * r;
+        dot += d[i][e] * gamma[i][e] * n;
+        dg[i][e] += d[i][e] * n;
+      }
+      __builtin_amdgcn_sched_barrier(0);   // eight columns at a time: no registers for all of them in fp32
+    }
+    const float mean = sum_over(dot) / (float)a.h;
+    const int col = (wave * 64 + lane_of()) * 8 * ES;
+    const auto out = __builtin_amdgcn_make_buffer_rsrc(static_cast<char *>(a.dx) + row * bytes, 0, (int)bytes, 0x00020000);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      E o[8];
+      keep(gamma[i]);
+      keep(x[i]);
+      keep(d[i]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        float v = r * (d[i][e] * gamma[i][e] - x[i][e] * r * mean);
+        if (with_dres) v += res[i][e];
+        o[e] = from_f32<E>(v);
+      }
+#pragma unroll
+      for (int k = 0; k < HALVES; ++k) {
+        u32x4 v;
+        __builtin_memcpy(&v, o + k * (16 / ES), 16);
+        __builtin_amdgcn_raw_buffer_store_b128(v, out, col + i * 1024 * 8 * ES + k * 16, 0, 0);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(STORES) : "memory");   // the next row's have landed
+  }
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int col = (i * 1024 + wave * 64 + lane_of()) * 8;
+    if (col < a.h) store8(a.partial + (int64_t)blockIdx.x * a.h + col, dg[i]);
+  }
+}
+template <typename E, int NV> constexpr int wide_ahead() { return 3 * NV * 16 * 64 * 8 * (int)sizeof(E) <= 156 * 1024 ? 3 : 2 * NV * 16 * 64 * 8 * (int)sizeof(E) <= 156 * 1024 ? 2 : 1; }
+template <typename E, int NV>
+int bwd_wide_launch(const NormBwdArgs &a, unsigned groups, hipStream_t st) {
+  constexpr int PRE = wide_ahead<E, NV>(), lds = PRE * NV * 16 * 64 * 8 * (int)sizeof(E);
+  static unsigned long long attr_done = 0;
+  int device;
+  if (!attr_is_set(attr_done, &device)) {
+    if (hipFuncSetAttribute((const void *)rmsnorm_bwd_wide_kernel<E, NV, PRE>, hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess) return MTNLG_HIP_ERROR;
+    attr_mark_set(attr_done, device);
+  }
+  rmsnorm_bwd_wide_kernel<E, NV, PRE><<<groups, 1024, lds, st>>>(a);
+  return check_launch();
 }
 
 // dgamma from the workgroups' sums: 32 columns to a workgroup, 8 lanes across them, 32 down; a fixed order
@@ -304,9 +437,7 @@ int bwd_launch(const NormBwdArgs &a, void *dgamma, int grad_f32, int accumulate,
   else if (nvec <= 256) RMS(1, 4);
   else if (nvec <= 512) RMS(4, 2);
   else if (nvec <= 1024) RMS(4, 4);
-  else if (nvec <= 2048) RMS(16, 2);
-  else if (nvec <= 3072) RMS(16, 3);
-  else RMS(16, 4);
+  else MTNLG_TRY((nvec <= 2048 ? bwd_wide_launch<E, 2>(a, groups, st) : nvec <= 3072 ? bwd_wide_launch<E, 3>(a, groups, st) : bwd_wide_launch<E, 4>(a, groups, st)));
 #undef RMS
   MTNLG_TRY(check_launch());
   const unsigned blocks = (a.h + 31) / 32;
