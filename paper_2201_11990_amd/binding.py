@@ -6,6 +6,7 @@ library is not built this module raises -- there is no fallback.
 """
 import ctypes
 import os
+import struct
 
 import torch
 
@@ -106,7 +107,6 @@ def lib():
                                       ctypes.c_uint32, ctypes.c_float)
         dp = ctypes.POINTER(LayerDesc)
         pp = ctypes.POINTER(_Ptrs12)
-        hp = ctypes.POINTER(Heads)
         sigs = {
             "mtnlg_version": (ctypes.c_int, []),
             "mtnlg_status_string": (ctypes.c_char_p, [ctypes.c_int]),
@@ -150,14 +150,12 @@ def lib():
             "mtnlg_rmsnorm_bwd_workspace": (sz, [i64, i64]),
             "mtnlg_rmsnorm_bwd": (ctypes.c_int, [ctypes.c_int, i64, i64, vp, vp, vp, vp, vp, vp, vp, ctypes.c_int, ctypes.c_int,
                                                  vp, sz, vp]),
-            "mtnlg_rotary_fwd": (ctypes.c_int, [ctypes.POINTER(RotaryDesc), hp, hp, hp, hp, vp, vp]),
-            "mtnlg_rotary_bwd": (ctypes.c_int, [ctypes.POINTER(RotaryDesc), hp, hp, hp, hp, vp, vp]),
+            "mtnlg_rotary_fwd": (ctypes.c_int, [vp, vp, vp, vp, vp, vp, vp]),
+            "mtnlg_rotary_bwd": (ctypes.c_int, [vp, vp, vp, vp, vp, vp, vp]),
             "mtnlg_packed_attention_fwd_workspace": (sz, [ctypes.POINTER(PackedDesc)]),
-            "mtnlg_packed_attention_fwd": (ctypes.c_int, [ctypes.POINTER(PackedDesc), ctypes.POINTER(PackedSequences), hp, hp, hp, hp,
-                                                          vp, vp, sz, vp]),
+            "mtnlg_packed_attention_fwd": (ctypes.c_int, [vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]),
             "mtnlg_packed_attention_bwd_workspace": (sz, [ctypes.POINTER(PackedDesc)]),
-            "mtnlg_packed_attention_bwd": (ctypes.c_int, [ctypes.POINTER(PackedDesc), ctypes.POINTER(PackedSequences), hp, hp, hp, hp,
-                                                          vp, hp, hp, hp, hp, vp, sz, vp]),
+            "mtnlg_packed_attention_bwd": (ctypes.c_int, [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]),
             "mtnlg_calibrate_mfma_operand_bytes": (sz, [ctypes.c_int]),
             "mtnlg_calibrate_mfma_flops": (i64, [ctypes.c_int, ctypes.c_int]),
             "mtnlg_calibrate_mfma": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, vp, vp, vp]),
@@ -467,72 +465,99 @@ def mtnlg_lm_head_step(desc, x, ln_g, ln_b, emb, targets, dloss, loss, dx, d_ln_
                                     _nbytes(workspace), _op_hook(reduce), None, _stream()), "mtnlg_lm_head_step")
 
 
-def _here(*tensors):
-    """The tensors (None aside) are on the current device, whose current stream the call goes to."""
+def _device_stream(*tensors):
+    """The current stream, of the current device, on which all the tensors (None aside) have to be."""
     device = torch.cuda.current_device()
     for t in tensors:
-        if t is not None and not (t.is_cuda and t.device.index == device):
+        if t is not None and t.get_device() != device:
             raise ValueError("tensors handed to the library must be on the current device")
+    return torch._C._cuda_getCurrentRawStream(device)
 
 
 def _like(t, dtype, shape, what):
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+    if t.dtype != dtype or t.shape != shape:
         raise ValueError(f"{what}: expected {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
 
 
-def _heads(t, kv_heads):
-    """A matrix of heads [tokens, heads, head_dim] or [tokens, kv_heads, heads of a group, head_dim], any strides but the last's."""
+def _dense(t):
+    """Address of a contiguous tensor (None -> NULL)."""
     if t is None:
         return None
-    if t.dim() not in (3, 4) or t.shape[-1] == 0 or (t.shape[-1] > 1 and t.stride(-1) != 1):
+    if not t.is_contiguous():
+        raise ValueError("tensors handed to the library must be contiguous device tensors")
+    return t.data_ptr()
+
+
+def _strides(t, kv_heads):
+    """Address and strides (token, group, head of the group) of a matrix of heads: [tokens, heads, head_dim] or [tokens, kv_heads, heads of a
+    group, head_dim], any strides but the last's."""
+    st, shape = t.stride(), t.shape
+    if len(st) not in (3, 4) or shape[-1] == 0 or (shape[-1] > 1 and st[-1] != 1):
         raise ValueError("heads: [tokens, heads, head_dim] or [tokens, kv_heads, group, head_dim] with dense rows")
-    if t.dim() == 4:
-        return Heads(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2))
-    return Heads(t.data_ptr(), t.stride(0), t.stride(1) * (t.shape[1] // kv_heads), t.stride(1))
+    if len(st) == 4:
+        return t.data_ptr(), st[0], st[1], st[2]
+    return t.data_ptr(), st[0], st[1] * (shape[1] // kv_heads), st[1]
 
 
-def _ref(h):
-    return None if h is None else ctypes.byref(h)
+def _heads(t, kv_heads):
+    return None if t is None else Heads(*_strides(t, kv_heads))
 
 
 def _counts(q, k):
     """heads, kv_heads, head_dim of a matrix of query heads beside one of key heads."""
-    heads = q.shape[1] if q.dim() == 3 else q.shape[1] * q.shape[2]
-    kv_heads = k.shape[1] if k is not None else q.shape[1]
-    if k is not None and (k.dim() != 3 or k.shape[2] != q.shape[-1] or k.dtype != q.dtype):
-        raise ValueError("keys and values: [tokens, kv_heads, head_dim] of the queries' type and head size")
-    if kv_heads == 0 or heads % kv_heads or (q.dim() == 4 and q.shape[1] != kv_heads):
+    if q.dim() not in (3, 4):
+        raise ValueError("heads: [tokens, heads, head_dim] or [tokens, kv_heads, group, head_dim]")
+    shape = q.shape
+    heads = shape[1] if len(shape) == 3 else shape[1] * shape[2]
+    kv_heads = shape[1]
+    if k is not None:
+        if k.dim() != 3 or k.shape[2] != shape[-1] or k.dtype != q.dtype:
+            raise ValueError("keys and values: [tokens, kv_heads, head_dim] of the queries' type and head size")
+        kv_heads = k.shape[1]
+    if kv_heads == 0 or heads % kv_heads or (len(shape) == 4 and shape[1] != kv_heads):
         raise ValueError("the number of query heads is a multiple of that of key heads")
-    return heads, kv_heads, q.shape[-1]
+    return heads, kv_heads, shape[-1]
+
+
+class _Structs:
+    """The structs of a call side by side in one buffer: one packing for all their fields, and an address for each."""
+
+    def __init__(self, layout, *fields):
+        self.bytes = bytearray(layout.pack(*fields))
+        self.at = ctypes.addressof(ctypes.c_char.from_buffer(self.bytes))
 
 
 def mtnlg_rmsnorm_fwd(x, gamma, eps, out, rstd, residual=None, xsum=None):
     """x, residual, xsum, out: [T, h] (contiguous); rstd: fp32 [T]."""
-    T, h = x.shape
-    _here(x, gamma, out, rstd, residual, xsum)
-    _like(out, x.dtype, (T, h), "out")
-    _like(gamma, x.dtype, (h,), "gamma")
+    T, h = shape = x.shape
+    dtype = x.dtype
+    stream = _device_stream(x, gamma, out, rstd, residual, xsum)
+    _like(out, dtype, shape, "out")
+    _like(gamma, dtype, (h,), "gamma")
     _like(rstd, torch.float32, (T,), "rstd")
-    for t, what in ((residual, "residual"), (xsum, "xsum")):
-        if t is not None:
-            _like(t, x.dtype, (T, h), what)
-    _check(lib().mtnlg_rmsnorm_fwd(_dtype_code(x), T, h, _p(x), _p(residual), _p(gamma), eps, _p(xsum), _p(out), _p(rstd), _stream()),
-           "mtnlg_rmsnorm_fwd")
+    if residual is not None:
+        _like(residual, dtype, shape, "residual")
+    if xsum is not None:
+        _like(xsum, dtype, shape, "xsum")
+    _check(lib().mtnlg_rmsnorm_fwd(_dtype_code(x), T, h, _dense(x), _dense(residual), _dense(gamma), eps, _dense(xsum), _dense(out),
+                                   _dense(rstd), stream), "mtnlg_rmsnorm_fwd")
 
 
 def mtnlg_rmsnorm_fwd_e4m3(x, gamma, eps, out, scale, rstd, columns=0, residual=None, xsum=None):
     """out: e4m3 [T, h]; scale: fp32 [T, number of groups of `columns` columns] (columns 0: one to a row)."""
-    T, h = x.shape
-    _here(x, gamma, out, scale, rstd, residual, xsum)
-    _like(out, torch.float8_e4m3fn, (T, h), "out")
-    _like(gamma, x.dtype, (h,), "gamma")
+    T, h = shape = x.shape
+    dtype = x.dtype
+    stream = _device_stream(x, gamma, out, scale, rstd, residual, xsum)
+    _like(out, torch.float8_e4m3fn, shape, "out")
+    _like(gamma, dtype, (h,), "gamma")
     _like(scale, torch.float32, (T, -(-h // columns) if columns > 0 else 1), "scale")
     _like(rstd, torch.float32, (T,), "rstd")
-    for t, what in ((residual, "residual"), (xsum, "xsum")):
-        if t is not None:
-            _like(t, x.dtype, (T, h), what)
-    _check(lib().mtnlg_rmsnorm_fwd_e4m3(_dtype_code(x), T, h, _p(x), _p(residual), _p(gamma), eps, columns, _p(xsum), _p(out), _p(scale),
-                                        _p(rstd), _stream()), "mtnlg_rmsnorm_fwd_e4m3")
+    if residual is not None:
+        _like(residual, dtype, shape, "residual")
+    if xsum is not None:
+        _like(xsum, dtype, shape, "xsum")
+    _check(lib().mtnlg_rmsnorm_fwd_e4m3(_dtype_code(x), T, h, _dense(x), _dense(residual), _dense(gamma), eps, columns, _dense(xsum),
+                                        _dense(out), _dense(scale), _dense(rstd), stream), "mtnlg_rmsnorm_fwd_e4m3")
 
 
 def mtnlg_rmsnorm_bwd_workspace(T, h):
@@ -541,16 +566,19 @@ def mtnlg_rmsnorm_bwd_workspace(T, h):
 
 def mtnlg_rmsnorm_bwd(x, gamma, rstd, dout, dx, dgamma, workspace, dres=None, accumulate=False):
     """x: what was normalised; dgamma: [h], fp32 or x's type."""
-    T, h = x.shape
-    _here(x, gamma, rstd, dout, dx, dgamma, workspace, dres)
-    for t, what in ((dout, "dout"), (dx, "dx"), (dres, "dres")):
-        if t is not None:
-            _like(t, x.dtype, (T, h), what)
-    _like(gamma, x.dtype, (h,), "gamma")
+    T, h = shape = x.shape
+    dtype = x.dtype
+    stream = _device_stream(x, gamma, rstd, dout, dx, dgamma, workspace, dres)
+    _like(dout, dtype, shape, "dout")
+    _like(dx, dtype, shape, "dx")
+    if dres is not None:
+        _like(dres, dtype, shape, "dres")
+    _like(gamma, dtype, (h,), "gamma")
     _like(rstd, torch.float32, (T,), "rstd")
-    _like(dgamma, torch.float32 if dgamma.dtype == torch.float32 else x.dtype, (h,), "dgamma")
-    _check(lib().mtnlg_rmsnorm_bwd(_dtype_code(x), T, h, _p(x), _p(gamma), _p(rstd), _p(dout), _p(dres), _p(dx), _p(dgamma),
-                                   int(dgamma.dtype == torch.float32), int(accumulate), _p(workspace), _nbytes(workspace), _stream()),
+    grad_f32 = dgamma.dtype == torch.float32
+    _like(dgamma, torch.float32 if grad_f32 else dtype, (h,), "dgamma")
+    _check(lib().mtnlg_rmsnorm_bwd(_dtype_code(x), T, h, _dense(x), _dense(gamma), _dense(rstd), _dense(dout), _dense(dres), _dense(dx),
+                                   _dense(dgamma), int(grad_f32), int(accumulate), _dense(workspace), _nbytes(workspace), stream),
            "mtnlg_rmsnorm_bwd")
 
 
@@ -560,24 +588,30 @@ def rotary_desc(rotary_dim, layout=ROTARY_HALF, base=10000.0, scaling=ROTARY_UNS
     return RotaryDesc(0, 0, 0, 0, rotary_dim, layout, scaling, original_positions, 0, base, factor, slow, fast, amplitude)
 
 
+# a RotaryDesc, then four Heads
+_ROTARY = struct.Struct("8i q5d 16q")
+
+
 def _rotary(name, desc, q, k, q_out, k_out, positions):
-    if q.dim() not in (3, 4):
-        raise ValueError("heads: [tokens, heads, head_dim] or [tokens, kv_heads, group, head_dim]")
-    heads, kv_heads, d = _counts(q, k)
-    _here(q, k, q_out, k_out, positions)
+    heads, n, d = _counts(q, k)
+    stream = _device_stream(q, k, q_out, k_out, positions)
     if (k is None) != (k_out is None):
         raise ValueError("keys go with an output of theirs")
     _like(q_out, q.dtype, q.shape, "the output of the queries")
+    tokens = q.shape[0]
+    none = (0, 0, 0, 0)
     if k is not None:
-        if k.shape[0] != q.shape[0]:
+        if k.shape[0] != tokens:
             raise ValueError("queries and keys of the same tokens")
         _like(k_out, k.dtype, k.shape, "the output of the keys")
     if positions is not None:
-        _like(positions, torch.int32, (q.shape[0],), "positions")
-    full = RotaryDesc(_dtype_code(q), heads, kv_heads, d, desc.rotary_dim, desc.layout, desc.scaling, desc.original_positions,
-                      q.shape[0], desc.base, desc.factor, desc.slow, desc.fast, desc.amplitude)
-    _check(getattr(lib(), name)(ctypes.byref(full), _ref(_heads(q, kv_heads)), _ref(_heads(k, kv_heads)), _ref(_heads(q_out, kv_heads)),
-                                _ref(_heads(k_out, kv_heads)), _p(positions), _stream()), name)
+        _like(positions, torch.int32, (tokens,), "positions")
+    s = _Structs(_ROTARY, _dtype_code(q), heads, n, d, desc.rotary_dim, desc.layout, desc.scaling, desc.original_positions, tokens,
+                 desc.base, desc.factor, desc.slow, desc.fast, desc.amplitude, *_strides(q, n), *(_strides(k, n) if k is not None else none),
+                 *_strides(q_out, n), *(_strides(k_out, n) if k is not None else none))
+    first = s.at + ctypes.sizeof(RotaryDesc)
+    _check(getattr(lib(), name)(s.at, first, first + 32 if k is not None else None, first + 64, first + 96 if k is not None else None,
+                                _dense(positions), stream), name)
 
 
 def mtnlg_rotary_fwd(desc, q, k, q_out, k_out, positions=None):
@@ -603,43 +637,53 @@ def mtnlg_packed_attention_bwd_workspace(desc):
     return lib().mtnlg_packed_attention_bwd_workspace(ctypes.byref(desc))
 
 
+# a PackedDesc, a PackedSequences, then Heads
+_PACKED = "7i4x2qf4x 4P"
+_PACKED_FWD, _PACKED_BWD = struct.Struct(_PACKED + "16q"), struct.Struct(_PACKED + "32q")
+_PACKED_HEADS = ctypes.sizeof(PackedDesc) + ctypes.sizeof(PackedSequences)
+
+
 def _packed(q, k, v, a, lse, q_offsets, k_offsets, max_q, max_k, scale, q_lengths, k_lengths):
-    if q.dim() not in (3, 4) or k is None:
-        raise ValueError("heads: [tokens, heads, head_dim] or [tokens, kv_heads, group, head_dim]")
-    desc = packed_desc(q, k, q_offsets.shape[0] - 1, max_q, max_k, scale)
-    _here(q, k, v, a, lse, q_offsets, k_offsets, q_lengths, k_lengths)
+    """Fields of the descriptor, the sequences and the heads of q, k, v, a; the number of key heads."""
+    heads, n, d = _counts(q, k)
+    sequences = q_offsets.shape[0] - 1
     _like(v, k.dtype, k.shape, "v")
     _like(a, q.dtype, q.shape, "a")
-    _like(lse, torch.float32, (desc.heads, q.shape[0]), "lse")
-    for t, n, what in ((q_offsets, desc.sequences + 1, "q_offsets"), (k_offsets, desc.sequences + 1, "k_offsets"),
-                       (q_lengths, desc.sequences, "q_lengths"), (k_lengths, desc.sequences, "k_lengths")):
-        if t is not None:
-            _like(t, torch.int32, (n,), what)
-    return desc, PackedSequences(_p(q_offsets), _p(k_offsets), _p(q_lengths), _p(k_lengths))
+    _like(lse, torch.float32, (heads, q.shape[0]), "lse")
+    _like(q_offsets, torch.int32, (sequences + 1,), "q_offsets")
+    _like(k_offsets, torch.int32, (sequences + 1,), "k_offsets")
+    if q_lengths is not None:
+        _like(q_lengths, torch.int32, (sequences,), "q_lengths")
+    if k_lengths is not None:
+        _like(k_lengths, torch.int32, (sequences,), "k_lengths")
+    return (_dtype_code(q), heads, n, d, sequences, max_q, max_k, q.shape[0], k.shape[0], scale, _dense(q_offsets), _dense(k_offsets),
+            _dense(q_lengths) or 0, _dense(k_lengths) or 0, *_strides(q, n), *_strides(k, n), *_strides(v, n), *_strides(a, n)), n
 
 
 def mtnlg_packed_attention_fwd(q, k, v, a, lse, q_offsets, k_offsets, max_q, max_k, scale=0.0, q_lengths=None, k_lengths=None,
                                workspace=None):
     """q, a: [tokens, heads, head_dim] or [tokens, kv_heads, group, head_dim]; k, v: [tokens, kv_heads, head_dim]; lse: fp32 [heads, tokens];
     offsets: int32 [sequences + 1] on the device, lengths (nullable) [sequences]; max_q, max_k: no sequence is longer."""
-    desc, where = _packed(q, k, v, a, lse, q_offsets, k_offsets, max_q, max_k, scale, q_lengths, k_lengths)
-    _here(workspace)
-    n = desc.kv_heads
-    _check(lib().mtnlg_packed_attention_fwd(ctypes.byref(desc), ctypes.byref(where), _ref(_heads(q, n)), _ref(_heads(k, n)), _ref(_heads(v, n)),
-                                            _ref(_heads(a, n)), _p(lse), _p(workspace), _nbytes(workspace) if workspace is not None else 0,
-                                            _stream()), "mtnlg_packed_attention_fwd")
+    stream = _device_stream(q, k, v, a, lse, q_offsets, k_offsets, q_lengths, k_lengths, workspace)
+    fields, _ = _packed(q, k, v, a, lse, q_offsets, k_offsets, max_q, max_k, scale, q_lengths, k_lengths)
+    s = _Structs(_PACKED_FWD, *fields)
+    h = s.at + _PACKED_HEADS
+    _check(lib().mtnlg_packed_attention_fwd(s.at, s.at + ctypes.sizeof(PackedDesc), h, h + 32, h + 64, h + 96, _dense(lse), _dense(workspace),
+                                            _nbytes(workspace) if workspace is not None else 0, stream), "mtnlg_packed_attention_fwd")
 
 
 def mtnlg_packed_attention_bwd(q, k, v, a, lse, da, dq, dk, dv, q_offsets, k_offsets, max_q, max_k, workspace, scale=0.0, q_lengths=None,
                                k_lengths=None):
-    desc, where = _packed(q, k, v, a, lse, q_offsets, k_offsets, max_q, max_k, scale, q_lengths, k_lengths)
-    _here(da, dq, dk, dv, workspace)
-    for t, like, what in ((da, q, "da"), (dq, q, "dq"), (dk, k, "dk"), (dv, k, "dv")):
-        _like(t, like.dtype, like.shape, what)
-    n = desc.kv_heads
-    _check(lib().mtnlg_packed_attention_bwd(ctypes.byref(desc), ctypes.byref(where), _ref(_heads(q, n)), _ref(_heads(k, n)), _ref(_heads(v, n)),
-                                            _ref(_heads(a, n)), _p(lse), _ref(_heads(da, n)), _ref(_heads(dq, n)), _ref(_heads(dk, n)),
-                                            _ref(_heads(dv, n)), _p(workspace), _nbytes(workspace), _stream()), "mtnlg_packed_attention_bwd")
+    stream = _device_stream(q, k, v, a, lse, da, dq, dk, dv, q_offsets, k_offsets, q_lengths, k_lengths, workspace)
+    fields, n = _packed(q, k, v, a, lse, q_offsets, k_offsets, max_q, max_k, scale, q_lengths, k_lengths)
+    _like(da, q.dtype, q.shape, "da")
+    _like(dq, q.dtype, q.shape, "dq")
+    _like(dk, k.dtype, k.shape, "dk")
+    _like(dv, k.dtype, k.shape, "dv")
+    s = _Structs(_PACKED_BWD, *fields, *_strides(da, n), *_strides(dq, n), *_strides(dk, n), *_strides(dv, n))
+    h = s.at + _PACKED_HEADS
+    _check(lib().mtnlg_packed_attention_bwd(s.at, s.at + ctypes.sizeof(PackedDesc), h, h + 32, h + 64, h + 96, _dense(lse), h + 128, h + 160,
+                                            h + 192, h + 224, _dense(workspace), _nbytes(workspace), stream), "mtnlg_packed_attention_bwd")
 
 
 def mtnlg_grad_sqnorm_workspace():

@@ -33,11 +33,13 @@ struct PackedFwdArgs {
 
 struct PackedBwdArgs {
   Sequences where;
-  int kv_heads, group, d, splits;   // splits: parts of a group
+  int kv_heads, group, d, splits;   // splits: parts of a dk / dv workgroup's tiles
   float scale;
   Heads q, k, v, a, da, dq, dk, dv;
   const float *lse;
   float *D, *part;
+  int chunk, chunks;   // packed_plain.hip: keys that a dq workgroup takes at most (0: all), how many of those there are at most
+  float *dq_part;      // of chunks
 };
 
 // Head sizes up to which bf16 has kernels of its own (packed_fwd.hip, packed_bwd.hip); others and fp32: packed_plain.hip.

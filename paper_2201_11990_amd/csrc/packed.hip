@@ -42,7 +42,26 @@ __global__ __launch_bounds__(256) void packed_join_kernel(PackedFwdArgs w) {
   if (lane == 0) w.lse[(int64_t)head * w.where.q_tokens + s.q0 + tok] = nc ? plus_log(product_of(most, w.scale), total) : -INFINITY;
 }
 
-// The parts of a group added up: a wave to a key, four columns of dv (lower half of the lanes' columns) and dk to a lane in turn.
+// dq from its chunks of keys: a wave to a row, four columns to a lane.
+template <typename E>
+__global__ __launch_bounds__(256) void packed_dq_join_kernel(PackedBwdArgs w) {
+  const int lane = threadIdx.x & 63, r = w.group, d = w.d, j = blockIdx.x % w.kv_heads;
+  Span s;
+  unsigned at;
+  if (!find_piece(w.where, blockIdx.x / w.kv_heads, [&](const Span &s) { return (unsigned)((s.lq * r + 3) / 4); }, s, at)) return;
+  const int row = at * 4 + (threadIdx.x >> 6);
+  if (row >= s.lq * r || lane * 4 >= d) return;
+  const int tok = row / r, g = row - tok * r, limit = min(tok + s.lk - s.lq, s.lk - 1);
+  const int nc = min(limit < 0 ? 0 : limit / w.chunk + 1, w.chunks);
+  const int64_t all = (int64_t)w.where.q_tokens * w.kv_heads * r;
+  const float *from = w.dq_part + ((int64_t)(s.q0 + tok) * ((int64_t)w.kv_heads * r) + j * r + g) * d + lane * 4;
+  f32x4 sum = {};
+#pragma unroll 4
+  for (int i = 0; i < nc; ++i) sum += *reinterpret_cast<const f32x4 *>(from + i * all * d);
+  put4(row_at<E>(w.dq, s.q0 + tok, j, g) + lane * 4, sum * w.scale);
+}
+
+// The parts of dk and dv added up: a wave to a key, four columns of dv (lower half of the lanes' columns) and dk to a lane in turn.
 template <typename E>
 __global__ __launch_bounds__(256) void packed_dkv_join_kernel(PackedBwdArgs w) {
   const int lane = threadIdx.x & 63, d = w.d, j = blockIdx.x % w.kv_heads;
@@ -63,21 +82,38 @@ __global__ __launch_bounds__(256) void packed_dkv_join_kernel(PackedBwdArgs w) {
 }
 
 // How the keys are cut where the rows alone leave most of the chip idle.
-#ifndef CUT_INTO
-#define CUT_INTO 1024
-#endif
-#ifndef CUT_BELOW
-#define CUT_BELOW 512
-#endif
-#ifndef CUT_LEAST
-#define CUT_LEAST 256
-#endif
 struct FwdPlan {
   int owned;
   int64_t pieces;   // workgroups of a head of keys at most, without cuts
   int chunk, chunks;
   size_t part_bytes, bytes;
 };
+// Estimated microseconds with and without: a workgroup takes about 0.9 us a tile of 64 keys where two share a unit (fp32 by its matrix instructions), 3.5 us to start, and
+// a cut call 8 us and the way of its parts through memory (at 4 TB/s) to join them.  Cut where that is
+// half as much again faster, into about 1024 pieces.  Measured: 32 single tokens, 64 to 15872 keys, 32 heads of 128 on 8: 280 us whole, 96 cut (104 into 512 pieces, 112 into
+// 2048); 973 tokens behind up to 4608 keys, 62 us whole, 89 and 101 in chunks of 2304 and 1024.
+constexpr int CUT_LEAST = 256, SLOTS = 512;   // keys of a chunk at least; workgroups at once
+struct Cut {
+  int chunk, chunks;
+};
+Cut cut_keys(const PackedShape &S, int64_t pieces, double tile, int least, int into) {   // tile: us of 64 keys
+  const double wide = (double)(pieces * S.kv_heads), mean = (double)S.where.k_tokens / S.where.count;
+  if (S.max_k < 2 * least || wide >= 2 * SLOTS) return Cut{0, 1};
+  const double work = wide * mean / 64 / SLOTS;   // tiles of a slot where all come out even
+  const int want = (int)fmax(least, fmax(S.max_k / 64.0, wide * mean / into));   // (64: a lane of the joining wave to each)
+  const int chunk = (want + 63) / 64 * 64;
+  const double each = fmax(1.0, mean / chunk);   // chunks of a sequence
+  const double whole = tile * fmax(S.max_k / 64.0, work);
+  const double cut = tile * fmax(chunk / 64.0, work) + 3.5 * wide * each / SLOTS + 8.0 + (double)S.where.q_tokens * S.heads * each * S.d * 8.0 / 4.0e6;
+  if (chunk >= S.max_k || 1.5 * cut >= whole) return Cut{0, 1};
+  return Cut{chunk, (S.max_k + chunk - 1) / chunk};
+}
+// all pieces with their chunks: all keys in chunks and the last ones of each sequence, for every block that a sequence can have
+int64_t cut_pieces(const PackedShape &S, const Cut &c, int64_t pieces, int owned) {
+  if (c.chunks == 1) return pieces;
+  const int64_t blocks_of = ((int64_t)S.max_q * S.group + owned - 1) / owned, by_keys = blocks_of * (S.where.k_tokens / c.chunk + S.where.count);
+  return pieces * c.chunks < by_keys ? pieces * c.chunks : by_keys;
+}
 FwdPlan fwd_plan(const PackedShape &S) {
   FwdPlan p{};
   const int64_t rows = (int64_t)S.where.q_tokens * S.group, most = (int64_t)S.max_q * S.group;
@@ -87,19 +123,13 @@ FwdPlan fwd_plan(const PackedShape &S) {
     p.owned = 64;
     p.pieces = pieces_bound(rows, most, S.where.count, p.owned);
   }
-  p.chunks = 1;
-  const int64_t wide = p.pieces * S.kv_heads;
-  if (wide < CUT_BELOW && S.max_k > 2 * CUT_LEAST) {
-    int64_t chunk = wide * (S.where.k_tokens / S.where.count) / CUT_INTO;
-    chunk = chunk < CUT_LEAST ? CUT_LEAST : chunk;
-    if (chunk * 64 < S.max_k) chunk = (S.max_k + 63) / 64;   // a lane of the joining wave to each
-    chunk = (chunk + 63) / 64 * 64;
-    p.chunk = (int)chunk;
-    p.chunks = (int)((S.max_k + chunk - 1) / chunk);
+  const Cut c = cut_keys(S, p.pieces, S.dtype == MTNLG_F32 ? 0.11 * S.d : 0.9, CUT_LEAST, 1024);
+  p.chunk = c.chunk;
+  p.chunks = c.chunks;
+  if (p.chunks > 1) {
     const size_t all = (size_t)S.where.q_tokens * S.heads;
     p.part_bytes = align_up(p.chunks * all * S.d * sizeof(float), 256);
     p.bytes = p.part_bytes + align_up(p.chunks * all * 2 * sizeof(float), 256);
-    if (p.chunks == 1) p.chunk = 0, p.bytes = 0;
   }
   return p;
 }
@@ -109,9 +139,10 @@ bool unaligned(const mtnlg_packed_sequences *w) {
 }
 
 struct BwdPlan {
-  int owned, key_owned, splits;   // rows of a dq workgroup, keys of one of dk / dv; parts of a group
+  int owned, key_owned, splits;   // rows of a dq workgroup, keys of one of dk / dv; parts of its tiles
+  Cut cut;                        // of the keys of dq (packed_plain.hip)
   int64_t pieces, key_pieces;
-  size_t d_bytes, bytes;
+  size_t d_bytes, part_bytes, bytes;
 };
 BwdPlan bwd_plan(const PackedShape &S) {
   BwdPlan p{};
@@ -128,10 +159,18 @@ BwdPlan bwd_plan(const PackedShape &S) {
     p.key_owned = packed_dkv_least(S.d);
     p.key_pieces = pieces_bound(S.where.k_tokens, S.max_k, S.where.count, p.key_owned);
   }
-  const int64_t wide = p.key_pieces * S.kv_heads, splits = (512 + wide - 1) / wide;
-  p.splits = (int)(splits < S.group ? splits : S.group);
+  // Where the keys leave units idle, a workgroup's tiles of queries (of all heads of the group) are dealt out: about 512 workgroups, of 8 tiles at least, which the
+  // joining launch and the parts' way through memory cost.
+  const int64_t wide = p.key_pieces * S.kv_heads, tiles = (int64_t)S.group * ((S.max_q + 31) / 32);
+  int64_t splits = wide >= 512 ? 1 : (512 + wide - 1) / wide;
+  if (splits > tiles / 8) splits = tiles / 8;
+  p.splits = (int)(splits < 1 ? 1 : splits > 64 ? 64 : splits);
   p.d_bytes = align_up((size_t)S.where.q_tokens * S.heads * sizeof(float), 256);
-  p.bytes = p.d_bytes + (p.splits > 1 ? (size_t)p.splits * S.where.k_tokens * S.kv_heads * 2 * S.d * sizeof(float) : 0);
+  p.part_bytes = p.splits > 1 ? align_up((size_t)p.splits * S.where.k_tokens * S.kv_heads * 2 * S.d * sizeof(float), 256) : 0;
+  // fp32: a tile of dq is long, and few rows are few workgroups (1536 tokens in 4 documents, 8 heads of 96 on 4: 114 us whole, 45 so)
+  p.cut = S.dtype == MTNLG_F32 ? cut_keys(S, p.pieces, 0.16 * S.d, 64, 512) : Cut{0, 1};
+  p.pieces = cut_pieces(S, p.cut, p.pieces, p.owned);
+  p.bytes = p.d_bytes + p.part_bytes + (p.cut.chunks > 1 ? (size_t)p.cut.chunks * S.where.q_tokens * S.heads * S.d * sizeof(float) : 0);
   return p;
 }
 
@@ -198,11 +237,7 @@ int mtnlg_packed_attention_fwd(const mtnlg_packed_desc *desc, const mtnlg_packed
   w.lse = lse;
   w.part = (float *)workspace;
   w.stat = (float *)((char *)workspace + plan.part_bytes);
-  int64_t pieces = plan.pieces;
-  if (plan.chunks > 1) {   // all keys in chunks and the last ones of each sequence, for every block that a sequence can have
-    const int64_t blocks_of = ((int64_t)S.max_q * S.group + plan.owned - 1) / plan.owned, by_keys = blocks_of * (S.where.k_tokens / plan.chunk + S.where.count);
-    pieces = pieces * plan.chunks < by_keys ? pieces * plan.chunks : by_keys;
-  }
+  const int64_t pieces = cut_pieces(S, Cut{plan.chunk, plan.chunks}, plan.pieces, plan.owned);
   const int64_t blocks = pieces * S.kv_heads;
   if (blocks > 0x7FFFFFFF) return MTNLG_UNSUPPORTED_SHAPE;
   const hipStream_t st = (hipStream_t)stream;
@@ -257,10 +292,18 @@ int mtnlg_packed_attention_bwd(const mtnlg_packed_desc *desc, const mtnlg_packed
   w.lse = lse;
   w.D = (float *)workspace;
   w.part = (float *)((char *)workspace + plan.d_bytes);
+  w.chunk = plan.cut.chunk;
+  w.chunks = plan.cut.chunks;
+  w.dq_part = (float *)((char *)workspace + plan.d_bytes + plan.part_bytes);
   const hipStream_t st = (hipStream_t)stream;
   LaunchScope scope(MTNLG_K_ATTN_BWD, st);
   MTNLG_TRY(packed_tuned(S.dtype, S.d) ? packed_bwd_tuned(w, plan.owned, plan.pieces, plan.key_owned, plan.key_pieces, st)
                                        : packed_bwd_plain(S.dtype, w, plan.pieces, plan.key_pieces, st));
+  if (plan.cut.chunks > 1) {
+    const unsigned joins = (unsigned)(pieces_bound((int64_t)S.where.q_tokens * S.group, (int64_t)S.max_q * S.group, S.where.count, 4) * S.kv_heads);
+    packed_dq_join_kernel<float><<<joins, 256, 0, st>>>(w);   // (bf16 is not cut)
+    MTNLG_TRY(check_launch());
+  }
   if (plan.splits == 1) return MTNLG_OK;
   const unsigned joins = (unsigned)(pieces_bound(S.where.k_tokens, S.max_k, S.where.count, 16) * S.kv_heads);
   if (S.dtype == MTNLG_F32) packed_dkv_join_kernel<float><<<joins, 256, 0, st>>>(w);

@@ -298,11 +298,12 @@ __global__ __launch_bounds__(DKV_THREADS) void packed_dkv_kernel(PackedBwdArgs w
   unsigned at;
   if (!find_piece(w.where, blockIdx.x / w.kv_heads, [&](const Span &s) { return (unsigned)((s.lk + OWNED - 1) / OWNED * w.splits); }, s, at)) return;
   const int split = at % w.splits, block0 = (int)(at / w.splits) * OWNED, shift = s.lk - s.lq;
-  const int each = (r + w.splits - 1) / w.splits, g0 = split * each, g1 = min(r, g0 + each);
   const int part = L::PARTS == 2 ? wave >> 1 & 1 : 0, role = wave >> 2;
   const int own0 = block0 + (wave & (L::GROUPS - 1)) * 32, mine = own0 + (lane & 31), key = min(mine, s.lk - 1);
   const int first = max(0, block0 - shift) / ROWS * ROWS, tiles = s.lq > first ? (s.lq - first + ROWS - 1) / ROWS : 0;   // of a head: from the first query that sees the block on
-  const int n = max(0, g1 - g0) * tiles;
+  // The workgroup's part of the tiles of all heads of the group, one head after the other: n from tile t0 of head g0 on.
+  const int n0 = (int)((int64_t)r * tiles * split / w.splits), n = (int)((int64_t)r * tiles * (split + 1) / w.splits) - n0;
+  const int g0 = tiles ? n0 / tiles : 0, t0 = n0 - g0 * tiles;
   const float f = w.scale * kLog2e;
   typename P::Lane ln(lane);
   const uint32_t smem_addr = lds_address(smem);
@@ -317,12 +318,10 @@ __global__ __launch_bounds__(DKV_THREADS) void packed_dkv_kernel(PackedBwdArgs w
   uint32_t dma_off[IPW];
 #pragma unroll
   for (int i = 0; i < IPW; ++i) dma_off[i] = T::dma_offset(pitch, instruction(i) / T::NI, lane, instruction(i) % T::NI, d);
-  auto rows_at = [&](int g) { return RowWalk(row_at<bf16>(mat, s.q0 + first, j, g), s.lq - first, pitch, ROWS); };
-  auto stats_at = [&](int g) {
-    return RowWalk((wave & 1 ? w.D : w.lse) + ((int64_t)(j * r + g) * w.where.q_tokens + s.q0 + first), s.lq - first, 4, ROWS);
-  };
-  RowWalk stream = rows_at(g0), stats = stats_at(g0);
-  int to_come = tiles, g_in = g0;   // tiles of the head g_in that have not been fetched
+  auto rows_at = [&](int g, int row) { return RowWalk(row_at<bf16>(mat, s.q0 + row, j, g), s.lq - row, pitch, ROWS); };
+  auto stats_at = [&](int g, int row) { return RowWalk((wave & 1 ? w.D : w.lse) + ((int64_t)(j * r + g) * w.where.q_tokens + s.q0 + row), s.lq - row, 4, ROWS); };
+  RowWalk stream = rows_at(g0, first + t0 * ROWS), stats = stats_at(g0, first + t0 * ROWS);
+  int to_come = tiles - t0, g_in = g0;   // tiles of the head g_in that have not been fetched
   auto issue_one = [&](auto tag, int st, int i) {   // i == IPW: the statistics (with tiles of 32 rows those of the next tile as well, unused)
     constexpr int TAG = decltype(tag)::value;
     const uint32_t stage = smem_addr + st * STAGE;
@@ -332,10 +331,10 @@ __global__ __launch_bounds__(DKV_THREADS) void packed_dkv_kernel(PackedBwdArgs w
   auto advance = [&] {
     stream.advance<ROWS>();
     stats.advance<ROWS>();
-    if (--to_come == 0 && g_in + 1 < g1) {   // the next head of the group
+    if (--to_come == 0 && g_in + 1 < r) {   // the next head of the group
       to_come = tiles;
-      stream = rows_at(++g_in);
-      stats = stats_at(g_in);
+      stream = rows_at(++g_in, first);
+      stats = stats_at(g_in, first);
     }
   };
   auto issue_tile = [&](int st) {
@@ -403,7 +402,7 @@ __global__ __launch_bounds__(DKV_THREADS) void packed_dkv_kernel(PackedBwdArgs w
 #pragma unroll
     for (int i = 0; i < PF; ++i) load(i);
     __builtin_amdgcn_sched_barrier(0);
-    int row = first + 32 * part, left = tiles;   // the tile's first query (of this part), tiles of the head from it on
+    int row = first + t0 * ROWS + 32 * part, left = tiles - t0;   // the tile's first query (of this part), tiles of the head from it on
     int row_before = row;                        // ... of the tile before
     // element e: query row + 8 (e / 4) + 4 h + e % 4; not seen: before the own key, or past the end
     auto hide = [&](int row, f32x16 &v) {
@@ -554,9 +553,10 @@ __global__ __launch_bounds__(DKV_THREADS) void packed_dkv_kernel(PackedBwdArgs w
       for (int e = 0; e < 8; ++e) sum[kk][e] = 0.0f;
     const bf16 *kr = row_at<bf16>(w.k, s.k0 + key, j, 0), *vr = row_at<bf16>(w.v, s.k0 + key, j, 0);
 #pragma unroll 1
-    for (int g = g0; g < g1; ++g) {
+    for (int it = n0; it < n0 + n; ++it) {
+      const int g = it / tiles, q0 = first + (it - g * tiles) * ROWS;
 #pragma unroll 1
-      for (int q = max(0, own0 - shift); q < s.lq; ++q) {
+      for (int q = q0; q < min(q0 + ROWS, s.lq); ++q) {
         const bf16 *qr = row_at<bf16>(w.q, s.q0 + q, j, g), *dr = row_at<bf16>(w.da, s.q0 + q, j, g);
         float sk = 0.0f, dpk = 0.0f;
 #pragma unroll

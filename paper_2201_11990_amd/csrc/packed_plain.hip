@@ -181,18 +181,25 @@ __global__ __launch_bounds__(256, (dq_per_unit<E, D>())) void plain_dq_kernel(Pa
   const int j = blockIdx.x % w.kv_heads;
   Span s;
   unsigned at;
-  if (!find_piece(w.where, blockIdx.x / w.kv_heads, [&](const Span &s) { return (unsigned)((s.lq * r + OWNED - 1) / OWNED); }, s, at)) return;
-  const int count = (s.lq * r + OWNED - 1) / OWNED, shift = s.lk - s.lq, block = count - 1 - at;   // falling work
+  const bool chunked = w.chunk > 0;
+  auto chunks_of = [&](const Span &s) { return chunked ? min((max(s.lk, 1) + w.chunk - 1) / w.chunk, w.chunks) : 1; };
+  if (!find_piece(w.where, blockIdx.x / w.kv_heads, [&](const Span &s) { return (unsigned)((s.lq * r + OWNED - 1) / OWNED * chunks_of(s)); }, s, at)) return;
+  const int nc = chunks_of(s), count = (s.lq * r + OWNED - 1) / OWNED, shift = s.lk - s.lq;
+  const int chunk = at % nc, block = count - 1 - at / nc;   // falling work
   const int rows = s.lq * r, block0 = block * OWNED, last_row = min(block0 + OWNED, rows) - 1;
-  const int end = max(0, min(s.lk, last_row / r + shift + 1)), ntiles = (end + TR - 1) / TR;
+  const int begin = chunk * w.chunk;
+  int end = min(s.lk, last_row / r + shift + 1);   // keys that the block sees
+  if (chunked && chunk + 1 < nc) end = min(end, begin + w.chunk);
+  if (chunked && end <= begin && chunk > 0) return;
+  const int ntiles = end > begin ? (end - begin + TR - 1) / TR : 0;
 
   const int own0 = block0 + wave * 32, mine = own0 + (lane & 31), row = min(mine, rows - 1);
   const int tok = row / r, g = row - tok * r, head = j * r + g;
-  const int limit = min(tok + shift, s.lk - 1);
+  const int limit = min(tok + shift, end - 1);   // the last key here that the row sees
   const int least = __builtin_amdgcn_readfirstlane(limit), most = own0 < rows ? __builtin_amdgcn_readlane(limit, 31) : -1;
 
-  const RowStream ks{reinterpret_cast<const char *>(row_at<E>(w.k, s.k0, j, 0)), end, (uint32_t)(w.k.token * sizeof(E))};
-  const RowStream vs{reinterpret_cast<const char *>(row_at<E>(w.v, s.k0, j, 0)), end, (uint32_t)(w.v.token * sizeof(E))};
+  const RowStream ks{reinterpret_cast<const char *>(row_at<E>(w.k, s.k0 + begin, j, 0)), end - begin, (uint32_t)(w.k.token * sizeof(E))};
+  const RowStream vs{reinterpret_cast<const char *>(row_at<E>(w.v, s.k0 + begin, j, 0)), end - begin, (uint32_t)(w.v.token * sizeof(E))};
   constexpr int IPW = TR / 32 * P::NI;
   const int half = wave >> 1, band = (wave & 1) * (TR / 32);
   const uint32_t pitch = half ? vs.pitch : ks.pitch;
@@ -220,7 +227,7 @@ __global__ __launch_bounds__(256, (dq_per_unit<E, D>())) void plain_dq_kernel(Pa
   dsum += __shfl_xor(dsum, 32, 64);
   constexpr bool EXACT = sizeof(E) == 4;
   const int64_t stat = (int64_t)head * w.where.q_tokens + s.q0 + tok;
-  if (mine < rows && h == 0) w.D[stat] = dsum;
+  if (mine < rows && h == 0 && chunk == 0) w.D[stat] = dsum;
   float lse = w.lse[stat];
   lse = lse == -INFINITY ? INFINITY : EXACT ? lse : lse * kLog2e;   // a row that sees nothing: weights of 0
 #pragma unroll
@@ -240,7 +247,7 @@ __global__ __launch_bounds__(256, (dq_per_unit<E, D>())) void plain_dq_kernel(Pa
     if (it + 1 < ntiles) issue(it + 1);
 #pragma unroll
     for (int sub = 0; sub < SUBS; ++sub) {
-      const int key0 = it * TR + 32 * sub;
+      const int key0 = begin + it * TR + 32 * sub;
       if (key0 > most) continue;
       const char *K = smem + (it & 1) * STAGE + sub * SUB, *V = K + MATRIX;
       f32x16 sc = {}, pc = {};
@@ -269,6 +276,17 @@ __global__ __launch_bounds__(256, (dq_per_unit<E, D>())) void plain_dq_kernel(Pa
     }
   }
   if (mine >= rows) return;
+  if (chunked) {
+    float *const to = w.dq_part + (chunk * ((int64_t)w.where.q_tokens * w.kv_heads * r) + (int64_t)(s.q0 + tok) * ((int64_t)w.kv_heads * r) + head) * d;
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int col = 32 * cb + 8 * q + 4 * h;
+        if (col < d) *reinterpret_cast<f32x4 *>(to + col) = quarter_of(acc[cb], q);
+      }
+    return;
+  }
   E *const to = row_at<E>(w.dq, s.q0 + tok, j, g);
 #pragma unroll
   for (int cb = 0; cb < CB; ++cb)
@@ -301,11 +319,12 @@ __global__ __launch_bounds__((Dkv<E, D>::THREADS)) void plain_dkv_kernel(PackedB
   unsigned at;
   if (!find_piece(w.where, blockIdx.x / w.kv_heads, [&](const Span &s) { return (unsigned)((s.lk + L::OWNED - 1) / L::OWNED * w.splits); }, s, at)) return;
   const int split = at % w.splits, block0 = (int)(at / w.splits) * L::OWNED, shift = s.lk - s.lq;
-  const int each = (r + w.splits - 1) / w.splits, g0 = split * each, g1 = min(r, g0 + each);
   const int role = wave / L::PAIRS, pair = wave % L::PAIRS;
   const int own0 = block0 + pair * 32, mine = own0 + (lane & 31), key = min(mine, s.lk - 1);
   const int first = max(0, block0 - shift) / 32, tiles = s.lq > first * 32 ? (s.lq - first * 32 + 31) / 32 : 0;   // of a head: from the first query that sees the block on
-  const int n = max(0, g1 - g0) * tiles;
+  // the workgroup's part of the tiles of all heads of the group, one head after the other: n from tile t0 of head g0 on
+  const int n0 = (int)((int64_t)r * tiles * split / w.splits), n = (int)((int64_t)r * tiles * (split + 1) / w.splits) - n0;
+  const int g0 = tiles ? n0 / tiles : 0, t0 = n0 - g0 * tiles;
 
   // two matrices of two bands, NI instructions each, dealt out over the waves
   constexpr int ALL = 4 * P::NI, IPW = (ALL + WAVES - 1) / WAVES;
@@ -317,7 +336,7 @@ __global__ __launch_bounds__((Dkv<E, D>::THREADS)) void plain_dkv_kernel(PackedB
     dma_off[i] = P::dma_offset(second ? dp : qp, in / P::NI, lane, in % P::NI, d);
   }
   const uint32_t lds0 = lds_address(smem);
-  int ig = g0, it_of = 0;   // what is issued next
+  int ig = g0, it_of = t0;   // what is issued next
   auto issue = [&](int stage) {
     const int row0 = (first + it_of) * 32;
     const RowStream qs{reinterpret_cast<const char *>(row_at<E>(w.q, s.q0 + row0, j, ig)), s.lq - row0, qp};
@@ -354,7 +373,7 @@ __global__ __launch_bounds__((Dkv<E, D>::THREADS)) void plain_dkv_kernel(PackedB
 #pragma unroll
   for (int cb = 0; cb < CB; ++cb) acc[cb] = f32x16{};
   f32x4 *const xchg = reinterpret_cast<f32x4 *>(smem + 2 * L::STAGE) + pair * 256 + lane;
-  int t = 0;
+  int t = t0;
   for (int it = 0; it < n; ++it) {
     wait_and_barrier<0>();
     if (it + 1 < n) issue((it + 1) & 1);

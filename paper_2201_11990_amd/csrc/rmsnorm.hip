@@ -126,12 +126,12 @@ __global__ __launch_bounds__(threads_of<W>()) void rmsnorm_fwd_kernel(NormArgs a
         for (int off = 1; off < a.columns / 8; off *= 2) m = fmaxf(m, __shfl_xor(m, off, 64));
       }
       if (j >= nvec) continue;
-      const float scale = m > 0.0f ? m / E4M3_MOST : 1.0f;
+      const float scale = m > 0.0f ? m * (1.0f / E4M3_MOST) : 1.0f, inverse = m > 0.0f ? E4M3_MOST / m : 1.0f;
       const int first = a.columns ? 8 * j % a.columns : j;
       if (first == 0) a.scale[row * a.scales + (a.columns ? 8 * j / a.columns : 0)] = scale;
       float y[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = v[i][e] / scale;
+      for (int e = 0; e < 8; ++e) y[e] = v[i][e] * inverse;
       *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(a.out) + row * a.h + 8 * j) =
           uint2{e4m3_of4(y[0], y[1], y[2], y[3]), e4m3_of4(y[4], y[5], y[6], y[7])};
     }
@@ -276,7 +276,7 @@ __global__ __launch_bounds__(1024) void rmsnorm_bwd_wide_kernel(NormBwdArgs a) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
   __shared__ float red[16];
   constexpr int ES = sizeof(E), HALVES = ES / 2, SEG = 64 * 8 * ES, STORES = NV * HALVES;   // SEG: a wave's bytes of a piece
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), nvec = a.h / 8;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const bool with_dres = a.dres != nullptr;
   const uint32_t bytes = (uint32_t)a.h * ES;
   char *const mine = smem + wave * (PRE * NV * SEG);
@@ -318,13 +318,13 @@ __global__ __launch_bounds__(1024) void rmsnorm_bwd_wide_kernel(NormBwdArgs a) {
     gamma[i] = Raw8<E>{};
     if (column(i) < a.h) gamma[i].load(static_cast<const E *>(a.gamma) + column(i));
   }
+  // rstd by scalar loads, which are counted apart: a vector load behind the next row's DMA would be waited for with it
+  const auto rstd = (const __attribute__((address_space(4))) float *)a.rstd;
   int64_t row = blockIdx.x;
-  float r_next = a.rstd[row];
   fetch(row);
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   for (; row < a.rows; row += gridDim.x) {
-    float r = r_next;
-    asm volatile("" : "+v"(r));   // here: a wait for it behind the next row's DMA would be one for that too
+    const float r = rstd[row];
     Raw8<E> x[NV], d[NV], res[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
@@ -339,10 +339,7 @@ __global__ __launch_bounds__(1024) void rmsnorm_bwd_wide_kernel(NormBwdArgs a) {
       keep(res[i]);
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    if (row + gridDim.x < a.rows) {
-      r_next = a.rstd[row + gridDim.x];
-      fetch(row + gridDim.x);
-    }
+    if (row + gridDim.x < a.rows) fetch(row + gridDim.x);
     float dot = 0.0f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {

@@ -29,7 +29,10 @@ struct RotaryArgs {
   int tile;     // tokens of a workgroup
 };
 
-constexpr int THREADS = 256, MAX_PAIRS = 1024, MAX_TILE = 8;   // pairs and tokens of a tile
+// Pairs of a tile: one to a thread.  8192 tokens of 20 heads of 128 on buffers that no cache holds, halves, then side by side: 3 tokens to a tile 22.5 and 31 us, 6 and 3 22.5 and
+// 27.5, 4 (side by side) 25.4, 8 27 and 28.7.
+constexpr int THREADS = 256, MAX_PAIRS = THREADS, MAX_TILE = 64;
+constexpr int AHEAD = 2;   // rows of a thread at once: 3 and 4 cost registers and with them waves (24.6, 27 us)
 
 // turns of pair i for one position
 __device__ double frequency(const RotaryArgs &a, int i) {
@@ -42,88 +45,98 @@ __device__ double frequency(const RotaryArgs &a, int i) {
   return f;
 }
 
-template <typename E, int V> struct Piece { E v[V]; };
 template <typename E, int V>
-__device__ __forceinline__ void load_piece(const E *p, float (&x)[V]) {
-  struct alignas(sizeof(E) * V < 16 ? sizeof(E) * V : 16) Raw { E v[V]; };
-  const Raw t = *reinterpret_cast<const Raw *>(p);
-#pragma unroll
-  for (int e = 0; e < V; ++e) x[e] = to_f32(t.v[e]);
-}
-template <typename E, int V>
-__device__ __forceinline__ void store_piece(E *p, const float (&x)[V]) {
-  struct alignas(sizeof(E) * V < 16 ? sizeof(E) * V : 16) Raw { E v[V]; };
-  Raw t;
-#pragma unroll
-  for (int e = 0; e < V; ++e) t.v[e] = from_f32<E>(x[e]);
-  *reinterpret_cast<Raw *>(p) = t;
-}
+struct alignas(sizeof(E) * V < 16 ? sizeof(E) * V : 16) Piece { E v[V]; };
 
-// An item is V pairs of a head (HALF: V columns of either half) or V columns (interleaved: V / 2 pairs), or V columns that are copied.
+// A thread takes the same item of every head it works on: V pairs (HALF: V columns of either half), V columns (interleaved: V / 2 pairs), or V columns that are copied.
+// The first AHEAD rows of each are read before the sines are worked out, which takes about as long as the reads.
 template <typename E, int V, bool HALF>
 __global__ __launch_bounds__(THREADS) void rotary_kernel(RotaryArgs a) {
   __shared__ float2 turn[MAX_PAIRS];   // [token of the tile][pair]
   __shared__ int place[MAX_TILE];      // positions of the tile's tokens
+  __shared__ double rate[128];         // turns of each pair for one position
   const int pairs = a.n / 2;
   const int64_t first = (int64_t)blockIdx.x * a.tile;
   const int tokens = (int)(a.tokens - first < a.tile ? a.tokens - first : a.tile);
-  for (int t = threadIdx.x; t < tokens; t += THREADS) place[t] = a.positions ? a.positions[first + t] : (int)(first + t);
-  __syncthreads();
-  for (int p = threadIdx.x; p < tokens * pairs; p += THREADS) {
-    const int t = p / pairs, i = p - t * pairs;
-    double x = place[t] * frequency(a, i);
-    x -= rint(x);
-    float s, c;
-    sincospif(2.0f * (float)x, &s, &c);
-    turn[p] = float2{c * a.amplitude, s * a.amplitude * a.sign};
-  }
-  __syncthreads();
   const int turned = HALF ? pairs / V : a.n / V, items = turned + a.copied, at_once = THREADS / items;
-  const int item = threadIdx.x % items, row0 = threadIdx.x / items;
-  if (row0 >= at_once) return;
-  const int rows = a.heads + a.kv_heads;
+  const int item = threadIdx.x % items, row0 = threadIdx.x / items, heads = a.heads + a.kv_heads, rows = row0 < at_once ? tokens * heads : 0;
   const bool copy = item >= turned;
   const int col = copy ? a.n + (item - turned) * V : item * V;
-  int t = row0 / rows, head = row0 % rows;
-  for (; t < tokens;) {
-    if (place[t] >= 0) {   // a negative position: a row of padding, left as it is
-      const bool query = head < a.heads;
-      const int j = query ? head / a.group : head - a.heads, g = query ? head - j * a.group : 0;
-      const int64_t *is = query ? a.qs : a.ks, *os = query ? a.qos : a.kos;
-      const E *in = static_cast<const E *>(query ? a.q : a.k) + (first + t) * is[0] + j * is[1] + g * is[2] + col;
-      E *out = static_cast<E *>(query ? a.q_out : a.k_out) + (first + t) * os[0] + j * os[1] + g * os[2] + col;
-      float x[V];
-      load_piece<E, V>(in, x);
-      if (copy) {
-        store_piece<E, V>(out, x);
-      } else if constexpr (HALF) {
-        float y[V], u[V], w[V];
-        load_piece<E, V>(in + pairs, y);
+  struct Spot {
+    const E *in;
+    E *out;
+    int t;
+  };
+  auto spot = [&](int row) {
+    Spot s;
+    s.t = row / heads;
+    const int head = row - s.t * heads;
+    const bool query = head < a.heads;
+    const int j = query ? head / a.group : head - a.heads, g = query ? head - j * a.group : 0;
+    const int64_t *is = query ? a.qs : a.ks, *os = query ? a.qos : a.kos;
+    s.in = static_cast<const E *>(query ? a.q : a.k) + (first + s.t) * is[0] + j * is[1] + g * is[2] + col;
+    s.out = static_cast<E *>(query ? a.q_out : a.k_out) + (first + s.t) * os[0] + j * os[1] + g * os[2] + col;
+    return s;
+  };
+  auto work_out_turns = [&] {
+    if (threadIdx.x < pairs) rate[threadIdx.x] = frequency(a, threadIdx.x);
+    else if (threadIdx.x >= 128 && threadIdx.x - 128 < tokens) place[threadIdx.x - 128] = a.positions ? a.positions[first + threadIdx.x - 128] : (int)(first + threadIdx.x - 128);
+    __syncthreads();
+    for (int p = threadIdx.x; p < tokens * pairs; p += THREADS) {
+      const int t = p / pairs, i = p - t * pairs;
+      double x = place[t] * rate[i];
+      x -= rint(x);
+      float s, c;
+      sincospif(2.0f * (float)x, &s, &c);
+      turn[p] = float2{c * a.amplitude, s * a.amplitude * a.sign};
+    }
+    __syncthreads();
+  };
+  bool begun = false;
+  int row = row0;
+  do {
+    Piece<E, V> x[AHEAD], y[HALF ? AHEAD : 1];
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-          const float2 cs = turn[t * pairs + col + e];
-          u[e] = x[e] * cs.x - y[e] * cs.y;
-          w[e] = x[e] * cs.y + y[e] * cs.x;
-        }
-        store_piece<E, V>(out, u);
-        store_piece<E, V>(out + pairs, w);
-      } else {
-        float u[V];
-#pragma unroll
-        for (int e = 0; e < V; e += 2) {
-          const float2 cs = turn[t * pairs + (col + e) / 2];
-          u[e] = x[e] * cs.x - x[e + 1] * cs.y;
-          u[e + 1] = x[e] * cs.y + x[e + 1] * cs.x;
-        }
-        store_piece<E, V>(out, u);
+    for (int u = 0; u < AHEAD; ++u) {
+      if (row + u * at_once < rows) {
+        const Spot s = spot(row + u * at_once);
+        x[u] = *reinterpret_cast<const Piece<E, V> *>(s.in);
+        if (HALF && !copy) y[HALF ? u : 0] = *reinterpret_cast<const Piece<E, V> *>(s.in + pairs);
       }
     }
-    head += at_once;
-    while (head >= rows) {
-      head -= rows;
-      ++t;
+    if (!begun) work_out_turns();
+    begun = true;
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      if (row + u * at_once >= rows) continue;
+      const Spot s = spot(row + u * at_once);
+      if (place[s.t] < 0) continue;   // a row of padding, left as it is
+      Piece<E, V> out[HALF ? 2 : 1];
+      const float2 *const by = turn + s.t * pairs;
+      if (copy) {
+        out[0] = x[u];
+      } else if constexpr (HALF) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          const float2 cs = by[col + e];
+          const float v = to_f32(x[u].v[e]), w = to_f32(y[u].v[e]);
+          out[0].v[e] = from_f32<E>(v * cs.x - w * cs.y);
+          out[HALF].v[e] = from_f32<E>(v * cs.y + w * cs.x);
+        }
+        *reinterpret_cast<Piece<E, V> *>(s.out + pairs) = out[HALF];
+      } else {
+#pragma unroll
+        for (int e = 0; e < V; e += 2) {
+          const float2 cs = by[(col + e) / 2];
+          const float v = to_f32(x[u].v[e]), w = to_f32(x[u].v[e + 1]);
+          out[0].v[e] = from_f32<E>(v * cs.x - w * cs.y);
+          out[0].v[e + 1] = from_f32<E>(v * cs.y + w * cs.x);
+        }
+      }
+      *reinterpret_cast<Piece<E, V> *>(s.out) = out[0];
     }
-  }
+    row += AHEAD * at_once;
+  } while (row - row0 < tokens * heads);   // the same number of turns for all threads
 }
 
 template <typename E, bool HALF>
@@ -133,8 +146,10 @@ int launch(RotaryArgs &a, bool in_place, hipStream_t st) {
   const int V = unit % 8 == 0 ? 8 : unit % 4 == 0 ? 4 : HALF ? 1 : 2;
   a.copied = in_place ? 0 : (a.d - a.n) / V;
   const int pairs = a.n / 2, rows = a.heads + a.kv_heads;
+  const int at_once = THREADS / ((HALF ? pairs / V : a.n / V) + a.copied), want = 2 * AHEAD * at_once / rows;   // two rounds of a workgroup's reads
   a.tile = MAX_PAIRS / pairs < MAX_TILE ? MAX_PAIRS / pairs : MAX_TILE;
-  if (rows > 64) a.tile = (a.tile + 3) / 4;
+  if (want < a.tile) a.tile = want < 1 ? 1 : want;
+  if (a.tokens < 512 * (int64_t)a.tile) a.tile = (int)((a.tokens + 511) / 512);   // few tokens: more workgroups
   const unsigned blocks = (unsigned)((a.tokens + a.tile - 1) / a.tile);
   LaunchScope scope(MTNLG_K_ELEMENTWISE, st);
   if (V == 8) rotary_kernel<E, 8, HALF><<<blocks, THREADS, 0, st>>>(a);

@@ -206,7 +206,7 @@ def test_a_row_by_row_product_matches_the_matrix_instructions():
 def test_single_tokens_over_long_caches(dtype, keys, group, d):
     c = Case([1] * len(keys), keys, 2, group, d, dtype, backward=False, seed=len(keys))
     fwd, _ = c.workspaces()
-    assert fwd is not None   # the keys are cut
+    assert fwd is not None or max(keys) < 1000   # the keys are cut where they are long enough
     c.run()
     want = c.want()
     c.check(want)
