@@ -48,10 +48,10 @@ inline bool packed_tuned(int dtype, int d) { return dtype == MTNLG_BF16 && d <= 
 // owned: rows of a workgroup (plain: 128); blocks, pieces: workgroups, of all heads of keys and of one
 int packed_fwd_tuned(const PackedFwdArgs &w, int owned, int64_t blocks, hipStream_t st);
 int packed_fwd_plain(int dtype, const PackedFwdArgs &w, int64_t blocks, hipStream_t st);
-int packed_bwd_tuned(const PackedBwdArgs &w, int owned, int64_t pieces, int key_owned, int64_t key_pieces, hipStream_t st);
+int packed_bwd_tuned(const PackedBwdArgs &w, int owned, int64_t pieces, int64_t key_pieces, hipStream_t st);
 int packed_bwd_plain(int dtype, const PackedBwdArgs &w, int64_t pieces, int64_t key_pieces, hipStream_t st);
 int packed_dkv_plain_owned(int dtype, int d);   // keys of a workgroup of dk / dv
-int packed_dkv_least(int d);                    // ... of the tuned kernels: this many or 128
+int packed_dkv_tuned_owned(int d);              // ... of the tuned kernels
 
 namespace {
 
@@ -332,37 +332,6 @@ __device__ __forceinline__ void add_seen_rows(f32x16 (&acc)[D / 32], const f32x1
         for (int e = 0; e < 4; ++e) acc[cb][4 * q + e] = fmaf(p, v[e], acc[cb][4 * q + e]);
         __builtin_amdgcn_sched_barrier(0);   // no registers for more reads at once
       }
-  }
-}
-
-// The two kinds of product of 32 rows of a tile, fragments a few steps ahead of their MFMAs (bf16: in fenced steps, the compiler otherwise reads all
-// fragments first, into registers that the kernels do not have).
-template <typename E, int D>
-__device__ __forceinline__ void products_with_units(const char *t, const typename Elem<E, D>::Lane &ln, const typename Elem<E, D>::Unit (&own)[Elem<E, D>::K1], f32x16 &v) {
-  using P = Elem<E, D>;
-  if constexpr (sizeof(E) == 2) {
-    typename P::Unit fr[4];
-    pipelined<P::K1, 3>([&](int i) { fr[i & 3] = P::unit(t, ln, i); }, [&](int i) { v = P::mma(fr[i & 3], own[i], v); }, [](int) {});
-  } else {
-#pragma unroll
-    for (int kk = 0; kk < P::K1; ++kk) v = P::mma(P::unit(t, ln, kk), own[kk], v);
-  }
-}
-template <typename E, int D>
-__device__ __forceinline__ void products_with_rows(f32x16 (&acc)[D / 32], const f32x16 &v, const char *t, const typename Elem<E, D>::Lane &ln) {
-  using P = Elem<E, D>;
-  if constexpr (sizeof(E) == 2) {
-    const typename P::Weights x[2] = {P::weights(v, 0), P::weights(v, 1)};
-    typename P::Column fr[4];
-    pipelined<P::K1, 3>([&](int i) { fr[i & 3] = P::column(t, ln, i / 2, i % 2); }, [&](int i) { acc[i / 2] = P::mma_rows(fr[i & 3], x[i % 2], acc[i / 2]); },
-                        [](int) {});
-  } else {
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const typename P::Weights x = P::weights(v, u);
-#pragma unroll
-      for (int cb = 0; cb < D / 32; ++cb) acc[cb] = P::mma_rows(P::column(t, ln, cb, u), x, acc[cb]);
-    }
   }
 }
 

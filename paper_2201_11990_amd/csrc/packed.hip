@@ -153,12 +153,8 @@ BwdPlan bwd_plan(const PackedShape &S) {
     p.owned = 64;
     p.pieces = pieces_bound(rows, most, S.where.count, p.owned);
   }
-  p.key_owned = packed_tuned(S.dtype, S.d) ? 128 : packed_dkv_plain_owned(S.dtype, S.d);
+  p.key_owned = packed_tuned(S.dtype, S.d) ? packed_dkv_tuned_owned(S.d) : packed_dkv_plain_owned(S.dtype, S.d);
   p.key_pieces = pieces_bound(S.where.k_tokens, S.max_k, S.where.count, p.key_owned);
-  if (packed_tuned(S.dtype, S.d) && p.key_pieces * S.heads < 512) {
-    p.key_owned = packed_dkv_least(S.d);
-    p.key_pieces = pieces_bound(S.where.k_tokens, S.max_k, S.where.count, p.key_owned);
-  }
   // Where the keys leave units idle, a workgroup's tiles of queries (of all heads of the group) are dealt out: about 512 workgroups, of 8 tiles at least, which the
   // joining launch and the parts' way through memory cost.
   const int64_t wide = p.key_pieces * S.kv_heads, tiles = (int64_t)S.group * ((S.max_q + 31) / 32);
@@ -297,7 +293,7 @@ int mtnlg_packed_attention_bwd(const mtnlg_packed_desc *desc, const mtnlg_packed
   w.dq_part = (float *)((char *)workspace + plan.d_bytes + plan.part_bytes);
   const hipStream_t st = (hipStream_t)stream;
   LaunchScope scope(MTNLG_K_ATTN_BWD, st);
-  MTNLG_TRY(packed_tuned(S.dtype, S.d) ? packed_bwd_tuned(w, plan.owned, plan.pieces, plan.key_owned, plan.key_pieces, st)
+  MTNLG_TRY(packed_tuned(S.dtype, S.d) ? packed_bwd_tuned(w, plan.owned, plan.pieces, plan.key_pieces, st)
                                        : packed_bwd_plain(S.dtype, w, plan.pieces, plan.key_pieces, st));
   if (plan.cut.chunks > 1) {
     const unsigned joins = (unsigned)(pieces_bound((int64_t)S.where.q_tokens * S.group, (int64_t)S.max_q * S.group, S.where.count, 4) * S.kv_heads);

@@ -266,27 +266,27 @@ __global__ __launch_bounds__(DQ_THREADS, dq_per_unit<D>()) void packed_dq_kernel
 // ------------------------------------------------------------------ dk and dv
 // Eight waves, two to a SIMD, in pairs (roles 0 and 1) of which each owns 32 keys and takes 32 rows of a tile: role 0 forms S and P and accumulates dv,
 // role 1 forms dP and dS and accumulates dk.  P goes to role 1 through LDS in fp32.  The second product runs one tile behind, so that one barrier a tile serves the exchange as well.
-// OWNED 128: tiles of 32 rows; OWNED 64: of 64, the pairs of a group of keys take one half each and are merged through LDS at the end.
-constexpr int DKV_THREADS = 512;
-template <int D, int OWNED> struct DkvLds {
-  static constexpr int ROWS = OWNED == 128 ? 32 : 64, GROUPS = OWNED / 32, PARTS = ROWS / 32, PAIRS = GROUPS * PARTS;
+// D up to 128: a workgroup owns 64 keys and takes tiles of 64 rows; the two pairs of a group of keys take one half each and are merged through LDS at the end.
+// Wider ones: 128 keys and tiles of 32 rows (64 x 192 do not fit three times).  Both ways, median us, 64 / 128 keys: 16 sequences of 134 to 2048 tokens,
+// 16 heads of 128: 186 / 180 and 15 for the join of its tiles' parts, which 64 keys do without; 8192 tokens, 32 heads of 128 (4 of keys): 1970 / 2051;
+// 13 sequences of 512 tokens and fewer, 8 heads of 64: 13 / 17; 8 sequences, 12 heads of 160: 139 / 133.
+template <int D> struct Dkv {
+  static constexpr int OWNED = D <= 128 ? 64 : 128, PARTS = 128 / OWNED, PAIRS = 4, THREADS = 128 * PAIRS;
+  static constexpr int ROWS = 32 * PARTS, GROUPS = OWNED / 32;
   static constexpr int MATRIX = ROWS * D * 2, STAGE = 2 * MATRIX + 512;   // Q tile, dO tile, 256 bytes each of lse and -D
   static constexpr int XCHG = PAIRS * 4096;                               // P of a tile
-  static constexpr int ROOM = 160 * 1024;
-  static constexpr int RING = 4 * STAGE + 2 * XCHG <= ROOM ? 4 : 3, AHEAD = RING - 2;   // tiles in LDS, and fetched ahead
+  static constexpr int RING = 4 * STAGE + 2 * XCHG <= 160 * 1024 ? 4 : 3, AHEAD = RING - 2;   // tiles in LDS, and fetched ahead
   static constexpr int BYTES = RING * STAGE + 2 * XCHG;
-  static constexpr bool FITS = BYTES <= ROOM;
-  static_assert(128 * PAIRS == DKV_THREADS, "");
+  static_assert(BYTES <= 160 * 1024, "");
 };
-// Keys of a workgroup: 64 while 128 would leave units idle, where LDS has room for their tiles
-template <int D> constexpr int dkv_least() { return DkvLds<D, 64>::FITS ? 64 : 128; }
 
-template <int D, int OWNED>
-__global__ __launch_bounds__(DKV_THREADS) void packed_dkv_kernel(PackedBwdArgs w) {
+template <int D>
+__global__ __launch_bounds__(Dkv<D>::THREADS) void packed_dkv_kernel(PackedBwdArgs w) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
   using P = Elem<bf16, D>;
   using T = typename P::T;
-  using L = DkvLds<D, OWNED>;
+  using L = Dkv<D>;
+  constexpr int OWNED = L::OWNED, PARTS = L::PARTS, PAIRS = L::PAIRS;
   constexpr int K1 = D / 16, CB = D / 32, STAGE = L::STAGE, RING = L::RING, AHEAD = L::AHEAD, ROWS = L::ROWS;
   constexpr int N = 2 * K1, NF = D == 128 ? 8 : D == 160 ? 10 : 4, PF = D == 128 ? 5 : D == 160 ? 6 : NF - 1;   // steps of a tile: K1 for the first product, K1 for the second of the tile before
   constexpr int HAND_OVER = N - PF;
@@ -298,7 +298,7 @@ __global__ __launch_bounds__(DKV_THREADS) void packed_dkv_kernel(PackedBwdArgs w
   unsigned at;
   if (!find_piece(w.where, blockIdx.x / w.kv_heads, [&](const Span &s) { return (unsigned)((s.lk + OWNED - 1) / OWNED * w.splits); }, s, at)) return;
   const int split = at % w.splits, block0 = (int)(at / w.splits) * OWNED, shift = s.lk - s.lq;
-  const int part = L::PARTS == 2 ? wave >> 1 & 1 : 0, role = wave >> 2;
+  const int part = PARTS == 2 ? wave >> 1 & 1 : 0, role = wave / PAIRS;
   const int own0 = block0 + (wave & (L::GROUPS - 1)) * 32, mine = own0 + (lane & 31), key = min(mine, s.lk - 1);
   const int first = max(0, block0 - shift) / ROWS * ROWS, tiles = s.lq > first ? (s.lq - first + ROWS - 1) / ROWS : 0;   // of a head: from the first query that sees the block on
   // The workgroup's part of the tiles of all heads of the group, one head after the other: n from tile t0 of head g0 on.
@@ -308,13 +308,13 @@ __global__ __launch_bounds__(DKV_THREADS) void packed_dkv_kernel(PackedBwdArgs w
   typename P::Lane ln(lane);
   const uint32_t smem_addr = lds_address(smem);
 
-  // Waves 0-3 bring the Q tile, waves 4-7 the dO tile (bands of 16 rows, NI instructions each, dealt out over the four; what does not come out even is brought twice), and
+  // The waves of role 0 bring the Q tile, those of role 1 the dO tile (bands of 16 rows, NI instructions each, dealt out over them; what does not come out even is brought twice), and
   // every wave the tile's lse values (even waves) or -D values (odd ones): all issue the same number of memory operations, which the counted waits rely on.
-  constexpr int ALL = ROWS / 16 * T::NI, IPW = (ALL + 3) / 4, OPS = IPW + 1;
-  const int half = wave >> 2;
+  constexpr int ALL = ROWS / 16 * T::NI, IPW = (ALL + PAIRS - 1) / PAIRS, OPS = IPW + 1;
+  const int half = wave / PAIRS;
   const Heads &mat = half ? w.da : w.q;
   const uint32_t pitch = (uint32_t)(mat.token * 2);
-  auto instruction = [&](int i) { return ((wave & 3) + 4 * i) % ALL; };
+  auto instruction = [&](int i) { return (wave % PAIRS + PAIRS * i) % ALL; };
   uint32_t dma_off[IPW];
 #pragma unroll
   for (int i = 0; i < IPW; ++i) dma_off[i] = T::dma_offset(pitch, instruction(i) / T::NI, lane, instruction(i) % T::NI, d);
@@ -365,7 +365,7 @@ __global__ __launch_bounds__(DKV_THREADS) void packed_dkv_kernel(PackedBwdArgs w
     for (int kk = 0; kk < K1; ++kk) arrive(of[kk]);
   }
   // the loop, once for each role
-  f32x4 *const xchg = reinterpret_cast<f32x4 *>(smem + RING * STAGE) + (wave & 3) * 256 + lane;   // 4 x 64 of the pair
+  f32x4 *const xchg = reinterpret_cast<f32x4 *>(smem + RING * STAGE) + wave % PAIRS * 256 + lane;   // 4 x 64 of the pair
   auto run = [&](auto ROLE) __attribute__((always_inline)) {
     constexpr int me = decltype(ROLE)::value;
     const int part_rows = part * T::ROWS32;
@@ -399,6 +399,7 @@ __global__ __launch_bounds__(DKV_THREADS) void packed_dkv_kernel(PackedBwdArgs w
       for (int q = 0; q < 4; ++q) xchg[(odd ^ 1) * (L::XCHG / 16) + q * 64] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     }
     wait_and_barrier<(AHEAD - 1) * OPS>();   // tile 0 landed everywhere
+    redo |= rows_not_finite<bf16, D>(smem + SECOND_AT + part_rows, ln);   // whose rows those zeros meet
 #pragma unroll
     for (int i = 0; i < PF; ++i) load(i);
     __builtin_amdgcn_sched_barrier(0);
@@ -461,7 +462,7 @@ __global__ __launch_bounds__(DKV_THREADS) void packed_dkv_kernel(PackedBwdArgs w
           for (int e = 0; e < 16; ++e)
             if (r == 2 + e * (K1 - 2) / 16) prev[e] *= p[e];
           if (r == K1) {
-            if (masked(row_before)) {   // (before the first tile there is none: this looks at the first, which comes again)
+            if (masked(row_before)) {   // (before the first tile there is none: this looks at the first)
               hide(row_before, prev);
               redo |= rows_not_finite<bf16, D>(before + SECOND_AT + part_rows, ln);
             }
@@ -523,9 +524,9 @@ __global__ __launch_bounds__(DKV_THREADS) void packed_dkv_kernel(PackedBwdArgs w
 
   // Two parts: of the two waves with the same rows and role each hands over half of its columns and finishes the other half
   f32x4 *slots = reinterpret_cast<f32x4 *>(smem) + lane;
-  if constexpr (L::PARTS == 2) {
+  if constexpr (PARTS == 2) {
     int *const bad = reinterpret_cast<int *>(smem + 8 * CB * 2 * 1024);
-    static_assert(8 * CB * 2 * 1024 + 64 <= L::BYTES, "");
+    static_assert(PAIRS == 4 && 8 * CB * 2 * 1024 + 64 <= L::BYTES, "");
     __syncthreads();   // the rings are no longer read
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb)
@@ -590,7 +591,7 @@ __global__ __launch_bounds__(DKV_THREADS) void packed_dkv_kernel(PackedBwdArgs w
   if (mine >= s.lk) return;
 #pragma unroll
   for (int cb = 0; cb < CB; ++cb) {
-    if constexpr (L::PARTS == 2) {
+    if constexpr (PARTS == 2) {
 #pragma unroll
       for (int q = 0; q < 2; ++q) {
         const f32x4 other = slots[(((wave ^ 2) * CB + cb) * 2 + q) * 64];
@@ -605,35 +606,32 @@ __global__ __launch_bounds__(DKV_THREADS) void packed_dkv_kernel(PackedBwdArgs w
 }
 
 template <int D>
-int bwd_launch(const PackedBwdArgs &w, int owned, int64_t pieces, int key_owned, int64_t key_pieces, hipStream_t st) {
+int bwd_launch(const PackedBwdArgs &w, int owned, int64_t pieces, int64_t key_pieces, hipStream_t st) {
   constexpr int merge = 4 * (D / 32) * 2048 + 64, ring = 4 * Tile<D>::BYTES, smem = ring > merge ? ring : merge;
-  constexpr int LEAST = dkv_least<D>();
   static unsigned long long attr_done = 0;
   int device;
   if (!attr_is_set(attr_done, &device)) {
     MTNLG_TRY(set_lds(packed_dq_kernel<D, 1>, smem));
     MTNLG_TRY(set_lds(packed_dq_kernel<D, 2>, smem));
-    MTNLG_TRY(set_lds(packed_dkv_kernel<D, 128>, DkvLds<D, 128>::BYTES));
-    MTNLG_TRY(set_lds(packed_dkv_kernel<D, LEAST>, DkvLds<D, LEAST>::BYTES));
+    MTNLG_TRY(set_lds(packed_dkv_kernel<D>, Dkv<D>::BYTES));
     attr_mark_set(attr_done, device);
   }
   const unsigned blocks = (unsigned)(pieces * w.kv_heads), key_blocks = (unsigned)(key_pieces * w.splits * w.kv_heads);
   if (owned == 64) packed_dq_kernel<D, 2><<<blocks, DQ_THREADS, smem, st>>>(w);
   else packed_dq_kernel<D, 1><<<blocks, DQ_THREADS, smem, st>>>(w);
   MTNLG_TRY(check_launch());
-  if (key_owned == 128) packed_dkv_kernel<D, 128><<<key_blocks, DKV_THREADS, DkvLds<D, 128>::BYTES, st>>>(w);
-  else packed_dkv_kernel<D, LEAST><<<key_blocks, DKV_THREADS, DkvLds<D, LEAST>::BYTES, st>>>(w);
+  packed_dkv_kernel<D><<<key_blocks, Dkv<D>::THREADS, Dkv<D>::BYTES, st>>>(w);
   return check_launch();
 }
 
 }  // namespace
 
-int packed_dkv_least(int d) {
-  return packed_tuned_by_size(d, [&](auto D) { return dkv_least<decltype(D)::value>(); });
+int packed_dkv_tuned_owned(int d) {
+  return packed_tuned_by_size(d, [&](auto D) { return Dkv<decltype(D)::value>::OWNED; });
 }
 
-int packed_bwd_tuned(const PackedBwdArgs &w, int owned, int64_t pieces, int key_owned, int64_t key_pieces, hipStream_t st) {
-  return packed_tuned_by_size(w.d, [&](auto D) { return bwd_launch<decltype(D)::value>(w, owned, pieces, key_owned, key_pieces, st); });
+int packed_bwd_tuned(const PackedBwdArgs &w, int owned, int64_t pieces, int64_t key_pieces, hipStream_t st) {
+  return packed_tuned_by_size(w.d, [&](auto D) { return bwd_launch<decltype(D)::value>(w, owned, pieces, key_pieces, st); });
 }
 
 }  // namespace mtnlg

@@ -79,6 +79,8 @@ def reference(q, k, v, da, q_spans, k_spans, scale=None):
 
 def assert_within(got, want, what):
     value, bound = want
+    if not got.numel():
+        return
     got = got.double()
     same = (got == value) | (torch.isnan(got) & torch.isnan(value))
     off = torch.where(same, 0.0, (got - value).abs() - bound * (1 + 1e-6))

@@ -351,3 +351,73 @@ def test_gradients_against_differences():
         slope, along = (sums[0] - sums[1]) / (2 * h), (grad * way.double()).sum()
         size = (grad.abs() * way.double().abs()).sum()
         assert abs(slope - along) <= 2e-3 * size, (name, float(slope), float(along))
+
+
+@pytest.mark.parametrize("dtype,ql,kl,kv,group,d", [
+    ("fp32", [3, 40, 1], [900, 1300, 0], 2, 2, 96), ("fp32", [700], [700], 1, 1, 64), ("fp32", [130, 600, 0, 33], [130, 600, 70, 20], 2, 3, 128),
+    ("bf16", [700], [700], 1, 1, 64), ("bf16", [700, 64, 1], [900, 30, 700], 1, 8, 128), ("bf16", [520, 257], [520, 257], 2, 4, 160),
+    ("bf16", [600], [600], 1, 5, 192), ("bf16", [600, 100], [600, 100], 1, 4, 256)])
+def test_work_that_is_cut_and_joined(dtype, ql, kl, kv, group, d):
+    # few workgroups: dq's keys (fp32) and the queries of dk and dv are dealt out over more of them, whose parts a further launch adds
+    c = Case(ql, kl, kv, group, d, dtype, seed=21)
+    desc = M.packed_desc(c.q, c.k, len(ql), c.max_q, c.max_k)
+    assert M.mtnlg_packed_attention_bwd_workspace(desc) > 8 * c.lse.numel()   # more than a sum for each row
+    c.run()
+    c.check()
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 160), ("bf16", 256), ("fp32", 64)])
+def test_what_a_query_does_not_see_in_work_that_is_cut(dtype, d):
+    n, at, early = 1100, 901, 300
+    c = Case([n], [n], 1, 2, d, dtype, seed=22)
+    want = c.want()
+    part = lambda t, which: tuple(x[which] for x in t)   # noqa: E731
+    c.k[at], c.v[at] = float("nan"), float("inf")
+    c.run()
+    for name in ("a", "dq"):
+        assert_within(getattr(c, name)[:at], part(want[name], slice(0, at)), name)
+    assert not torch.isfinite(c.a[at:]).any()
+    c = Case([n], [n], 1, 2, d, dtype, seed=22)
+    c.da[early], c.q[early] = float("inf"), float("nan")
+    c.run()
+    for name in ("dk", "dv"):
+        assert_within(getattr(c, name)[early + 1:], part(want[name], slice(early + 1, None)), name)
+        assert not torch.isfinite(getattr(c, name)[:early + 1]).any()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("at", [0, 5, 70, 299])
+def test_an_infinity_that_is_seen_stays_one(dtype, d, at):
+    # one column of a value, or of an output's gradient: that column of what sees it is infinite, no other changes (weights are positive)
+    c = Case([300], [300], 1, 2, d, dtype, seed=23)
+    want = c.want()
+    c.v[at, 0, 3] = float("inf")
+    c.backward = False
+    c.run()
+    assert torch.isposinf(c.a[at:, ..., 3]).all()
+    others = torch.arange(d, device="cuda") != 3
+    assert_within(c.a[..., others], tuple(t[..., others] for t in want["a"]), "a")
+    assert_within(c.a[:at], tuple(t[:at] for t in want["a"]), "a")
+    c = Case([300], [300], 1, 2, d, dtype, seed=23)
+    c.da[at, 0, 1, 3] = float("inf")
+    c.run()
+    assert torch.isposinf(c.dv[:at + 1, 0, 3]).all()
+    assert_within(c.dv[..., others], tuple(t[..., others] for t in want["dv"]), "dv")
+    assert_within(c.dv[at + 1:], tuple(t[at + 1:] for t in want["dv"]), "dv")
+
+
+def test_two_calls_at_once():
+    # on two streams, each with its own workspace
+    cases = [Case([130, 700, 64], [130, 700, 64], 2, 4, 128, "bf16", seed=31), Case([500, 90], [500, 90], 1, 4, 64, "bf16", seed=32)]
+    alone = [{k: v.clone() for k, v in c.run().items()} for c in cases]
+    streams = [torch.cuda.Stream() for _ in cases]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for c, s in zip(cases, streams):
+            with torch.cuda.stream(s):
+                c.run()
+    torch.cuda.synchronize()
+    for c, want in zip(cases, alone):
+        for k, v in c.results().items():
+            assert torch.equal(v, want[k]), k
