@@ -61,23 +61,30 @@ __global__ __launch_bounds__(256) void packed_dq_join_kernel(PackedBwdArgs w) {
   put4(row_at<E>(w.dq, s.q0 + tok, j, g) + lane * 4, sum * w.scale);
 }
 
-// The parts of dk and dv added up: a wave to a key, four columns of dv (lower half of the lanes' columns) and dk to a lane in turn.
+// The parts of dk and dv added up: a wave to a key, four columns of dv (lower half of the lanes' columns) and dk to a lane in turn.  (Sixteen keys to a workgroup and a
+// part at a time: 8.5 us for 5 parts of 1536 keys, 4 heads of 96, and 12 for 11.)
+constexpr int DKV_JOINED = 4;   // keys of a workgroup
 template <typename E>
 __global__ __launch_bounds__(256) void packed_dkv_join_kernel(PackedBwdArgs w) {
   const int lane = threadIdx.x & 63, d = w.d, j = blockIdx.x % w.kv_heads;
   Span s;
   unsigned at;
-  if (!find_piece(w.where, blockIdx.x / w.kv_heads, [&](const Span &s) { return (unsigned)((s.lk + 15) / 16); }, s, at)) return;
+  if (!find_piece(w.where, blockIdx.x / w.kv_heads, [&](const Span &s) { return (unsigned)((s.lk + DKV_JOINED - 1) / DKV_JOINED); }, s, at)) return;
   const int64_t all = (int64_t)w.where.k_tokens * w.kv_heads * (2 * d);
-  for (int i = threadIdx.x >> 6; i < 16; i += 4) {
-    const int key = at * 16 + i;
-    if (key >= s.lk) return;
-    const float *from = w.part + ((int64_t)(s.k0 + key) * w.kv_heads + j) * (2 * d);
-    for (int col = lane * 4; col < 2 * d; col += 256) {
-      f32x4 v = *reinterpret_cast<const f32x4 *>(from + col);
-      for (int p = 1; p < w.splits; ++p) v += *reinterpret_cast<const f32x4 *>(from + p * all + col);
-      put4(col < d ? row_at<E>(w.dv, s.k0 + key, j, 0) + col : row_at<E>(w.dk, s.k0 + key, j, 0) + (col - d), v);
+  const int key = at * DKV_JOINED + (threadIdx.x >> 6);
+  if (key >= s.lk) return;
+  const float *from = w.part + ((int64_t)(s.k0 + key) * w.kv_heads + j) * (2 * d);
+  for (int col = lane * 4; col < 2 * d; col += 256) {
+    f32x4 v = {};
+    for (int p = 0; p < w.splits; p += 4) {   // four reads in flight (of the last part again past the end)
+      f32x4 part[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) part[u] = *reinterpret_cast<const f32x4 *>(from + min(p + u, w.splits - 1) * all + col);
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (p + u < w.splits) v += part[u];
     }
+    put4(col < d ? row_at<E>(w.dv, s.k0 + key, j, 0) + col : row_at<E>(w.dk, s.k0 + key, j, 0) + (col - d), v);
   }
 }
 
@@ -156,14 +163,16 @@ BwdPlan bwd_plan(const PackedShape &S) {
   p.key_owned = packed_tuned(S.dtype, S.d) ? packed_dkv_tuned_owned(S.d) : packed_dkv_plain_owned(S.dtype, S.d);
   p.key_pieces = pieces_bound(S.where.k_tokens, S.max_k, S.where.count, p.key_owned);
   // Where the keys leave units idle, a workgroup's tiles of queries (of all heads of the group) are dealt out: about 512 workgroups, of 8 tiles at least, which the
-  // joining launch and the parts' way through memory cost.
+  // joining launch and the parts' way through memory cost.  fp32: of 4, a tile takes longer (1536 tokens in 4 documents, 8 heads of 96 on 4: 73 and 7 us with 8
+  // tiles at least, 59 and 8 with 4, 61 and 11 with 2).
   const int64_t wide = p.key_pieces * S.kv_heads, tiles = (int64_t)S.group * ((S.max_q + 31) / 32);
   int64_t splits = wide >= 512 ? 1 : (512 + wide - 1) / wide;
-  if (splits > tiles / 8) splits = tiles / 8;
+  const int64_t most_splits = tiles / (S.dtype == MTNLG_F32 ? 4 : 8);
+  if (splits > most_splits) splits = most_splits;
   p.splits = (int)(splits < 1 ? 1 : splits > 64 ? 64 : splits);
   p.d_bytes = align_up((size_t)S.where.q_tokens * S.heads * sizeof(float), 256);
   p.part_bytes = p.splits > 1 ? align_up((size_t)p.splits * S.where.k_tokens * S.kv_heads * 2 * S.d * sizeof(float), 256) : 0;
-  // fp32: a tile of dq is long, and few rows are few workgroups (1536 tokens in 4 documents, 8 heads of 96 on 4: 114 us whole, 45 so)
+  // fp32: a tile of dq is long, and few rows are few workgroups (1536 tokens in 4 documents, 8 heads of 96 on 4: 114 us whole, 53 and 8 for the join so)
   p.cut = S.dtype == MTNLG_F32 ? cut_keys(S, p.pieces, 0.16 * S.d, 64, 512) : Cut{0, 1};
   p.pieces = cut_pieces(S, p.cut, p.pieces, p.owned);
   p.bytes = p.d_bytes + p.part_bytes + (p.cut.chunks > 1 ? (size_t)p.cut.chunks * S.where.q_tokens * S.heads * S.d * sizeof(float) : 0);
@@ -301,7 +310,7 @@ int mtnlg_packed_attention_bwd(const mtnlg_packed_desc *desc, const mtnlg_packed
     MTNLG_TRY(check_launch());
   }
   if (plan.splits == 1) return MTNLG_OK;
-  const unsigned joins = (unsigned)(pieces_bound(S.where.k_tokens, S.max_k, S.where.count, 16) * S.kv_heads);
+  const unsigned joins = (unsigned)(pieces_bound(S.where.k_tokens, S.max_k, S.where.count, DKV_JOINED) * S.kv_heads);
   if (S.dtype == MTNLG_F32) packed_dkv_join_kernel<float><<<joins, 256, 0, st>>>(w);
   else packed_dkv_join_kernel<bf16><<<joins, 256, 0, st>>>(w);
   return check_launch();
