@@ -45,6 +45,12 @@ struct PackedBwdArgs {
 // Head sizes up to which bf16 has kernels of its own (packed_fwd.hip, packed_bwd.hip); others and fp32: packed_plain.hip.
 constexpr int PACKED_TUNED = 192;
 inline bool packed_tuned(int dtype, int d) { return dtype == MTNLG_BF16 && d <= PACKED_TUNED; }
+// Rows of a workgroup of the forward pass and of dq: 128, and 64 (a pair of waves to 32 rows, each with half of a tile's keys) while 128 would leave some of the
+// places for workgroups, two to a unit or one, empty.  2501 and 1589 tokens, median us with 64 / 128: forward, 480 workgroups of 128 at heads of 128: 61 / 61, 384: 44 / 59;
+// heads of 192, 384: 73 / 64, 256: 52 / 62.  dq, dk and dv, heads of 128, 480: 194 / 188, 384: 145 / 157; heads of 192, 384: 265 / 251, 256: 174 / 183; heads of 160: 324 / 266
+// at 480 and 111 / 98 at 32 (64 keep twice as much in scratch memory), so always 128.
+constexpr int packed_fwd_places(int d) { return d <= 160 ? 512 : 256; }
+constexpr int packed_dq_places(int d) { return d <= 128 ? 512 : d <= 160 ? 0 : 256; }
 // owned: rows of a workgroup (plain: 128); blocks, pieces: workgroups, of all heads of keys and of one
 int packed_fwd_tuned(const PackedFwdArgs &w, int owned, int64_t blocks, hipStream_t st);
 int packed_fwd_plain(int dtype, const PackedFwdArgs &w, int64_t blocks, hipStream_t st);

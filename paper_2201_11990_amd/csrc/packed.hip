@@ -126,7 +126,7 @@ FwdPlan fwd_plan(const PackedShape &S) {
   const int64_t rows = (int64_t)S.where.q_tokens * S.group, most = (int64_t)S.max_q * S.group;
   p.owned = 128;
   p.pieces = pieces_bound(rows, most, S.where.count, p.owned);
-  if (packed_tuned(S.dtype, S.d) && p.pieces * S.kv_heads < 1024) {
+  if (packed_tuned(S.dtype, S.d) && p.pieces * S.kv_heads < packed_fwd_places(S.d)) {
     p.owned = 64;
     p.pieces = pieces_bound(rows, most, S.where.count, p.owned);
   }
@@ -156,7 +156,7 @@ BwdPlan bwd_plan(const PackedShape &S) {
   const int64_t rows = (int64_t)S.where.q_tokens * S.group, most = (int64_t)S.max_q * S.group;
   p.owned = 128;
   p.pieces = pieces_bound(rows, most, S.where.count, p.owned);
-  if (packed_tuned(S.dtype, S.d) && p.pieces * S.kv_heads < 1024) {
+  if (packed_tuned(S.dtype, S.d) && p.pieces * S.kv_heads < packed_dq_places(S.d)) {
     p.owned = 64;
     p.pieces = pieces_bound(rows, most, S.where.count, p.owned);
   }

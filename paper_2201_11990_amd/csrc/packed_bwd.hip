@@ -612,13 +612,15 @@ int bwd_launch(const PackedBwdArgs &w, int owned, int64_t pieces, int64_t key_pi
   int device;
   if (!attr_is_set(attr_done, &device)) {
     MTNLG_TRY(set_lds(packed_dq_kernel<D, 1>, smem));
-    MTNLG_TRY(set_lds(packed_dq_kernel<D, 2>, smem));
+    if constexpr (packed_dq_places(D) > 0) MTNLG_TRY(set_lds(packed_dq_kernel<D, 2>, smem));
     MTNLG_TRY(set_lds(packed_dkv_kernel<D>, Dkv<D>::BYTES));
     attr_mark_set(attr_done, device);
   }
   const unsigned blocks = (unsigned)(pieces * w.kv_heads), key_blocks = (unsigned)(key_pieces * w.splits * w.kv_heads);
-  if (owned == 64) packed_dq_kernel<D, 2><<<blocks, DQ_THREADS, smem, st>>>(w);
-  else packed_dq_kernel<D, 1><<<blocks, DQ_THREADS, smem, st>>>(w);
+  if constexpr (packed_dq_places(D) > 0) {
+    if (owned == 64) packed_dq_kernel<D, 2><<<blocks, DQ_THREADS, smem, st>>>(w);
+  }
+  if (owned == 128) packed_dq_kernel<D, 1><<<blocks, DQ_THREADS, smem, st>>>(w);
   MTNLG_TRY(check_launch());
   packed_dkv_kernel<D><<<key_blocks, Dkv<D>::THREADS, Dkv<D>::BYTES, st>>>(w);
   return check_launch();

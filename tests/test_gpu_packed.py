@@ -421,3 +421,27 @@ def test_two_calls_at_once():
     for c, want in zip(cases, alone):
         for k, v in c.results().items():
             assert torch.equal(v, want[k]), k
+
+
+@pytest.mark.parametrize("d", [64, 72, 128, 152, 192])
+def test_larger_workgroups_of_every_width(d):
+    # 128 rows to a workgroup; then with a token that is infinite, or not a number, and hidden from those before it
+    lengths, at = [300, 900, 1400], 700
+    c = Case(lengths, lengths, 8, 4, d, "bf16", seed=41)
+    want = c.want()
+    c.run()
+    c.check(want)
+    part = lambda t, which: tuple(x[which] for x in t)   # noqa: E731
+    c.k[at], c.v[at] = float("-inf"), float("nan")
+    c.run()
+    for which in (slice(0, at), slice(1200, None)):
+        for name in ("a", "dq"):
+            assert_within(getattr(c, name)[which], part(want[name], which), name)
+    assert not torch.isfinite(c.a[at:1200]).any()
+    c = Case(lengths, lengths, 8, 4, d, "bf16", seed=41)
+    c.q[at], c.da[at] = float("nan"), float("inf")
+    c.run()
+    for name in ("dk", "dv"):
+        for which in (slice(0, 300), slice(at + 1, None)):
+            assert_within(getattr(c, name)[which], part(want[name], which), name)
+        assert not torch.isfinite(getattr(c, name)[300:at + 1]).any()
