@@ -348,7 +348,7 @@ int mtnlg_rotary_bwd(const mtnlg_rotary_desc *desc, const mtnlg_heads *dq_out, c
 typedef struct {
   int32_t dtype;                       /* MTNLG_F32 or MTNLG_BF16                                          */
   int32_t heads, kv_heads, head_dim;   /* heads a multiple of kv_heads; head_dim of 8, <= 256                */
-  int32_t sequences;                   /* <= 2^20                                                          */
+  int32_t sequences;                   /* <= 2^16: a workgroup counts through them to its work                  */
   int32_t max_q, max_k;                /* no sequence has more queries, keys; what lies beyond is unspecified */
   int64_t q_tokens, k_tokens;          /* rows of q, a, da, dq; of k, v, dk, dv; times their heads < 2^31    */
   float scale;                         /* 0 => 1/sqrt(head_dim)                                            */

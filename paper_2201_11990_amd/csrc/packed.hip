@@ -187,7 +187,7 @@ int packed_shape(const mtnlg_packed_desc *D, PackedShape *S) {
   if (D->heads <= 0 || D->kv_heads <= 0 || D->heads % D->kv_heads || D->head_dim <= 0 || D->sequences <= 0) return MTNLG_INVALID_ARG;
   if (D->q_tokens <= 0 || D->k_tokens <= 0 || D->max_q <= 0 || D->max_k <= 0) return MTNLG_INVALID_ARG;
   if (!(D->scale >= 0.0f && D->scale < INFINITY)) return MTNLG_INVALID_ARG;
-  if (D->head_dim % 8 || D->head_dim > 256 || D->heads > 65535 || D->sequences > 1 << 20) return MTNLG_UNSUPPORTED_SHAPE;
+  if (D->head_dim % 8 || D->head_dim > 256 || D->heads > 65535 || D->sequences > 1 << 16) return MTNLG_UNSUPPORTED_SHAPE;
   if (D->q_tokens > 0x7FFFFFFF || D->k_tokens > 0x7FFFFFFF) return MTNLG_UNSUPPORTED_SHAPE;
   if (D->q_tokens * D->heads > 0x7FFFFFFF || D->k_tokens * D->kv_heads > 0x7FFFFFFF) return MTNLG_UNSUPPORTED_SHAPE;   // rows are counted in 32 bits
   *S = PackedShape{D->dtype, D->heads, D->kv_heads, D->heads / D->kv_heads, D->head_dim, D->scale > 0.0f ? D->scale : 1.0f / sqrtf((float)D->head_dim),

@@ -40,7 +40,7 @@ def attention(desc=None, where=None, backward=False, ws=1 << 40, **kw):
 
 
 BAD_DESC = [(dict(dtype=2), INVALID), (dict(heads=0), INVALID), (dict(kv_heads=0), INVALID), (dict(kv_heads=3), INVALID), (dict(head_dim=0), INVALID),
-            (dict(head_dim=60), SHAPE), (dict(head_dim=264), SHAPE), (dict(sequences=0), INVALID), (dict(sequences=(1 << 20) + 1), SHAPE),
+            (dict(head_dim=60), SHAPE), (dict(head_dim=264), SHAPE), (dict(sequences=0), INVALID), (dict(sequences=(1 << 16) + 1), SHAPE),
             (dict(max_q=0), INVALID), (dict(max_k=-1), INVALID), (dict(q_tokens=0), INVALID), (dict(k_tokens=0), INVALID),
             (dict(q_tokens=1 << 31), SHAPE), (dict(k_tokens=1 << 30), SHAPE), (dict(scale=-1.0), INVALID), (dict(scale=float("nan")), INVALID),
             (dict(scale=float("inf")), INVALID)]
