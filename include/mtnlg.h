@@ -296,7 +296,7 @@ int mtnlg_rmsnorm_fwd(int dtype, int64_t T, int64_t h, const void *x, const void
                       void *xsum, void *out, float *rstd, void *stream);
 /* The same with the result in 8 bits: out [T,h] holds e4m3 codes (bias 7, no infinities, 448 the largest) of s * rstd * gamma / scale,
  * rounded to nearest even; scale[t][i] = the largest magnitude of the row's i-th `columns` columns / 448 (the last may be fewer; 1 where
- * all are zeros), float [T][ceil(h / columns)].  columns: a power of two from 8 to 512, or 0: one scale to a row.  A NaN gives the
+ * all are zeros, else 2^-126 at least), float [T][ceil(h / columns)].  columns: a power of two from 8 to 512, or 0: one scale to a row.  A NaN gives the
  * code of NaN.  out 8-byte aligned. */
 int mtnlg_rmsnorm_fwd_e4m3(int dtype, int64_t T, int64_t h, const void *x, const void *residual, const void *gamma, float eps,
                            int32_t columns, void *xsum, void *out, float *scale, float *rstd, void *stream);

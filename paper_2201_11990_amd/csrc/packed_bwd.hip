@@ -7,7 +7,13 @@
 // keys and streams Q and dO of one head of the group after the other.  No atomics: where the keys alone leave units idle, the heads of a group are dealt out over workgroups,
 // whose sums packed.hip adds up in their order.  Keys that no query sees get zeros.
 //
-// P and dS round to bf16 before the products that sum them up (2^-8 of each term at most, as each result once more), D and all sums are fp32.
+// P and dS round to bf16 before the products that sum them up (2^-8 of each term at most, as each result once more), D and all sums are fp32.  D is worked out from the
+// stored a, which is rounded: forward keeps no other.  All in all dq and dk are off by 0.0025 to 0.0031 of their norm, 0.0017 of that by their own rounding.
+//
+// Bound by the matrix pipes, the seven products of which two (S and dP) are taken in both kernels: one kernel for all would add up either dq or dk and dv through atomics, whose
+// order changes results, or through memory (a part of dq to every block of keys).  Four sequences of 384 to 9001 tokens, 32 heads of 128 on 8: dq 1118 us, 1.2 PFLOP/s, pipes
+// busy 72 % of the time; dk / dv 1958 us, 0.9 PFLOP/s, 48 %.  Without its fragments' reads, DMA, exponentials and the exchange the dk / dv loop takes 1332 us, without one of the
+// first two 1790 to 1850, without one of the others 1870 to 1970: nothing of it stands out.  Eight of 77 to 2048, 16 heads on 4: 97 and 165 us; 2501 and 1589 tokens, 16 heads of 160: 97 and 131 us.
 #include "packed.h"
 
 namespace mtnlg {
@@ -267,9 +273,9 @@ __global__ __launch_bounds__(DQ_THREADS, dq_per_unit<D>()) void packed_dq_kernel
 // Eight waves, two to a SIMD, in pairs (roles 0 and 1) of which each owns 32 keys and takes 32 rows of a tile: role 0 forms S and P and accumulates dv,
 // role 1 forms dP and dS and accumulates dk.  P goes to role 1 through LDS in fp32.  The second product runs one tile behind, so that one barrier a tile serves the exchange as well.
 // D up to 128: a workgroup owns 64 keys and takes tiles of 64 rows; the two pairs of a group of keys take one half each and are merged through LDS at the end.
-// Wider ones: 128 keys and tiles of 32 rows (64 x 192 do not fit three times).  Both ways, median us, 64 / 128 keys: 16 sequences of 134 to 2048 tokens,
-// 16 heads of 128: 186 / 180 and 15 for the join of its tiles' parts, which 64 keys do without; 8192 tokens, 32 heads of 128 (4 of keys): 1970 / 2051;
-// 13 sequences of 512 tokens and fewer, 8 heads of 64: 13 / 17; 8 sequences, 12 heads of 160: 139 / 133.
+// Wider ones: 128 keys and tiles of 32 rows (64 x 192 do not fit three times).  Both ways, median us, 64 / 128 keys: eight sequences of 77 to 2048 tokens, 16 heads of 128 on 4:
+// 186 / 180 and 15 for the join of its tiles' parts, which 64 keys do without; four of 384 to 9001, 32 heads of 128 on 8: 1970 / 2051; 17, 64 and 130 tokens, 4 heads of
+// 64 on 2: 13 / 17; 2501 and 1589 tokens, 16 heads of 160: 139 / 133.
 template <int D> struct Dkv {
   static constexpr int OWNED = D <= 128 ? 64 : 128, PARTS = 128 / OWNED, PAIRS = 4, THREADS = 128 * PAIRS;
   static constexpr int ROWS = 32 * PARTS, GROUPS = OWNED / 32;

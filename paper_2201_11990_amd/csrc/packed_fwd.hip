@@ -7,6 +7,13 @@
 // them, and a single token's heads fill one block.  K and V stream through LDS past the own rows in tiles of 64; the products are those of attention_mfma.hip (the
 // streamed tile as A operand, 32 own rows to a wave as B, P from one product to the next in registers, fragments read a few steps ahead across the end of a tile).
 // Calls of few rows cut the keys into chunks, whose results packed.hip joins.
+//
+// P rounds to bf16 before its product (2^-8 of each term at most, as the result once more); scores, maxima, sums and results are fp32.
+//
+// Bound by the matrix and vector pipes alike: 64 keys and 128 rows of 128 are 32 MFMAs and 204 vector instructions to a wave, 34 of them exponentials at a quarter of
+// the rate.  Four sequences of 384 to 9001 tokens, 32 heads of 128 on 8: 897 us, 1.0 PFLOP/s of what is not masked, matrix pipes busy 55 % of the time (a large product of the
+// library reaches 1.2 PFLOP/s on this card); eight of 77 to 2048, 16 heads on 4: 77 us, 0.63 PFLOP/s, 37 %, since pieces are short; 2501 and 1589 tokens, 16 heads of 160: 71 us.
+// Single tokens read K and V once: 32 of them over 64 to 15872 keys, 425 MB in 88 us, 4.8 TB/s, and 8 us for the join.
 #include "packed.h"
 
 namespace mtnlg {

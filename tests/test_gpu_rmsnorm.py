@@ -11,7 +11,7 @@ pytestmark = pytest.mark.gpu
 DT = {"bf16": torch.bfloat16, "fp32": torch.float32}
 HALF_STEP = {"bf16": 2.0 ** -8, "fp32": 2.0 ** -24}
 F, EPS = 2.0 ** -23, 1e-5
-SIZES = [(1, 8), (3, 64), (5, 520), (61, 1032), (9, 2048), (7, 2056), (130, 4096), (5, 8200), (6, 16392), (3, 20480), (2, 24584), (2, 32768)]
+SIZES = [(1, 8), (3, 64), (5, 520), (61, 1032), (9, 2048), (7, 2056), (130, 4096), (301, 1024), (37, 4104), (600, 8192), (5, 8200), (6, 16392), (3, 20480), (2, 24584), (2, 32768)]
 
 
 def inputs(T, h, dtype, seed=0):
@@ -128,6 +128,19 @@ def test_rows_of_zeros_infinities_and_nan():
     codes, scale = torch.empty((5, 64), dtype=torch.float8_e4m3fn, device="cuda"), torch.empty((5, 1), device="cuda")
     M.mtnlg_rmsnorm_fwd_e4m3(x, gamma, EPS, codes, scale, rstd)
     assert (codes[1].float() == 0).all() and scale[1] == 1 and torch.isnan(codes[2].float()).all()
+
+
+@pytest.mark.parametrize("columns", [0, 32])
+def test_eight_bits_of_results_too_small_for_their_scale(columns):
+    # magnitudes / 448 below 2^-126: that is the scale then.  (F: half a step of the smallest fp32 numbers, 2^-150, many times over)
+    x = torch.randn((6, 64), generator=torch.Generator(device="cuda").manual_seed(4), device="cuda")
+    x[:, 40] = 0
+    gamma = torch.full((64,), 2.0 ** -120, device="cuda")
+    codes, scale, rstd = torch.empty((6, 64), dtype=torch.float8_e4m3fn, device="cuda"), torch.empty((6, 2 if columns else 1), device="cuda"), torch.empty(6, device="cuda")
+    M.mtnlg_rmsnorm_fwd_e4m3(x, gamma, EPS, codes, scale, rstd, columns=columns)
+    assert (scale == 2.0 ** -126).all()
+    code = norm64(x, gamma)[1] * 2.0 ** 126
+    within(codes, code, torch.maximum(2.0 ** -4 * code.abs(), torch.full_like(code, 2.0 ** -10)) + 50 * F * code.abs() + F, "codes")
 
 
 def test_runs_are_identical_and_replays_too():
