@@ -211,7 +211,7 @@ __global__ __launch_bounds__(64 * WAVES, per_unit<D>()) void packed_fwd_kernel(P
   // 32-key parts with a key that a row of the wave sees, and of those the first ones, which all rows see whole: a loop without masks for them, which has fewer values
   // to keep.  The parts after them are passed over.
   auto parts_of = [&](int keys) { return SPLIT == 2 ? (keys / 32 + 1 - part) / 2 : keys / 32; };
-  const int visible = parts_of(most - begin + 32), whole = parts_of(min(least, most) - begin + 1) / SUBS;
+  const int visible = max(0, parts_of(most - begin + 32)), whole = parts_of(min(least, most) - begin + 1) / SUBS;
   int it = 0;
   for (; it < whole; ++it) tile(std::integral_constant<int, SUBS>{}, std::false_type{}, it);
   for (; it < visible / SUBS; ++it) tile(std::integral_constant<int, SUBS>{}, std::true_type{}, it);

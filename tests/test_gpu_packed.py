@@ -445,3 +445,13 @@ def test_larger_workgroups_of_every_width(d):
         for which in (slice(0, 300), slice(at + 1, None)):
             assert_within(getattr(c, name)[which], part(want[name], which), name)
         assert not torch.isfinite(getattr(c, name)[300:at + 1]).any()
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 192), ("fp32", 64)])
+@pytest.mark.parametrize("keys", [3, 70])
+def test_many_queries_that_see_no_key(dtype, d, keys):
+    # all rows of some workgroups and of some waves; 128 rows to a workgroup
+    c = Case([400, 5], [keys, 5], 170, 1, d, dtype, seed=51)
+    c.run()
+    c.check()
+    assert torch.isneginf(c.lse[:, :400 - keys]).all() and (c.a[:400 - keys] == 0).all() and (c.dq[:400 - keys] == 0).all()
