@@ -11,7 +11,7 @@
 // stored a, which is rounded: forward keeps no other.  All in all dq and dk are off by 0.0025 to 0.0031 of their norm, 0.0017 of that by their own rounding.
 //
 // Bound by the matrix pipes, the seven products of which two (S and dP) are taken in both kernels: one kernel for all would add up either dq or dk and dv through atomics, whose
-// order changes results, or through memory (a part of dq to every block of keys).  Four sequences of 384 to 9001 tokens, 32 heads of 128 on 8: dq 1118 us, 1.2 PFLOP/s, pipes
+// order changes results, or through memory (a part of dq to every block of keys).  Four sequences of 384 to 9001 tokens, 32 heads of 128 on 8: dq 1120 us, 1.2 PFLOP/s, pipes
 // busy 72 % of the time; dk / dv 1958 us, 0.9 PFLOP/s, 48 %.  Without its fragments' reads, DMA, exponentials and the exchange the dk / dv loop takes 1332 us, without one of the
 // first two 1790 to 1850, without one of the others 1870 to 1970: nothing of it stands out.  Eight of 77 to 2048, 16 heads on 4: 97 and 165 us; 2501 and 1589 tokens, 16 heads of 160: 97 and 131 us.
 #include "packed.h"
@@ -51,6 +51,8 @@ __global__ __launch_bounds__(DQ_THREADS, dq_per_unit<D>()) void packed_dq_kernel
   const int least = __builtin_amdgcn_readfirstlane(limit), most = own0 < rows ? __builtin_amdgcn_readlane(limit, 31) : -1;
   const float f = w.scale * kLog2e;
   typename P::Lane ln(lane);
+  ln.n0 += part * T::ROWS32;
+  ln.t0 += part * T::ROWS32;
   const uint32_t smem_addr = lds_address(smem);
 
   constexpr int IPW = 2 * T::NI;
@@ -112,25 +114,25 @@ __global__ __launch_bounds__(DQ_THREADS, dq_per_unit<D>()) void packed_dq_kernel
   bf16x8 fr[NF];
   f32x16 sc, pc;   // pc accumulates dP - D
   bf16x8 x[2];
-  const char *Kt = smem;   // stage of the tile whose fragments are being read
-  auto load = [&](int i) {   // the fragment of step i
+  auto load = [&](int i, const char *Kt) {   // the fragment of step i, of the tile in stage Kt
     const int sub = i / N1, r = i % N1;
-    const char *k = Kt + (part + sub) * T::ROWS32;
+    const char *k = Kt + sub * T::ROWS32;
     bf16x8 &v = fr[i % NF];
     if (r < K1) v = T::nat32(k, ln, r);
     else if (r < 2 * K1) v = T::nat32(k + T::BYTES, ln, r - K1);
     else v = T::tr32(k, ln, (r - 2 * K1) / 2, r % 2);
   };
 #pragma unroll
-  for (int i = 0; i < PF; ++i) load(i);
+  for (int i = 0; i < PF; ++i) load(i, smem);
   __builtin_amdgcn_sched_barrier(0);
 
   int cur = 0;
-  auto tile = [&](auto TAKEN, auto MASKED, int it) __attribute__((always_inline)) {   // TAKEN: parts, SUBS or the first only
+  auto tile = [&](auto TAKEN, auto MASKED, auto STAGE_OF, int it) __attribute__((always_inline)) {   // TAKEN: parts, SUBS or the first only; STAGE_OF: -1 as it comes
     constexpr int N = decltype(TAKEN)::value * N1;
-    ln.here();
-    const int next = cur ^ 1;
-    const char *const K = smem + cur * STAGE;
+    constexpr int FIXED = decltype(STAGE_OF)::value;
+    if constexpr (FIXED < 0) ln.here();
+    const int now = FIXED < 0 ? cur : FIXED, next = now ^ 1;   // stages of tiles it, it + 1
+    const char *const K = smem + now * STAGE;
     auto step = [&](auto I) __attribute__((always_inline)) {
       constexpr int i = decltype(I)::value, sub = i / N1, r = i % N1;
       const int key0 = it * 64 + 32 * (part + sub);
@@ -153,16 +155,13 @@ __global__ __launch_bounds__(DQ_THREADS, dq_per_unit<D>()) void packed_dq_kernel
 #pragma unroll
           for (int e = 0; e < 16; ++e)
             if (8 * (e / 4) + e % 4 > seen) pc[e] = 0.0f;
-          redo |= rows_not_finite<bf16, D>(K + (part + sub) * T::ROWS32, ln);
+          redo |= rows_not_finite<bf16, D>(K + sub * T::ROWS32, ln);
         }
         x[0] = P::weights(pc, 0);
         x[1] = P::weights(pc, 1);
       }
-      if (i == N - PF) {   // all of tile `it` has been read; tile it + 1 landed everywhere
-        wait_and_barrier<0>();
-        Kt = smem + next * STAGE;
-      }
-      load((i + PF) % N);
+      if (i == N - PF) wait_and_barrier<0>();   // all of tile `it` has been read; tile it + 1 landed everywhere
+      load((i + PF) % N, smem + (i + PF < N ? now : next) * STAGE);
       if (i < ISSUE_STEPS) issue_step(i, next);
       const bf16x8 &v = fr[i % NF];
       if constexpr (r < K1) sc = MFMA32(v, of0[r], sc);
@@ -179,10 +178,17 @@ __global__ __launch_bounds__(DQ_THREADS, dq_per_unit<D>()) void packed_dq_kernel
   auto parts_of = [&](int keys) { return SPLIT == 2 ? (keys / 32 + 1 - part) / 2 : keys / 32; };
   const int visible = max(0, parts_of(most + 32)), whole = parts_of(min(least, most) + 1) / SUBS;
   int it = 0;
-  for (; it < whole; ++it) tile(std::integral_constant<int, SUBS>{}, std::false_type{}, it);
-  for (; it < visible / SUBS; ++it) tile(std::integral_constant<int, SUBS>{}, std::true_type{}, it);
+  using Any = std::integral_constant<int, -1>;
+  if constexpr (D <= 128) {   // in pairs, with the stages known (packed_fwd.hip): 1145 us, 1120 so; wider heads have no registers for it (heads of 160: 97 us, 112 so)
+    for (; it + 1 < whole; it += 2) {
+      tile(std::integral_constant<int, SUBS>{}, std::false_type{}, std::integral_constant<int, 0>{}, it);
+      tile(std::integral_constant<int, SUBS>{}, std::false_type{}, std::integral_constant<int, 1>{}, it + 1);
+    }
+  }
+  for (; it < whole; ++it) tile(std::integral_constant<int, SUBS>{}, std::false_type{}, Any{}, it);
+  for (; it < visible / SUBS; ++it) tile(std::integral_constant<int, SUBS>{}, std::true_type{}, Any{}, it);
   if constexpr (SUBS == 2) {
-    if (visible % 2) tile(std::integral_constant<int, 1>{}, std::true_type{}, it++);
+    if (visible % 2) tile(std::integral_constant<int, 1>{}, std::true_type{}, Any{}, it++);
   }
   for (; it < ntiles; ++it) {   // passed over: its share of a later tile, and the barrier
 #pragma unroll

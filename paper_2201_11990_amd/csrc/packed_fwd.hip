@@ -10,9 +10,9 @@
 //
 // P rounds to bf16 before its product (2^-8 of each term at most, as the result once more); scores, maxima, sums and results are fp32.
 //
-// Bound by the matrix and vector pipes alike: 64 keys and 128 rows of 128 are 32 MFMAs and 204 vector instructions to a wave, 34 of them exponentials at a quarter of
-// the rate.  Four sequences of 384 to 9001 tokens, 32 heads of 128 on 8: 897 us, 1.0 PFLOP/s of what is not masked, matrix pipes busy 55 % of the time (a large product of the
-// library reaches 1.2 PFLOP/s on this card); eight of 77 to 2048, 16 heads on 4: 77 us, 0.63 PFLOP/s, 37 %, since pieces are short; 2501 and 1589 tokens, 16 heads of 160: 71 us.
+// Bound by the matrix and vector pipes alike: 64 keys and 128 rows of 128 are 32 MFMAs and 168 vector instructions to a wave, 34 of them exponentials at a quarter of
+// the rate.  Four sequences of 384 to 9001 tokens, 32 heads of 128 on 8: 869 us, 1.04 PFLOP/s of what is not masked, matrix pipes busy 57 % of the time (a large product of the
+// library reaches 1.2 PFLOP/s on this card); eight of 77 to 2048, 16 heads on 4: 73 us, 0.67 PFLOP/s, 39 %, since pieces are short; 2501 and 1589 tokens, 16 heads of 160: 71 us.
 // Single tokens read K and V once: 32 of them over 64 to 15872 keys, 425 MB in 88 us, 4.8 TB/s, and 8 us for the join.
 #include "packed.h"
 
@@ -99,6 +99,8 @@ __global__ __launch_bounds__(64 * WAVES, per_unit<D>()) void packed_fwd_kernel(P
   const int least = __builtin_amdgcn_readfirstlane(limit), most = own0 < rows ? __builtin_amdgcn_readlane(limit, 31) : begin - 1;
   const float c = w.scale * kLog2e;
   typename P::Lane ln(lane);
+  ln.n0 += part * T::ROWS32;
+  ln.t0 += part * T::ROWS32;
   const uint32_t smem_addr = lds_address(smem);
 
   // waves 0, 1 bring 32 rows each of K, waves 2, 3 of V
@@ -138,23 +140,23 @@ __global__ __launch_bounds__(64 * WAVES, per_unit<D>()) void packed_fwd_kernel(P
   bf16x8 fr[NF];
   f32x16 sc;
   bf16x8 x[2];
-  const char *Kt = smem;   // stage of the tile whose fragments are being read
-  auto load = [&](int i) {   // the fragment of step i
+  auto load = [&](int i, const char *Kt) {   // the fragment of step i, of the tile in stage Kt
     const int sub = i / N1, r = i % N1;
-    const char *k = Kt + (part + sub) * T::ROWS32;
+    const char *k = Kt + sub * T::ROWS32;
     if (r < K1) fr[i % NF] = T::nat32(k, ln, r);
     else fr[i % NF] = T::tr32(k + T::BYTES, ln, (r - K1) / 2, r % 2);
   };
 #pragma unroll
-  for (int i = 0; i < PF; ++i) load(i);
+  for (int i = 0; i < PF; ++i) load(i, smem);
   __builtin_amdgcn_sched_barrier(0);
 
   int cur = 0;
-  auto tile = [&](auto TAKEN, auto MASKED, int it) __attribute__((always_inline)) {   // TAKEN: parts, SUBS or the first only
+  auto tile = [&](auto TAKEN, auto MASKED, auto STAGE_OF, int it) __attribute__((always_inline)) {   // TAKEN: parts, SUBS or the first only; STAGE_OF: -1 as it comes
     constexpr int N = decltype(TAKEN)::value * N1;
-    ln.here();
-    const int next = cur ^ 1;   // stage of tile it + 1
-    const char *const V = smem + cur * STAGE + T::BYTES;
+    constexpr int FIXED = decltype(STAGE_OF)::value;
+    if constexpr (FIXED < 0) ln.here();
+    const int now = FIXED < 0 ? cur : FIXED, next = now ^ 1;   // stages of tiles it, it + 1
+    const char *const V = smem + now * STAGE + T::BYTES;
     auto step = [&](auto I) __attribute__((always_inline)) {
       constexpr int i = decltype(I)::value, sub = i / N1, r = i % N1;
       const int key0 = begin + it * 64 + 32 * (part + sub);
@@ -166,7 +168,7 @@ __global__ __launch_bounds__(64 * WAVES, per_unit<D>()) void packed_fwd_kernel(P
 #pragma unroll
           for (int e = 0; e < 16; ++e)
             if (8 * (e / 4) + e % 4 > seen) sc[e] = -INFINITY;
-          redo |= rows_not_finite<bf16, D>(V + (part + sub) * T::ROWS32, ln);
+          redo |= rows_not_finite<bf16, D>(V + sub * T::ROWS32, ln);
         }
         // m: the running maximum of the raw scores; it follows when the row maximum has outgrown it by more than 2^8 in the exponent's units (any reference gives the
         // same sums; this one keeps p <= 256 and makes rescaling O rare), and in the first tile, where a weight of 1, which does not round, is the largest.
@@ -193,11 +195,8 @@ __global__ __launch_bounds__(64 * WAVES, per_unit<D>()) void packed_fwd_kernel(P
         x[0] = P::weights(sc, 0);
         x[1] = P::weights(sc, 1);
       }
-      if (i == N - PF) {   // all of tile `it` has been read; tile it + 1 landed everywhere
-        wait_and_barrier<0>();
-        Kt = smem + next * STAGE;
-      }
-      load((i + PF) % N);
+      if (i == N - PF) wait_and_barrier<0>();   // all of tile `it` has been read; tile it + 1 landed everywhere
+      load((i + PF) % N, smem + (i + PF < N ? now : next) * STAGE);
       if (i < ISSUE_STEPS) issue_step(i, next);
       const bf16x8 &v = fr[i % NF];
       if constexpr (r < K1) sc = MFMA32(v, qf[r], sc);
@@ -213,10 +212,19 @@ __global__ __launch_bounds__(64 * WAVES, per_unit<D>()) void packed_fwd_kernel(P
   auto parts_of = [&](int keys) { return SPLIT == 2 ? (keys / 32 + 1 - part) / 2 : keys / 32; };
   const int visible = max(0, parts_of(most - begin + 32)), whole = parts_of(min(least, most) - begin + 1) / SUBS;
   int it = 0;
-  for (; it < whole; ++it) tile(std::integral_constant<int, SUBS>{}, std::false_type{}, it);
-  for (; it < visible / SUBS; ++it) tile(std::integral_constant<int, SUBS>{}, std::true_type{}, it);
+  using Any = std::integral_constant<int, -1>;
+  // In pairs, with the stages known: fragments' addresses are registers and constants, 17 % fewer vector instructions (four sequences of 384 to 9001 tokens, 32 heads of 128 on 8: 905 us
+  // tile by tile, 869 so).  Not where 128 rows of 96 would need 187 registers then, not 168, and two workgroups share a unit in place of three (2501 and 1589 tokens, 32 heads: 77 us, 79 so).
+  if constexpr (D != 96 || SPLIT == 2) {
+    for (; it + 1 < whole; it += 2) {
+      tile(std::integral_constant<int, SUBS>{}, std::false_type{}, std::integral_constant<int, 0>{}, it);
+      tile(std::integral_constant<int, SUBS>{}, std::false_type{}, std::integral_constant<int, 1>{}, it + 1);
+    }
+  }
+  for (; it < whole; ++it) tile(std::integral_constant<int, SUBS>{}, std::false_type{}, Any{}, it);
+  for (; it < visible / SUBS; ++it) tile(std::integral_constant<int, SUBS>{}, std::true_type{}, Any{}, it);
   if constexpr (SUBS == 2) {
-    if (visible % 2) tile(std::integral_constant<int, 1>{}, std::true_type{}, it++);
+    if (visible % 2) tile(std::integral_constant<int, 1>{}, std::true_type{}, Any{}, it++);
   }
   for (; it < ntiles; ++it) {   // passed over: its share of the next tile, and the barrier
 #pragma unroll
