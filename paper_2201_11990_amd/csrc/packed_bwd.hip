@@ -12,8 +12,8 @@
 //
 // Bound by the matrix pipes, the seven products of which two (S and dP) are taken in both kernels: one kernel for all would add up either dq or dk and dv through atomics, whose
 // order changes results, or through memory (a part of dq to every block of keys).  Four sequences of 384 to 9001 tokens, 32 heads of 128 on 8: dq 1120 us, 1.2 PFLOP/s, pipes
-// busy 72 % of the time; dk / dv 1958 us, 0.9 PFLOP/s, 48 %.  Without its fragments' reads, DMA, exponentials and the exchange the dk / dv loop takes 1332 us, without one of the
-// first two 1790 to 1850, without one of the others 1870 to 1970: nothing of it stands out.  Eight of 77 to 2048, 16 heads on 4: 97 and 165 us; 2501 and 1589 tokens, 16 heads of 160: 97 and 131 us.
+// busy 72 % of the time; dk / dv 1890 us, 0.95 PFLOP/s, 50 %.  Without its fragments' reads, DMA, exponentials and the exchange that loop took 1332 us of 2020, without one of the
+// first two 1790 to 1850, without one of the others 1870 to 1970: nothing of it stands out.  Eight of 77 to 2048, 16 heads on 4: 96 and 160 us; 2501 and 1589 tokens, 16 heads of 160: 97 and 128 us.
 #include "packed.h"
 
 namespace mtnlg {
@@ -380,12 +380,11 @@ __global__ __launch_bounds__(Dkv<D>::THREADS) void packed_dkv_kernel(PackedBwdAr
   f32x4 *const xchg = reinterpret_cast<f32x4 *>(smem + RING * STAGE) + wave % PAIRS * 256 + lane;   // 4 x 64 of the pair
   auto run = [&](auto ROLE) __attribute__((always_inline)) {
     constexpr int me = decltype(ROLE)::value;
-    const int part_rows = part * T::ROWS32;
+    ln.n0 += part * T::ROWS32;
+    ln.t0 += part * T::ROWS32;
     constexpr int FIRST_AT = me ? L::MATRIX : 0, SECOND_AT = me ? 0 : L::MATRIX;   // S from Q, then dv from dO; dP from dO, then dk from Q
-    const char *now = smem, *before = smem;   // stages of the tile whose first product, and whose second, are next to be read
-    int cur = 0, odd = 0;
-    auto next_of = [](int cur) { return cur == RING - 1 ? 0 : cur + 1; };   // stages of tiles it + 1
-    auto ahead_of = [&](int cur) { return cur + AHEAD >= RING ? cur + AHEAD - RING : cur + AHEAD; };   // and it + AHEAD
+    int cur = 0, last = 0, odd = 0;   // stages of the tile and of the one before (of the first: its own); P's buffer
+    auto after = [](int cur, int n) { return cur + n >= RING ? cur + n - RING : cur + n; };   // stage of tile it + n
     bf16x8 fr[NF];
     f32x16 sc, prev = {};   // S and P (role 0); dP - D of this tile and of the one before
     bf16x8 x[2], xn[2];     // the second product's operand: what is in use, and (role 0) the next
@@ -393,9 +392,9 @@ __global__ __launch_bounds__(Dkv<D>::THREADS) void packed_dkv_kernel(PackedBwdAr
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[t][e] = (bf16)0.0f;
-    auto load = [&](int r) {   // the fragment of step r
-      if (r < K1) fr[r % NF] = T::nat32(now + FIRST_AT + part_rows, ln, r);
-      else fr[r % NF] = T::tr32(before + SECOND_AT + part_rows, ln, (r - K1) / 2, r % 2);
+    auto load = [&](int r, const char *t) {   // the fragment of step r, from stage t
+      if (r < K1) fr[r % NF] = T::nat32(t + FIRST_AT, ln, r);
+      else fr[r % NF] = T::tr32(t + SECOND_AT, ln, (r - K1) / 2, r % 2);
     };
     auto take = [&](int buffer, f32x16 &p) {
 #pragma unroll
@@ -411,9 +410,9 @@ __global__ __launch_bounds__(Dkv<D>::THREADS) void packed_dkv_kernel(PackedBwdAr
       for (int q = 0; q < 4; ++q) xchg[(odd ^ 1) * (L::XCHG / 16) + q * 64] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     }
     wait_and_barrier<(AHEAD - 1) * OPS>();   // tile 0 landed everywhere
-    redo |= rows_not_finite<bf16, D>(smem + SECOND_AT + part_rows, ln);   // whose rows those zeros meet
+    redo |= rows_not_finite<bf16, D>(smem + SECOND_AT, ln);   // whose rows those zeros meet
 #pragma unroll
-    for (int i = 0; i < PF; ++i) load(i);
+    for (int i = 0; i < PF; ++i) load(i, smem);
     __builtin_amdgcn_sched_barrier(0);
     int row = first + t0 * ROWS + 32 * part, left = tiles - t0;   // the tile's first query (of this part), tiles of the head from it on
     int row_before = row;                        // ... of the tile before
@@ -428,10 +427,12 @@ __global__ __launch_bounds__(Dkv<D>::THREADS) void packed_dkv_kernel(PackedBwdAr
       }
     };
     auto masked = [&](int row) { return row + shift < own0 + 31 || row + 32 > s.lq; };   // wave-uniform
-    for (int it = 0; it < n; ++it) {
-      ln.here();
-      const int next = next_of(cur), nn = ahead_of(cur);
-      const float *stat = reinterpret_cast<const float *>(smem + cur * STAGE + 2 * L::MATRIX) + 32 * part + 4 * h;
+    auto tile = [&](auto STAGE_OF) __attribute__((always_inline)) {   // STAGE_OF: -1 as it comes
+      constexpr int FIXED = decltype(STAGE_OF)::value;
+      if constexpr (FIXED < 0) ln.here();
+      const int at = FIXED < 0 ? cur : FIXED, next = after(at, 1), nn = after(at, AHEAD);
+      const char *const now = smem + at * STAGE, *const before = smem + (FIXED < 0 ? last : after(at, RING - 1)) * STAGE;
+      const float *stat = reinterpret_cast<const float *>(now + 2 * L::MATRIX) + 32 * part + 4 * h;
       f32x16 ls, p;
       if constexpr (me == 0) {
 #pragma unroll
@@ -461,7 +462,7 @@ __global__ __launch_bounds__(Dkv<D>::THREADS) void packed_dkv_kernel(PackedBwdAr
           if (r == HAND_OVER) {
             if (masked(row)) {
               hide(row, sc);
-              redo |= rows_not_finite<bf16, D>(now + SECOND_AT + part_rows, ln);
+              redo |= rows_not_finite<bf16, D>(now + SECOND_AT, ln);
             }
 #pragma unroll
             for (int t = 0; t < 2; ++t) xn[t] = P::weights(sc, t);
@@ -476,18 +477,14 @@ __global__ __launch_bounds__(Dkv<D>::THREADS) void packed_dkv_kernel(PackedBwdAr
           if (r == K1) {
             if (masked(row_before)) {   // (before the first tile there is none: this looks at the first)
               hide(row_before, prev);
-              redo |= rows_not_finite<bf16, D>(before + SECOND_AT + part_rows, ln);
+              redo |= rows_not_finite<bf16, D>(before + SECOND_AT, ln);
             }
 #pragma unroll
             for (int t = 0; t < 2; ++t) x[t] = P::weights(prev, t);
           }
         }
-        if (r == N - PF) {   // all that this iteration reads has been read, and all it hands over is written; tile it + 1 landed everywhere
-          wait_and_barrier<(AHEAD - 1) * OPS>();
-          before = now;
-          now = smem + next * STAGE;
-        }
-        load((r + PF) % N);
+        if (r == N - PF) wait_and_barrier<(AHEAD - 1) * OPS>();   // all that this iteration reads has been read, and all it hands over is written; tile it + 1 landed everywhere
+        load((r + PF) % N, r + PF >= N ? smem + next * STAGE : r + PF < K1 ? now : before);
         if (r < ISSUE_STEPS) issue_step(r, nn);
         const bf16x8 &v = fr[r % NF];
         if constexpr (r < K1) sc = MFMA32(v, of[r], sc);
@@ -508,10 +505,21 @@ __global__ __launch_bounds__(Dkv<D>::THREADS) void packed_dkv_kernel(PackedBwdAr
         left = tiles;
         row = first + 32 * part;
       }
+      last = at;
       cur = next;
       odd ^= 1;
+    };
+    using Any = std::integral_constant<int, -1>;
+    int it = 1;
+    tile(Any{});
+    // a round of the ring at a time, with the stages known (packed_fwd.hip): four sequences of 384 to 9001 tokens, 32 heads of 128 on 8, 2030 us one by one, 1910 so; heads of 160: 133 and
+    // 129.  Heads of 192 have no registers for it (505 us, 680 so).
+    if constexpr (D <= 160) {
+      for (; it + RING <= n; it += RING) for_each_step([&](auto I) __attribute__((always_inline)) { tile(std::integral_constant<int, (decltype(I)::value + 1) % RING>{}); }, std::make_integer_sequence<int, RING>{});
     }
+    for (; it < n; ++it) tile(Any{});
     // the second product of the last tile
+    const char *const before = smem + last * STAGE;
     if constexpr (me == 1) {
       f32x16 p;
       take(odd ^ 1, p);
@@ -519,13 +527,13 @@ __global__ __launch_bounds__(Dkv<D>::THREADS) void packed_dkv_kernel(PackedBwdAr
       for (int e = 0; e < 16; ++e) prev[e] *= p[e];
       if (masked(row_before)) {
         hide(row_before, prev);
-        redo |= rows_not_finite<bf16, D>(before + SECOND_AT + part_rows, ln);
+        redo |= rows_not_finite<bf16, D>(before + SECOND_AT, ln);
       }
 #pragma unroll
       for (int t = 0; t < 2; ++t) x[t] = P::weights(prev, t);
     }
     bf16x8 v[4];
-    pipelined<K1, 3>([&](int i) { v[i & 3] = T::tr32(before + SECOND_AT + part_rows, ln, i / 2, i % 2); },
+    pipelined<K1, 3>([&](int i) { v[i & 3] = T::tr32(before + SECOND_AT, ln, i / 2, i % 2); },
                      [&](int i) { acc[i / 2] = MFMA32(v[i & 3], x[i % 2], acc[i / 2]); }, [](int) {});
   };
   if (n > 0) {
