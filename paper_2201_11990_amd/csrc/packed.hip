@@ -95,32 +95,37 @@ struct FwdPlan {
   int chunk, chunks;
   size_t part_bytes, bytes;
 };
-// Estimated microseconds with and without: a workgroup takes about 0.9 us a tile of 64 keys where two share a unit (fp32 by its matrix instructions), 3.5 us to start, and
-// a cut call 8 us and the way of its parts through memory (at 4 TB/s) to join them.  Cut where that is
-// half as much again faster, into about 1024 pieces.  Measured: 32 single tokens, 64 to 15872 keys, 32 heads of 128 on 8: 280 us whole, 96 cut (104 into 512 pieces, 112 into
-// 2048); 973 tokens behind up to 4608 keys, 62 us whole, 89 and 101 in chunks of 2304 and 1024.
-constexpr int CUT_LEAST = 256, SLOTS = 512;   // keys of a chunk at least; workgroups at once
 struct Cut {
   int chunk, chunks;
 };
-Cut cut_keys(const PackedShape &S, int64_t pieces, double tile, int least, int into) {   // tile: us of 64 keys
-  const double wide = (double)(pieces * S.kv_heads), mean = (double)S.where.k_tokens / S.where.count;
-  if (S.max_k < 2 * least || wide >= 2 * SLOTS) return Cut{0, 1};
-  const double work = wide * mean / 64 / SLOTS;   // tiles of a slot where all come out even
-  const int want = (int)fmax(least, fmax(S.max_k / 64.0, wide * mean / into));   // (64: a lane of the joining wave to each)
-  const int chunk = (want + 63) / 64 * 64;
-  const double each = fmax(1.0, mean / chunk);   // chunks of a sequence
-  const double whole = tile * fmax(S.max_k / 64.0, work);
-  const double cut = tile * fmax(chunk / 64.0, work) + 3.5 * wide * each / SLOTS + 8.0 + (double)S.where.q_tokens * S.heads * each * S.d * 8.0 / 4.0e6;
-  if (chunk >= S.max_k || 1.5 * cut >= whole) return Cut{0, 1};
-  return Cut{chunk, (S.max_k + chunk - 1) / chunk};
-}
 // all pieces with their chunks: all keys in chunks and the last ones of each sequence, for every block that a sequence can have
 int64_t cut_pieces(const PackedShape &S, const Cut &c, int64_t pieces, int owned) {
   if (c.chunks == 1) return pieces;
   const int64_t blocks_of = ((int64_t)S.max_q * S.group + owned - 1) / owned, by_keys = blocks_of * (S.where.k_tokens / c.chunk + S.where.count);
   return pieces * c.chunks < by_keys ? pieces * c.chunks : by_keys;
 }
+// Estimated microseconds with and without: a workgroup takes `tile` us for 64 keys where all `slots` for workgroups are in use, 3.5 us to start (3 to find that there is
+// nothing for it), and a cut call 8 us and the way of its parts through memory (at 4 TB/s) to join them.  Cut where that is
+// half as much again faster, into about 1024 pieces.  Measured: 32 single tokens, 64 to 15872 keys, 32 heads of 128 on 8: 280 us whole, 96 cut (104 into 512 pieces, 112 into
+// 2048); 973 tokens behind up to 4608 keys, 60 us whole, 89 and 102 in chunks of 2304 and 1152; heads of 256: 806 and 110 tokens behind up to 1899 keys, 12 on 4, 172 us whole and 121
+// cut, 16 sequences of up to 968 tokens and 2058 keys, 16 on 8, 209 and 350 (most of 5120 workgroups find nothing).
+constexpr int CUT_LEAST = 256;   // keys of a chunk at least
+Cut cut_keys(const PackedShape &S, int64_t pieces, int owned, double tile, int slots, int least, int into) {
+  const double wide = (double)(pieces * S.kv_heads), mean = (double)S.where.k_tokens / S.where.count;
+  if (S.max_k < 2 * least || wide >= 1024) return Cut{0, 1};
+  const double work = wide * mean / 64 / slots;   // tiles of a slot where all come out even
+  const int want = (int)fmax(least, fmax(S.max_k / 64.0, wide * mean / into));   // (64: a lane of the joining wave to each)
+  const int chunk = (want + 63) / 64 * 64;
+  const Cut c{chunk, (S.max_k + chunk - 1) / chunk};
+  const double each = fmax(1.0, mean / chunk);   // chunks of a sequence
+  const double idle = fmax(0.0, (double)(cut_pieces(S, c, pieces, owned) * S.kv_heads) - wide * each);
+  const double whole = tile * fmax(S.max_k / 64.0, work);
+  const double cut = tile * fmax(chunk / 64.0, work) + (3.5 * wide * each + 3.0 * idle) / slots + 8.0 + (double)S.where.q_tokens * S.heads * each * S.d * 8.0 / 4.0e6;
+  return chunk >= S.max_k || 1.5 * cut >= whole ? Cut{0, 1} : c;
+}
+// us of 64 keys of the forward kernels, and how many of their workgroups run at once
+double fwd_tile(const PackedShape &S) { return S.dtype == MTNLG_F32 ? (S.d <= 160 ? 0.11 : 0.07) * S.d : S.d > PACKED_TUNED ? 5.0 : 0.9; }
+int fwd_slots(const PackedShape &S) { return S.d <= 160 ? 512 : 256; }
 FwdPlan fwd_plan(const PackedShape &S) {
   FwdPlan p{};
   const int64_t rows = (int64_t)S.where.q_tokens * S.group, most = (int64_t)S.max_q * S.group;
@@ -130,7 +135,7 @@ FwdPlan fwd_plan(const PackedShape &S) {
     p.owned = 64;
     p.pieces = pieces_bound(rows, most, S.where.count, p.owned);
   }
-  const Cut c = cut_keys(S, p.pieces, S.dtype == MTNLG_F32 ? 0.11 * S.d : 0.9, CUT_LEAST, 1024);
+  const Cut c = cut_keys(S, p.pieces, p.owned, fwd_tile(S), fwd_slots(S), CUT_LEAST, 1024);
   p.chunk = c.chunk;
   p.chunks = c.chunks;
   if (p.chunks > 1) {
@@ -173,7 +178,7 @@ BwdPlan bwd_plan(const PackedShape &S) {
   p.d_bytes = align_up((size_t)S.where.q_tokens * S.heads * sizeof(float), 256);
   p.part_bytes = p.splits > 1 ? align_up((size_t)p.splits * S.where.k_tokens * S.kv_heads * 2 * S.d * sizeof(float), 256) : 0;
   // fp32: a tile of dq is long, and few rows are few workgroups (1536 tokens in 4 documents, 8 heads of 96 on 4: 114 us whole, 53 and 8 for the join so)
-  p.cut = S.dtype == MTNLG_F32 ? cut_keys(S, p.pieces, 0.16 * S.d, 64, 512) : Cut{0, 1};
+  p.cut = S.dtype == MTNLG_F32 ? cut_keys(S, p.pieces, p.owned, 0.16 * S.d, 512, 64, 512) : Cut{0, 1};
   p.pieces = cut_pieces(S, p.cut, p.pieces, p.owned);
   p.bytes = p.d_bytes + p.part_bytes + (p.cut.chunks > 1 ? (size_t)p.cut.chunks * S.where.q_tokens * S.heads * S.d * sizeof(float) : 0);
   return p;
