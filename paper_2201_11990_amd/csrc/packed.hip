@@ -5,6 +5,8 @@ namespace mtnlg {
 
 namespace {
 
+constexpr int MOST_CHUNKS = 64;   // of a row: a lane of the wave that joins them to each
+
 // A row's results from those of its chunks: a wave to a row, four columns to a lane.
 template <typename E>
 __global__ __launch_bounds__(256) void packed_join_kernel(PackedFwdArgs w) {
@@ -114,7 +116,8 @@ Cut cut_keys(const PackedShape &S, int64_t pieces, int owned, double tile, int s
   const double wide = (double)(pieces * S.kv_heads), mean = (double)S.where.k_tokens / S.where.count;
   if (S.max_k < 2 * least || wide >= 1024) return Cut{0, 1};
   const double work = wide * mean / 64 / slots;   // tiles of a slot where all come out even
-  const int want = (int)fmax(least, fmax(S.max_k / 64.0, wide * mean / into));   // (64: a lane of the joining wave to each)
+  // (rounded up: 16385 keys in chunks of 256 are 65)
+  const int want = (int)fmax(least, fmax((S.max_k + (int64_t)MOST_CHUNKS - 1) / MOST_CHUNKS, wide * mean / into));
   const int chunk = (want + 63) / 64 * 64;
   const Cut c{chunk, (S.max_k + chunk - 1) / chunk};
   const double each = fmax(1.0, mean / chunk);   // chunks of a sequence

@@ -216,6 +216,22 @@ def test_single_tokens_over_long_caches(dtype, keys, group, d):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("queries,keys", [([1], [16384]), ([1], [16385]), ([1], [16447]), ([1, 1], [300, 20481]), ([1], [32769]), ([3], [16400])])
+def test_a_cache_in_as_many_chunks_as_there_are(dtype, queries, keys):
+    # the last key, which a further chunk would hold alone or with a few others, has most of the first head's weight
+    c = Case(queries, keys, 1, 2, 64, dtype, backward=False, seed=61)
+    c.k[-1, 0] = 3 * c.q[-1, 0, 0]
+    fwd, _ = c.workspaces()
+    assert fwd is not None
+    want = c.want()
+    c.run()
+    c.check(want)
+    c.a.fill_(SENTINEL), c.lse.fill_(SENTINEL)
+    c.run(with_workspace=False)
+    c.check(want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_prompts_continued_behind_a_cache(dtype):
     c = Case(None, None, 2, 2, 128, dtype, q_off=[0, 100, 133, 133], k_off=[0, 1536, 2048, 2304], k_len=[1400, 33, 100], backward=False)
     c.run()

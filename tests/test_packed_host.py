@@ -106,6 +106,20 @@ def test_workspace_sizes():
     assert bwd(packed(heads=8, kv_heads=8, q_tokens=1 << 20, k_tokens=1 << 20, max_q=1 << 20, max_k=1 << 20)) >= 8 * (1 << 20) * 4
 
 
+@pytest.mark.parametrize("dtype,d", [(B.BF16, 128), (B.F32, 64), (B.BF16, 256)])
+@pytest.mark.parametrize("sequences,kv_heads", [(1, 1), (1, 8), (2, 8), (32, 1)])
+def test_no_row_has_more_chunks_than_the_joining_wave_has_lanes(dtype, d, sequences, kv_heads):
+    # the workspace holds d sums, a maximum and a sum of each row and chunk, in two parts of whole 256 bytes
+    row, most = 4 * (d + 2) * 4 * kv_heads * sequences, 0
+    for n in range(64, 1 << 20, 64):
+        for max_k in (n - 1, n, n + 1, n + 32, n + 63):
+            size = M.mtnlg_packed_attention_fwd_workspace(packed(dtype=dtype, heads=4 * kv_heads, kv_heads=kv_heads, head_dim=d, sequences=sequences, max_q=1,
+                                                                 max_k=max_k, q_tokens=sequences, k_tokens=sequences * max_k))
+            most = max(most, size // row)
+            assert size // row <= 64, max_k
+    assert most > 32   # the limit is looked at
+
+
 def rotary(q=None, k=None, qo=None, ko=None, positions=None, backward=False, **kw):
     d = dict(dtype=B.BF16, heads=4, kv_heads=2, head_dim=64, rotary_dim=64, layout=0, scaling=0, original_positions=0, tokens=10, base=1e4, factor=1.0,
              slow=1.0, fast=32.0, amplitude=0.0)
