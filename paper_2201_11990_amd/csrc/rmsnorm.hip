@@ -64,6 +64,24 @@ __device__ __forceinline__ unsigned e4m3_of4(float a, float b, float c, float d)
   return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(within(c), within(d), w, true);
 }
 
+// y / scale, correctly rounded: codes are of quotients by the scale that is stored, and next to a border between two codes a product with a rounded reciprocal has the other
+// one.  Both are taken relative to the power of two in the scale (exact), so that nothing below overflows or loses bits that a code shows; the product with the
+// mantissa's reciprocal is corrected by its remainder (Markstein, "Computation of elementary functions on the IBM RISC System/6000 processor", 1990).  8192 rows of
+// 2048 columns to 8 bits: 26.0 us a call, 25.4 with products by 448 / m, 26.8 with eight divisions.
+struct QuotientBy {
+  float toward, mantissa, inverse;
+  __device__ __forceinline__ explicit QuotientBy(float scale) {   // normal, or infinite: quotients of what is finite are 0 then
+    const unsigned bits = __float_as_uint(scale);
+    toward = __uint_as_float(bits < 0x7F800000u ? 0x7F000000u - (bits & 0x7F800000u) : 0);
+    mantissa = __uint_as_float((bits & 0x7FFFFFu) | 0x3F800000u);
+    inverse = 1.0f / mantissa;
+  }
+  __device__ __forceinline__ float operator()(float y) const {
+    const float x = y * toward, q = x * inverse;
+    return fmaf(fmaf(-q, mantissa, x), inverse, q);
+  }
+};
+
 template <typename E, int W, int NV, bool E4M3>
 __global__ __launch_bounds__(threads_of<W>()) void rmsnorm_fwd_kernel(NormArgs a) {
   __shared__ float red[16];
@@ -129,13 +147,13 @@ __global__ __launch_bounds__(threads_of<W>()) void rmsnorm_fwd_kernel(NormArgs a
         for (int off = 1; off < a.columns / 8; off *= 2) m = fmaxf(m, __shfl_xor(m, off, 64));
       }
       if (j >= nvec) continue;
-      // (below SCALE_LEAST the reciprocal would overflow, and 0 times it be NaN)
-      const float scale = m > 0.0f ? fmaxf(m * (1.0f / E4M3_MOST), SCALE_LEAST) : 1.0f, inverse = m > E4M3_MOST * SCALE_LEAST ? E4M3_MOST / m : m > 0.0f ? 1.0f / SCALE_LEAST : 1.0f;
+      const float scale = m > 0.0f ? fmaxf(m / E4M3_MOST, SCALE_LEAST) : 1.0f;
+      const QuotientBy by(scale);
       const int first = a.columns ? 8 * j % a.columns : j;
       if (first == 0) a.scale[row * a.scales + (a.columns ? 8 * j / a.columns : 0)] = scale;
       float y[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = v[i][e] * inverse;
+      for (int e = 0; e < 8; ++e) y[e] = by(v[i][e]);
       *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(a.out) + row * a.h + 8 * j) =
           uint2{e4m3_of4(y[0], y[1], y[2], y[3]), e4m3_of4(y[4], y[5], y[6], y[7])};
     }

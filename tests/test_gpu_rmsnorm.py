@@ -117,6 +117,38 @@ def test_eight_bits(dtype, T, h, columns):
     within(out, code, torch.maximum(2.0 ** -4 * code.abs(), torch.full_like(code, 2.0 ** -10)) + 50 * F * code.abs(), "out")
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("T,h,columns", [(2000, 2048, 128), (1500, 1000, 0), (70, 20480, 8)])
+def test_codes_and_scales_bit_by_bit(dtype, T, h, columns):
+    # from the norm's rstd on every operation rounds once to fp32, here as there: two products, the largest magnitude / 448, the quotient by that scale; then to the nearest code
+    s = inputs(T, h, dtype, 7)
+    n = columns or h
+    scale, rstd = torch.empty((T, -(-h // n)), device="cuda"), torch.empty(T, device="cuda")
+    out, xsum = torch.empty((T, h), dtype=torch.float8_e4m3fn, device="cuda"), torch.empty_like(s["x"])
+    M.mtnlg_rmsnorm_fwd_e4m3(s["x"], s["gamma"], EPS, out, scale, rstd, columns=columns, residual=s["residual"], xsum=xsum)
+    y = xsum.cpu().float() * rstd.cpu()[:, None] * s["gamma"].cpu().float()
+    want_scale = torch.stack([p.abs().amax(-1) for p in y.split(n, -1)], -1) / 448
+    assert torch.equal(scale.cpu(), want_scale)
+    codes = (y / torch.repeat_interleave(want_scale, n, -1)[:, :h]).clamp(-448, 448).to(torch.float8_e4m3fn)
+    assert torch.equal(out.cpu().view(torch.uint8), codes.view(torch.uint8))
+
+
+@pytest.mark.parametrize("columns", [0, 32])
+def test_eight_bits_beside_an_infinity(columns):
+    # an infinite scale: quotients of what is finite are zeros, of the infinity itself not a number; other groups are as they were
+    x, gamma = torch.randn((3, 64), generator=torch.Generator(device="cuda").manual_seed(6), device="cuda"), torch.ones(64, device="cuda")
+    new = lambda: (torch.empty((3, 64), dtype=torch.float8_e4m3fn, device="cuda"), torch.empty((3, 2 if columns else 1), device="cuda"))   # noqa: E731
+    (codes, scale), (want, want_scale), rstd = new(), new(), torch.empty(3, device="cuda")
+    M.mtnlg_rmsnorm_fwd_e4m3(x, gamma, EPS, want, want_scale, rstd, columns=columns)
+    gamma[5] = float("inf")
+    M.mtnlg_rmsnorm_fwd_e4m3(x, gamma, EPS, codes, scale, rstd, columns=columns)
+    assert torch.isposinf(scale[:, 0]).all() and torch.isnan(codes[:, 5].float()).all()
+    others = [i for i in range(columns or 64) if i != 5]
+    assert (codes.float()[:, others] == 0).all()
+    if columns:
+        assert torch.equal(scale[:, 1], want_scale[:, 1]) and torch.equal(codes.float()[:, columns:], want.float()[:, columns:])
+
+
 def test_rows_of_zeros_infinities_and_nan():
     x = torch.randn((5, 64), device="cuda")
     x[1], x[2, 5], x[3, 7] = 0, float("nan"), float("inf")
