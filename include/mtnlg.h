@@ -350,7 +350,7 @@ typedef struct {
   int32_t heads, kv_heads, head_dim;   /* heads a multiple of kv_heads; head_dim of 8, <= 256                */
   int32_t sequences;                   /* <= 2^16: a workgroup counts through them to its work                  */
   int32_t max_q, max_k;                /* no sequence has more queries, keys; what lies beyond is unspecified */
-  int64_t q_tokens, k_tokens;          /* rows of q, a, da, dq; of k, v, dk, dv; times their heads < 2^31    */
+  int64_t q_tokens, k_tokens;          /* rows of q, a, da, dq; of k, v, dk, dv; times their heads at most 2^31 - 2^8 */
   float scale;                         /* 0 => 1/sqrt(head_dim)                                            */
 } mtnlg_packed_desc;
 /* Sequence i has the rows offsets[i] .. offsets[i + 1] - 1, or the first lengths[i] of them (lengths nullable: a cache whose regions

@@ -6,6 +6,7 @@ namespace mtnlg {
 namespace {
 
 constexpr int MOST_CHUNKS = 64;   // of a row: a lane of the wave that joins them to each
+constexpr int64_t MOST_ROWS = ((int64_t)1 << 31) - 256;
 
 // A row's results from those of its chunks: a wave to a row, four columns to a lane.
 template <typename E>
@@ -117,14 +118,16 @@ Cut cut_keys(const PackedShape &S, int64_t pieces, int owned, double tile, int s
   if (S.max_k < 2 * least || wide >= 1024) return Cut{0, 1};
   const double work = wide * mean / 64 / slots;   // tiles of a slot where all come out even
   // (rounded up: 16385 keys in chunks of 256 are 65)
-  const int want = (int)fmax(least, fmax((S.max_k + (int64_t)MOST_CHUNKS - 1) / MOST_CHUNKS, wide * mean / into));
-  const int chunk = (want + 63) / 64 * 64;
-  const Cut c{chunk, (S.max_k + chunk - 1) / chunk};
+  const double want = fmax(least, fmax((S.max_k + (int64_t)MOST_CHUNKS - 1) / MOST_CHUNKS, wide * mean / into));
+  if (want >= S.max_k) return Cut{0, 1};
+  const int64_t chunk = ((int64_t)want + 63) / 64 * 64;
+  if (chunk >= S.max_k) return Cut{0, 1};
+  const Cut c{(int)chunk, (int)((S.max_k + chunk - 1) / chunk)};
   const double each = fmax(1.0, mean / chunk);   // chunks of a sequence
   const double idle = fmax(0.0, (double)(cut_pieces(S, c, pieces, owned) * S.kv_heads) - wide * each);
   const double whole = tile * fmax(S.max_k / 64.0, work);
   const double cut = tile * fmax(chunk / 64.0, work) + (3.5 * wide * each + 3.0 * idle) / slots + 8.0 + (double)S.where.q_tokens * S.heads * each * S.d * 8.0 / 4.0e6;
-  return chunk >= S.max_k || 1.5 * cut >= whole ? Cut{0, 1} : c;
+  return 1.5 * cut >= whole ? Cut{0, 1} : c;
 }
 // us of 64 keys of the forward kernels, and how many of their workgroups run at once
 double fwd_tile(const PackedShape &S) { return S.dtype == MTNLG_F32 ? (S.d <= 160 ? 0.11 : 0.07) * S.d : S.d > PACKED_TUNED ? 5.0 : 0.9; }
@@ -197,7 +200,8 @@ int packed_shape(const mtnlg_packed_desc *D, PackedShape *S) {
   if (!(D->scale >= 0.0f && D->scale < INFINITY)) return MTNLG_INVALID_ARG;
   if (D->head_dim % 8 || D->head_dim > 256 || D->heads > 65535 || D->sequences > 1 << 16) return MTNLG_UNSUPPORTED_SHAPE;
   if (D->q_tokens > 0x7FFFFFFF || D->k_tokens > 0x7FFFFFFF) return MTNLG_UNSUPPORTED_SHAPE;
-  if (D->q_tokens * D->heads > 0x7FFFFFFF || D->k_tokens * D->kv_heads > 0x7FFFFFFF) return MTNLG_UNSUPPORTED_SHAPE;   // rows are counted in 32 bits
+  // rows are counted in 32 bits, up to the end of the block that has the last one
+  if (D->q_tokens * D->heads > MOST_ROWS || D->k_tokens * D->kv_heads > MOST_ROWS) return MTNLG_UNSUPPORTED_SHAPE;
   *S = PackedShape{D->dtype, D->heads, D->kv_heads, D->heads / D->kv_heads, D->head_dim, D->scale > 0.0f ? D->scale : 1.0f / sqrtf((float)D->head_dim),
                    Sequences{nullptr, nullptr, nullptr, nullptr, D->sequences, (int)D->q_tokens, (int)D->k_tokens}, D->max_q, D->max_k};
   // no sequence is longer than the matrix

@@ -78,7 +78,7 @@ __global__ __launch_bounds__(64 * WAVES, per_unit<D>()) void packed_fwd_kernel(P
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int j = blockIdx.x % w.kv_heads;
   const bool chunked = w.chunk > 0;
-  auto chunks_of = [&](const Span &s) { return chunked ? min((max(s.lk, 1) + w.chunk - 1) / w.chunk, w.chunks) : 1; };
+  auto chunks_of = [&](const Span &s) { return chunked ? min((int)(((unsigned)max(s.lk, 1) + w.chunk - 1) / w.chunk), w.chunks) : 1; };   // (unsigned: the sum may pass 2^31)
   Span s;
   unsigned at;
   if (!find_piece(w.where, blockIdx.x / w.kv_heads, [&](const Span &s) { return (unsigned)((s.lq * r + OWNED - 1) / OWNED * chunks_of(s)); }, s, at)) return;

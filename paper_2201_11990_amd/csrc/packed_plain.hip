@@ -25,7 +25,7 @@ __global__ __launch_bounds__(256, (fwd_per_unit<E, D>())) void plain_fwd_kernel(
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int j = blockIdx.x % w.kv_heads;
   const bool chunked = w.chunk > 0;
-  auto chunks_of = [&](const Span &s) { return chunked ? min((max(s.lk, 1) + w.chunk - 1) / w.chunk, w.chunks) : 1; };
+  auto chunks_of = [&](const Span &s) { return chunked ? min((int)(((unsigned)max(s.lk, 1) + w.chunk - 1) / w.chunk), w.chunks) : 1; };   // (unsigned: the sum may pass 2^31)
   Span s;
   unsigned at;
   if (!find_piece(w.where, blockIdx.x / w.kv_heads, [&](const Span &s) { return (unsigned)((s.lq * r + OWNED - 1) / OWNED * chunks_of(s)); }, s, at)) return;
@@ -185,7 +185,7 @@ __global__ __launch_bounds__(256, (dq_per_unit<E, D>())) void plain_dq_kernel(Pa
   Span s;
   unsigned at;
   const bool chunked = w.chunk > 0;
-  auto chunks_of = [&](const Span &s) { return chunked ? min((max(s.lk, 1) + w.chunk - 1) / w.chunk, w.chunks) : 1; };
+  auto chunks_of = [&](const Span &s) { return chunked ? min((int)(((unsigned)max(s.lk, 1) + w.chunk - 1) / w.chunk), w.chunks) : 1; };   // (unsigned: the sum may pass 2^31)
   if (!find_piece(w.where, blockIdx.x / w.kv_heads, [&](const Span &s) { return (unsigned)((s.lq * r + OWNED - 1) / OWNED * chunks_of(s)); }, s, at)) return;
   const int nc = chunks_of(s), count = (s.lq * r + OWNED - 1) / OWNED, shift = s.lk - s.lq;
   const int chunk = at % nc, block = count - 1 - at / nc;   // falling work

@@ -349,6 +349,24 @@ def test_a_cache_beyond_32_bits_of_elements():
     small.check()
 
 
+def test_a_cache_of_nearly_as_many_keys_as_there_may_be():
+    # their number and a chunk's add up to more than 2^31.  All scores are 0 but the last one, that key's value 3 where all others are 1
+    tk, d = (1 << 31) - 300, 8
+    k, v = torch.zeros((tk, 1, d), dtype=torch.bfloat16, device="cuda"), torch.ones((tk, 1, d), dtype=torch.bfloat16, device="cuda")
+    q, a, lse = torch.ones((1, 1, d), dtype=torch.bfloat16, device="cuda"), torch.full((1, 1, d), SENTINEL, dtype=torch.bfloat16, device="cuda"), torch.full((1, 1), SENTINEL, device="cuda")
+    k[-1], v[-1] = 8, 3
+    score = 64 / math.sqrt(d)
+    desc = M.packed_desc(q, k, 1, 1, tk)
+    ws = torch.full((M.mtnlg_packed_attention_fwd_workspace(desc),), 0xFF, dtype=torch.uint8, device="cuda")
+    assert ws.numel() > 0
+    M.mtnlg_packed_attention_fwd(q, k, v, a, lse, i32([0, 1]), i32([0, tk]), 1, tk, workspace=ws)
+    total = tk - 1 + math.exp(score)
+    # sums of equal weights are whole numbers up to 2^24 for each part of a chunk, exact; the other weights' exponent, 33, is off by 2^-18, and the score by 2^-18 as well
+    assert abs(float(lse) - math.log(total)) <= 2.0 ** -16
+    want = (tk - 1 + 3 * math.exp(score)) / total
+    assert (a.double() - want).abs().max() <= 2.0 ** -8 * want * 1.01 + 2.0 ** -15
+
+
 def test_gradients_against_differences():
     # the sum of da . a and its change with each input along a random direction, in fp32 with 64-bit sums; central differences of step h are off by
     # h^2 times a third derivative, and by the fp32 roundings of a over 2 h

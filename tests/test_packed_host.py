@@ -56,6 +56,17 @@ def test_descriptors_that_are_refused(bad, status, backward):
 
 
 @pytest.mark.parametrize("backward", [False, True])
+def test_rows_that_are_counted_past_32_bits_are_refused(backward):
+    # a count of rows goes on to the end of the block that holds the last one: 2^31 - 2^8 rows at most
+    size = M.mtnlg_packed_attention_bwd_workspace if backward else M.mtnlg_packed_attention_fwd_workspace
+    for most in (dict(q_tokens=(1 << 31) - 255, heads=1, kv_heads=1), dict(q_tokens=(1 << 29) - 63), dict(k_tokens=(1 << 30) - 127)):
+        desc = packed(**most)
+        assert attention(desc, backward=backward) == SHAPE, most
+        assert size(desc) == 0
+    assert M.mtnlg_packed_attention_bwd_workspace(packed(q_tokens=(1 << 29) - 64, k_tokens=(1 << 30) - 128)) > 0
+
+
+@pytest.mark.parametrize("backward", [False, True])
 def test_null_pointers_and_workspaces_that_are_too_small(backward):
     for n in ("q", "k", "v", "a") + (("da", "dq", "dk", "dv") if backward else ()):
         assert attention(backward=backward, **{n: None}) == NULL
