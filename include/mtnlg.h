@@ -353,6 +353,7 @@ typedef struct {
   int64_t q_tokens, k_tokens;          /* rows of q, a, da, dq; of k, v, dk, dv; times their heads at most 2^31 - 2^8 */
   float scale;                         /* 0 => 1/sqrt(head_dim)                                            */
 } mtnlg_packed_desc;
+/* Unsupported shapes too: calls of 2^24 workgroups or more (one to 128 rows of a head of keys, at least one to a sequence and head); backward, of 2^23 (one to 64 keys). */
 /* Sequence i has the rows offsets[i] .. offsets[i + 1] - 1, or the first lengths[i] of them (lengths nullable: a cache whose regions
  * are not full, a padded batch).  Device arrays of sequences + 1 and sequences int32; offsets do not fall.  Lengths may be 0.  Values that lie
  * outside the matrices are taken for the nearest inside; offsets that fall leave results unspecified. */

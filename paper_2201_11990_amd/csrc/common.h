@@ -304,6 +304,8 @@ struct LaunchScope {
   ~LaunchScope();
 };
 
+// A launch has fewer than 2^32 work items in a dimension of its grid.
+inline bool grid_fits(int64_t blocks, int threads) { return blocks <= 0xFFFFFFFFll / threads; }
 inline int check_launch() { return hipGetLastError() == hipSuccess ? MTNLG_OK : MTNLG_HIP_ERROR; }
 
 // Kernel attributes (dynamic LDS size) are set once per device and kernel: `done` is a bit mask of

@@ -256,7 +256,7 @@ int mtnlg_packed_attention_fwd(const mtnlg_packed_desc *desc, const mtnlg_packed
   w.stat = (float *)((char *)workspace + plan.part_bytes);
   const int64_t pieces = cut_pieces(S, Cut{plan.chunk, plan.chunks}, plan.pieces, plan.owned);
   const int64_t blocks = pieces * S.kv_heads;
-  if (blocks > 0x7FFFFFFF) return MTNLG_UNSUPPORTED_SHAPE;
+  if (!grid_fits(blocks, 256)) return MTNLG_UNSUPPORTED_SHAPE;
   const hipStream_t st = (hipStream_t)stream;
   LaunchScope scope(MTNLG_K_ATTN_FWD, st);
   MTNLG_TRY(packed_tuned(S.dtype, S.d) ? packed_fwd_tuned(w, plan.owned, blocks, st) : packed_fwd_plain(S.dtype, w, blocks, st));
@@ -290,7 +290,8 @@ int mtnlg_packed_attention_bwd(const mtnlg_packed_desc *desc, const mtnlg_packed
   if (((uintptr_t)lse & 3) || ((uintptr_t)workspace & 15) || unaligned(where)) return MTNLG_INVALID_ARG;
   const BwdPlan plan = bwd_plan(S);
   if (workspace_bytes < plan.bytes) return MTNLG_WORKSPACE_TOO_SMALL;
-  if (plan.pieces * S.kv_heads > 0x7FFFFFFF || plan.key_pieces * plan.splits * S.kv_heads > 0x7FFFFFFF) return MTNLG_UNSUPPORTED_SHAPE;
+  const int key_threads = packed_tuned(S.dtype, S.d) ? 512 : 4 * plan.key_owned;   // of a dk / dv workgroup
+  if (!grid_fits(plan.pieces * S.kv_heads, 256) || !grid_fits(plan.key_pieces * plan.splits * S.kv_heads, key_threads)) return MTNLG_UNSUPPORTED_SHAPE;
   PackedBwdArgs w{};
   w.where = Sequences{where->q_offsets, where->k_offsets, where->q_lengths, where->k_lengths, S.where.count, S.where.q_tokens, S.where.k_tokens};
   w.kv_heads = S.kv_heads;

@@ -66,6 +66,15 @@ def test_rows_that_are_counted_past_32_bits_are_refused(backward):
     assert M.mtnlg_packed_attention_bwd_workspace(packed(q_tokens=(1 << 29) - 64, k_tokens=(1 << 30) - 128)) > 0
 
 
+def test_launches_of_more_work_items_than_there_may_be_are_refused():
+    # 2^16 sequences of a token each, 256 heads of keys: 2^24 workgroups of 256
+    wide = dict(heads=256, kv_heads=256, head_dim=8, sequences=1 << 16, max_q=1, max_k=1, q_tokens=1 << 16, k_tokens=1 << 16)
+    m = {n: heads((i + 1) << 36, 2048, 8, 0) for i, n in enumerate(("q", "k", "v", "a", "da", "dq", "dk", "dv"))}
+    assert attention(packed(**wide), **m) == SHAPE and attention(packed(**wide), backward=True, **m) == SHAPE
+    # a workgroup of 512 to 64 keys: 2^23 of them from 2^29 keys on
+    assert attention(packed(k_tokens=1 << 28, max_k=1 << 28), backward=True) == SHAPE
+
+
 @pytest.mark.parametrize("backward", [False, True])
 def test_null_pointers_and_workspaces_that_are_too_small(backward):
     for n in ("q", "k", "v", "a") + (("da", "dq", "dk", "dv") if backward else ()):
