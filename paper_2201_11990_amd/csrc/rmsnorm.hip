@@ -160,22 +160,38 @@ __global__ __launch_bounds__(threads_of<W>()) void rmsnorm_fwd_kernel(NormArgs a
   }
 }
 
+// Rows of a launch: 16 waves to each would pass 2^32 work items from 2^22 on.
+constexpr int64_t LAUNCHED_ROWS = 1 << 21;
+
 template <typename E, bool E4M3>
-int fwd_launch(const NormArgs &a, hipStream_t st) {
-  const int nvec = a.h / 8;
+int fwd_launch(const NormArgs &all, hipStream_t st) {
+  const int nvec = all.h / 8;
   LaunchScope scope(MTNLG_K_LN_FWD, st);
+  for (int64_t first = 0; first < all.rows; first += LAUNCHED_ROWS) {
+    NormArgs a = all;
+    a.rows = all.rows - first < LAUNCHED_ROWS ? all.rows - first : LAUNCHED_ROWS;
+    a.x = static_cast<const E *>(all.x) + first * all.h;
+    if (all.residual) {
+      a.residual = static_cast<const E *>(all.residual) + first * all.h;
+      a.xsum = static_cast<E *>(all.xsum) + first * all.h;
+    }
+    a.out = static_cast<char *>(all.out) + first * all.h * (E4M3 ? 1 : sizeof(E));
+    a.rstd = all.rstd + first;
+    if (E4M3) a.scale = all.scale + first * all.scales;
 #define RMS(W, NV) \
   rmsnorm_fwd_kernel<E, W, NV, E4M3><<<(unsigned)((a.rows + threads_of<W>() / (64 * W) - 1) / (threads_of<W>() / (64 * W))), threads_of<W>(), 0, st>>>(a)
-  if (nvec <= 64) RMS(1, 1);
-  else if (nvec <= 128) RMS(1, 2);
-  else if (nvec <= 256) RMS(4, 1);
-  else if (nvec <= 512) RMS(4, 2);
-  else if (nvec <= 1024) RMS(16, 1);
-  else if (nvec <= 2048) RMS(16, 2);
-  else if (nvec <= 3 * 1024) RMS(16, 3);
-  else RMS(16, 4);
+    if (nvec <= 64) RMS(1, 1);
+    else if (nvec <= 128) RMS(1, 2);
+    else if (nvec <= 256) RMS(4, 1);
+    else if (nvec <= 512) RMS(4, 2);
+    else if (nvec <= 1024) RMS(16, 1);
+    else if (nvec <= 2048) RMS(16, 2);
+    else if (nvec <= 3 * 1024) RMS(16, 3);
+    else RMS(16, 4);
 #undef RMS
-  return check_launch();
+    MTNLG_TRY(check_launch());
+  }
+  return MTNLG_OK;
 }
 
 // ------------------------------------------------------------------ backward

@@ -175,6 +175,38 @@ def test_eight_bits_of_results_too_small_for_their_scale(columns):
     within(codes, code, torch.maximum(2.0 ** -4 * code.abs(), torch.full_like(code, 2.0 ** -10)) + 50 * F * code.abs() + F, "codes")
 
 
+@pytest.mark.parametrize("T,h", [((1 << 21) + 5, 16), ((1 << 22) + 3, 4104), ((1 << 26) + 5, 8)])
+@pytest.mark.parametrize("with_residual", [True, False])
+def test_more_rows_than_a_launch_has(T, h, with_residual):
+    # with a workgroup of 16 waves to a row, or four rows to one of 256 threads, 2^22 and 2^26 rows are 2^32 work items.  Rows that all look alike but for their sign and a factor of 2
+    g = torch.Generator(device="cuda").manual_seed(8)
+    one, gamma = torch.randn(h, generator=g, device="cuda").bfloat16(), (1 + 0.2 * torch.randn(h, generator=g, device="cuda")).bfloat16()
+    rows = torch.arange(T, device="cuda") % 3
+    factor = torch.tensor([1.0, -1.0, 2.0], device="cuda").bfloat16()
+    x = factor[rows][:, None] * one
+    residual = x if with_residual else None
+    out, rstd = torch.empty_like(x), torch.full((T,), float("nan"), device="cuda")
+    out.fill_(float("nan"))
+    xsum = torch.empty_like(x) if with_residual else None
+    M.mtnlg_rmsnorm_fwd(x, gamma, EPS, out, rstd, residual=residual, xsum=xsum)
+    three = factor[:, None] * one * (2 if with_residual else 1)
+    r, y = norm64(three, gamma)
+    within(out[-3:], y[rows[-3:]], (2.0 ** -8 + 45 * F) * y[rows[-3:]].abs(), "out")
+    within(rstd[-3:], r[rows[-3:], 0], 40 * F * r[rows[-3:], 0], "rstd")
+    same = lambda t: (t[:T // 3 * 3].unflatten(0, (-1, 3)) == t[:3]).all() and torch.equal(t[T // 3 * 3:], t[:T % 3])   # noqa: E731
+    within(out[:3], y, (2.0 ** -8 + 45 * F) * y.abs(), "out")
+    assert same(rstd) and same(out)
+    if with_residual:
+        assert torch.equal(xsum[:3], three) and same(xsum)
+    del out, x, residual
+    codes, scale = torch.zeros((T, h), dtype=torch.uint8, device="cuda"), torch.zeros((T, 1), device="cuda")
+    x = factor[rows][:, None] * one
+    M.mtnlg_rmsnorm_fwd_e4m3(x, gamma, EPS, codes.view(torch.float8_e4m3fn), scale, rstd)
+    assert same(codes) and same(scale) and (scale > 0).all()
+    del x, codes, xsum
+    torch.cuda.empty_cache()
+
+
 def test_runs_are_identical_and_replays_too():
     s = inputs(700, 2048, "bf16", 3)
     rstd, out, dx, dgamma = torch.empty(700, device="cuda"), torch.empty_like(s["x"]), torch.empty_like(s["x"]), torch.empty(2048, device="cuda")
