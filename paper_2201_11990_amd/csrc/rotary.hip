@@ -16,7 +16,7 @@ namespace mtnlg {
 namespace {
 
 struct RotaryArgs {
-  int64_t tokens;
+  int64_t tokens, begin;   // begin: first token of the launch
   int heads, kv_heads, group, d, n;   // rows of a token: its query heads, then its key heads
   const void *q, *k;
   void *q_out, *k_out;
@@ -32,6 +32,7 @@ struct RotaryArgs {
 // Pairs of a tile: one to a thread.  8192 tokens of 20 heads of 128 on buffers that no cache holds, halves, then side by side: 3 tokens to a tile 22.5 and 31 us, 6 and 3 22.5 and
 // 27.5, 4 (side by side) 25.4, 8 27 and 28.7.
 constexpr int THREADS = 256, MAX_PAIRS = THREADS, MAX_TILE = 64;
+constexpr int MOST_BLOCKS = 1 << 23;   // of a launch, which has fewer than 2^32 work items
 constexpr int AHEAD = 2;   // rows of a thread at once: 3 and 4 cost registers and with them waves (24.6, 27 us)
 
 // turns of pair i for one position
@@ -56,7 +57,7 @@ __global__ __launch_bounds__(THREADS) void rotary_kernel(RotaryArgs a) {
   __shared__ int place[MAX_TILE];      // positions of the tile's tokens
   __shared__ double rate[128];         // turns of each pair for one position
   const int pairs = a.n / 2;
-  const int64_t first = (int64_t)blockIdx.x * a.tile;
+  const int64_t first = a.begin + (int64_t)blockIdx.x * a.tile;
   const int tokens = (int)(a.tokens - first < a.tile ? a.tokens - first : a.tile);
   const int turned = HALF ? pairs / V : a.n / V, items = turned + a.copied, at_once = THREADS / items;
   const int item = threadIdx.x % items, row0 = threadIdx.x / items, heads = a.heads + a.kv_heads, rows = row0 < at_once ? tokens * heads : 0;
@@ -150,12 +151,16 @@ int launch(RotaryArgs &a, bool in_place, hipStream_t st) {
   a.tile = MAX_PAIRS / pairs < MAX_TILE ? MAX_PAIRS / pairs : MAX_TILE;
   if (want < a.tile) a.tile = want < 1 ? 1 : want;
   if (a.tokens < 512 * (int64_t)a.tile) a.tile = (int)((a.tokens + 511) / 512);   // few tokens: more workgroups
-  const unsigned blocks = (unsigned)((a.tokens + a.tile - 1) / a.tile);
   LaunchScope scope(MTNLG_K_ELEMENTWISE, st);
-  if (V == 8) rotary_kernel<E, 8, HALF><<<blocks, THREADS, 0, st>>>(a);
-  else if (V == 4) rotary_kernel<E, 4, HALF><<<blocks, THREADS, 0, st>>>(a);
-  else rotary_kernel<E, HALF ? 1 : 2, HALF><<<blocks, THREADS, 0, st>>>(a);
-  return check_launch();
+  for (a.begin = 0; a.begin < a.tokens; a.begin += (int64_t)MOST_BLOCKS * a.tile) {
+    const int64_t tiles = (a.tokens - a.begin + a.tile - 1) / a.tile;
+    const unsigned blocks = (unsigned)(tiles < MOST_BLOCKS ? tiles : MOST_BLOCKS);
+    if (V == 8) rotary_kernel<E, 8, HALF><<<blocks, THREADS, 0, st>>>(a);
+    else if (V == 4) rotary_kernel<E, 4, HALF><<<blocks, THREADS, 0, st>>>(a);
+    else rotary_kernel<E, HALF ? 1 : 2, HALF><<<blocks, THREADS, 0, st>>>(a);
+    MTNLG_TRY(check_launch());
+  }
+  return MTNLG_OK;
 }
 
 int rotary(const mtnlg_rotary_desc *D, const mtnlg_heads *q, const mtnlg_heads *k, const mtnlg_heads *q_out, const mtnlg_heads *k_out,

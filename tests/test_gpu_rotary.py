@@ -126,6 +126,27 @@ def test_turning_back_gives_the_heads_again_and_the_products_go_by_distance():
     assert ((near_products - far_products).abs() <= 2.0 ** -19 * sizes).all()
 
 
+def test_more_tokens_than_a_launch_has():
+    # 64 tokens to a workgroup of 256: 2^30 of them are 2^32 work items.  Rows look alike, and so do the positions of all tokens but the ones that are looked at
+    tokens = (1 << 30) + 100
+    row = torch.randn((1, 1, 8), generator=torch.Generator(device="cuda").manual_seed(11), device="cuda").bfloat16()
+    q, out = row.expand(tokens, 1, 8).contiguous(), torch.zeros((tokens, 1, 8), dtype=torch.bfloat16, device="cuda")
+    for given in (True, False):
+        positions = torch.full((tokens,), 77, dtype=torch.int32, device="cuda") if given else None
+        at = [0, 1, (1 << 29) - 1, 1 << 29, (1 << 29) + 1, (1 << 30) - 1, 1 << 30, tokens - 1]
+        if given:
+            positions[at] = torch.arange(len(at), dtype=torch.int32, device="cuda") + 1000
+        M.mtnlg_rotary_fwd(M.rotary_desc(2), q, None, out, None, positions=positions)
+        check(out[at], turned(q[at], positions[at] if given else torch.tensor(at), 2, M.ROTARY_HALF, "none"), "bf16", "q")
+        if given:
+            others = (out == out[5]).all(-1)[:, 0]
+            others[at] = True
+            assert others.all()
+        out.zero_()
+    del q, out, positions
+    torch.cuda.empty_cache()
+
+
 def test_a_captured_call_replays():
     q, k = heads(300, 2, 4, 128, "bf16", 4)
     positions = torch.arange(300, dtype=torch.int32, device="cuda")
