@@ -338,7 +338,7 @@ typedef struct {
  * Rows of a negative position (padding) are neither read nor written.  MTNLG_ROTARY_LINEAR: frequencies divided by factor;
  * _BASE: base * factor^(n / (n - 2)); _PARTS: of a pair that makes fewer than `slow` turns in the original context divided by factor, of one of
  * more than `fast` left, in between by their share.  Angles are worked out in 64 bits.  An output may be its input (same
- * strides); k and k_out may both be NULL. */
+ * strides), and nothing else that is read or written; k and k_out may both be NULL. */
 int mtnlg_rotary_fwd(const mtnlg_rotary_desc *desc, const mtnlg_heads *q, const mtnlg_heads *k, const mtnlg_heads *q_out,
                      const mtnlg_heads *k_out, const int32_t *positions, void *stream);
 /* Adjoint: gradients of q_out and k_out in, of q and k out (the heads turned back, with the same amplitude). */

@@ -186,6 +186,8 @@ int rotary(const mtnlg_rotary_desc *D, const mtnlg_heads *q, const mtnlg_heads *
   auto same = [](const mtnlg_heads *x, const mtnlg_heads *y) { return x->data == y->data && x->token == y->token && x->group == y->group && x->head == y->head; };
   // in place or apart; the same address with other strides would read what another row has written
   if ((q->data == q_out->data && !same(q, q_out)) || (k && k->data == k_out->data && !same(k, k_out))) return MTNLG_INVALID_ARG;
+  // ... and so would an output that is the other one, or the other one's input
+  if (k && (q_out->data == k->data || k_out->data == q->data || q_out->data == k_out->data)) return MTNLG_INVALID_ARG;
   RotaryArgs a{};
   a.tokens = D->tokens;
   a.heads = D->heads;

@@ -166,6 +166,15 @@ def test_rotary_calls_that_are_refused(bad, status, backward):
     assert rotary(backward=backward, **bad) == status
 
 
+@pytest.mark.parametrize("backward", [False, True])
+def test_rotary_outputs_on_one_another_or_on_the_other_input_are_refused(backward):
+    keys = lambda p: heads(p << 30, 128, 64, 0)   # noqa: E731
+    assert rotary(backward=backward, qo=heads(2 << 30)) == INVALID      # the keys that are read
+    assert rotary(backward=backward, ko=keys(1)) == INVALID             # the queries that are read
+    assert rotary(backward=backward, ko=keys(3)) == INVALID             # the queries that are written
+    assert rotary(backward=backward, q=heads(2 << 30), qo=heads(2 << 30)) == INVALID   # queries in place, of which the first are the keys
+
+
 def test_norms_that_are_refused():
     L = B.lib()
     fwd = lambda dtype=1, T=4, h=16, x=ONE, res=None, gamma=ONE, eps=1e-5, xsum=None, out=TWO, rstd=ONE: L.mtnlg_rmsnorm_fwd(   # noqa: E731
