@@ -331,12 +331,12 @@ typedef struct {
   double base;                         /* pair i turns by position * base^(-2 i / n) radians                    */
   double factor;                       /* >= 1, scaled only                                                   */
   double slow, fast;                   /* MTNLG_ROTARY_PARTS: turns in the original context, slow < fast        */
-  double amplitude;                    /* what cosines and sines are multiplied with; 0: 1, and 0.1 log(factor) + 1 of MTNLG_ROTARY_PARTS */
+  double amplitude;                    /* what cosines and sines are multiplied with, a finite float; 0: 1, and 0.1 log(factor) + 1 of MTNLG_ROTARY_PARTS */
 } mtnlg_rotary_desc;
 
 /* q_out, k_out = the heads of q and k turned by their tokens' positions (int32 [tokens], device; NULL: token t is at position t).
  * Rows of a negative position (padding) are neither read nor written.  MTNLG_ROTARY_LINEAR: frequencies divided by factor;
- * _BASE: base * factor^(n / (n - 2)); _PARTS: of a pair that makes fewer than `slow` turns in the original context divided by factor, of one of
+ * _BASE: base * factor^(n / (n - 2)), finite; _PARTS: of a pair that makes fewer than `slow` turns in the original context divided by factor, of one of
  * more than `fast` left, in between by their share.  Angles are worked out in 64 bits.  An output may be its input (same
  * strides), and nothing else that is read or written; k and k_out may both be NULL. */
 int mtnlg_rotary_fwd(const mtnlg_rotary_desc *desc, const mtnlg_heads *q, const mtnlg_heads *k, const mtnlg_heads *q_out,

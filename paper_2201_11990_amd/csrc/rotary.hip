@@ -188,6 +188,10 @@ int rotary(const mtnlg_rotary_desc *D, const mtnlg_heads *q, const mtnlg_heads *
   if ((q->data == q_out->data && !same(q, q_out)) || (k && k->data == k_out->data && !same(k, k_out))) return MTNLG_INVALID_ARG;
   // ... and so would an output that is the other one, or the other one's input
   if (k && (q_out->data == k->data || k_out->data == q->data || q_out->data == k_out->data)) return MTNLG_INVALID_ARG;
+  double base = D->base;
+  if (D->scaling == MTNLG_ROTARY_BASE && D->rotary_dim > 2) base *= pow(D->factor, (double)D->rotary_dim / (D->rotary_dim - 2));
+  const double amplitude = D->amplitude > 0.0 ? D->amplitude : D->scaling == MTNLG_ROTARY_PARTS ? 0.1 * log(D->factor) + 1.0 : 1.0;
+  if (!(base < INFINITY) || !((float)amplitude < INFINITY)) return MTNLG_INVALID_ARG;   // (their products would be NaN)
   RotaryArgs a{};
   a.tokens = D->tokens;
   a.heads = D->heads;
@@ -208,15 +212,13 @@ int rotary(const mtnlg_rotary_desc *D, const mtnlg_heads *q, const mtnlg_heads *
     a.k_out = take(k_out, a.kos);
   }
   a.positions = positions;
-  double base = D->base;
-  if (D->scaling == MTNLG_ROTARY_BASE && a.n > 2) base *= pow(D->factor, (double)a.n / (a.n - 2));
   a.base_log2 = log2(base);
   a.scaling = D->scaling;
   a.factor = D->factor;
   a.original = D->original_positions;
   a.slow = D->slow;
   a.fast = D->fast;
-  a.amplitude = (float)(D->amplitude > 0.0 ? D->amplitude : D->scaling == MTNLG_ROTARY_PARTS ? 0.1 * log(D->factor) + 1.0 : 1.0);
+  a.amplitude = (float)amplitude;
   a.sign = sign;
   const bool in_place = q->data == q_out->data && (!k || k->data == k_out->data);
   if (D->layout == MTNLG_ROTARY_HALF)

@@ -175,6 +175,11 @@ def test_rotary_outputs_on_one_another_or_on_the_other_input_are_refused(backwar
     assert rotary(backward=backward, q=heads(2 << 30), qo=heads(2 << 30)) == INVALID   # queries in place, of which the first are the keys
 
 
+@pytest.mark.parametrize("bad", [dict(scaling=2, factor=1e200, rotary_dim=4), dict(scaling=2, factor=1e300, base=1e10), dict(amplitude=1e39)])
+def test_rotary_bases_and_amplitudes_that_are_not_finite_are_refused(bad):
+    assert rotary(**bad) == INVALID
+
+
 def test_norms_that_are_refused():
     L = B.lib()
     fwd = lambda dtype=1, T=4, h=16, x=ONE, res=None, gamma=ONE, eps=1e-5, xsum=None, out=TWO, rstd=ONE: L.mtnlg_rmsnorm_fwd(   # noqa: E731
