@@ -183,9 +183,12 @@ int rotary(const mtnlg_rotary_desc *D, const mtnlg_heads *q, const mtnlg_heads *
     MTNLG_TRY(heads_check(k, D->tokens, D->kv_heads, 1, D->head_dim, D->dtype));
     MTNLG_TRY(heads_check(k_out, D->tokens, D->kv_heads, 1, D->head_dim, D->dtype));
   }
-  auto same = [](const mtnlg_heads *x, const mtnlg_heads *y) { return x->data == y->data && x->token == y->token && x->group == y->group && x->head == y->head; };
+  // (strides of a dimension of one are not looked at)
+  auto same = [&](const mtnlg_heads *x, const mtnlg_heads *y, int heads) {
+    return x->data == y->data && (D->tokens == 1 || x->token == y->token) && (D->kv_heads == 1 || x->group == y->group) && (heads == 1 || x->head == y->head);
+  };
   // in place or apart; the same address with other strides would read what another row has written
-  if ((q->data == q_out->data && !same(q, q_out)) || (k && k->data == k_out->data && !same(k, k_out))) return MTNLG_INVALID_ARG;
+  if ((q->data == q_out->data && !same(q, q_out, group)) || (k && k->data == k_out->data && !same(k, k_out, 1))) return MTNLG_INVALID_ARG;
   // ... and so would an output that is the other one, or the other one's input
   if (k && (q_out->data == k->data || k_out->data == q->data || q_out->data == k_out->data)) return MTNLG_INVALID_ARG;
   double base = D->base;

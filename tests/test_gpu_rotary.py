@@ -1,11 +1,13 @@
 """Rotary positions against 64 bits: amplitude (u cos - w sin) is off by the roundings of cosine, sine (each 2^-22: angle and function in fp32),
 two products and a sum (2^-23), and half a step of the storage type."""
+import ctypes
 import math
 
 import pytest
 import torch
 
 import paper_2201_11990_amd as M
+from paper_2201_11990_amd import binding as B
 
 pytestmark = pytest.mark.gpu
 DT = {"bf16": torch.bfloat16, "fp32": torch.float32}
@@ -124,6 +126,20 @@ def test_turning_back_gives_the_heads_again_and_the_products_go_by_distance():
     far_products = far[0][:, 0, 0].double() @ far[1][:, 0].double().T
     sizes = one[0][:, 0, 0].double().norm(dim=-1)[:, None] * one[1][:, 0].double().norm(dim=-1)
     assert ((near_products - far_products).abs() <= 2.0 ** -19 * sizes).all()
+
+
+@pytest.mark.parametrize("tokens,kv", [(5, 1), (1, 2), (1, 1)])
+def test_in_place_with_strides_that_are_not_looked_at(tokens, kv):
+    # of dimensions of one, and a head of keys' heads: whatever stands there, the same matrix is the same
+    q, k = heads(tokens, kv, 1, 64, "bf16", 12)
+    before = q.clone(), k.clone()
+    desc = B.RotaryDesc(B.BF16, kv, kv, 64, 64, M.ROTARY_HALF, M.ROTARY_UNSCALED, 0, tokens, 1e4, 1.0, 1.0, 32.0, 0.0)
+    m = lambda t, other: B.Heads(t.data_ptr(), 64 * kv if tokens > 1 else 24 * other, 64 if kv > 1 else 40 * other, 8 * other)   # noqa: E731
+    args = [m(q, 1), m(k, 2), m(q, 3), m(k, 4)]
+    status = B.lib().mtnlg_rotary_fwd(ctypes.byref(desc), *(ctypes.byref(a) for a in args), None, torch.cuda.current_stream().cuda_stream)
+    assert status == 0
+    for got, x in ((q, before[0]), (k, before[1])):
+        check(got, turned(x, torch.arange(tokens), 64, M.ROTARY_HALF, "none"), "bf16", "in place")
 
 
 def test_more_tokens_than_a_launch_has():
