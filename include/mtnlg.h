@@ -291,7 +291,7 @@ int mtnlg_bias_residual(int dtype, int64_t T, int64_t h, const void *res, const 
 
 /* s = x [+ residual] (stored to xsum, rounded; norms are of what is stored), rstd[t] = 1 / sqrt(mean over h of s^2 + eps),
  * out = s * rstd * gamma.  residual NULL: s is x, and xsum is not written.  x, residual, xsum, out [T,h], gamma [h] in the storage type;
- * xsum may be x or residual.  h a multiple of 8, <= 32768. */
+ * xsum may be x or residual, and is not out.  h a multiple of 8, <= 32768. */
 int mtnlg_rmsnorm_fwd(int dtype, int64_t T, int64_t h, const void *x, const void *residual, const void *gamma, float eps,
                       void *xsum, void *out, float *rstd, void *stream);
 /* The same with the result in 8 bits: out [T,h] holds e4m3 codes (bias 7, no infinities, 448 the largest) of s * rstd * gamma / scale,

@@ -507,6 +507,7 @@ int mtnlg_rmsnorm_fwd(int dtype, int64_t T, int64_t h, const void *x, const void
   if (!x || !gamma || !out || !rstd || (residual && !xsum)) return MTNLG_NULL_POINTER;
   MTNLG_TRY(check_norm(dtype, T, h));
   if (!(eps >= 0.0f && eps < INFINITY) || unaligned({x, residual, gamma, xsum, out}) || ((uintptr_t)rstd & 3)) return MTNLG_INVALID_ARG;
+  if (residual && out == xsum) return MTNLG_INVALID_ARG;   // the sum would be lost
   const NormArgs a{T, (int)h, x, residual, gamma, xsum, out, eps, rstd, nullptr, 0, 0};
   return dtype == MTNLG_F32 ? fwd_launch<float, false>(a, (hipStream_t)stream) : fwd_launch<bf16, false>(a, (hipStream_t)stream);
 }

@@ -198,6 +198,11 @@ def test_norms_that_are_refused():
     assert bwd(n=size - 1) == SMALL and bwd(ws=None) == NULL and bwd(T=0) == INVALID and bwd(h=20) == SHAPE and bwd(dx=ctypes.c_void_p(2)) == INVALID
 
 
+def test_a_norm_over_its_sum_is_refused():
+    # the stored sum is what the backward pass needs
+    assert B.lib().mtnlg_rmsnorm_fwd(1, I64(4), I64(16), ONE, TWO, ONE, F32(1e-5), THREE, THREE, ONE, None) == INVALID
+
+
 def test_the_binding_refuses_what_it_can_see():
     q, k = torch.zeros(5, 4, 64), torch.zeros(5, 2, 64)
     with pytest.raises(ValueError):
