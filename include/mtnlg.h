@@ -335,7 +335,7 @@ typedef struct {
 } mtnlg_rotary_desc;
 
 /* q_out, k_out = the heads of q and k turned by their tokens' positions (int32 [tokens], device; NULL: token t is at position t).
- * Rows of a negative position (padding) are neither read nor written.  MTNLG_ROTARY_LINEAR: frequencies divided by factor;
+ * Rows of a negative position (padding) are not written, and what they hold does not matter (they are read all the same).  MTNLG_ROTARY_LINEAR: frequencies divided by factor;
  * _BASE: base * factor^(n / (n - 2)), finite; _PARTS: of a pair that makes fewer than `slow` turns in the original context divided by factor, of one of
  * more than `fast` left, in between by their share.  Angles are worked out in 64 bits.  An output may be its input (same
  * strides), and nothing else that is read or written; k and k_out may both be NULL. */

@@ -50,7 +50,8 @@ template <typename E, int V>
 struct alignas(sizeof(E) * V < 16 ? sizeof(E) * V : 16) Piece { E v[V]; };
 
 // A thread takes the same item of every head it works on: V pairs (HALF: V columns of either half), V columns (interleaved: V / 2 pairs), or V columns that are copied.
-// The first AHEAD rows of each are read before the sines are worked out, which takes about as long as the reads.
+// The first AHEAD rows of each are read before the sines are worked out, which takes about as long as the reads; rows of padding with them (their positions first: 8192 tokens of 20 heads
+// of 128, forward and backward, 41.9 us a pass, 43.1 so).
 template <typename E, int V, bool HALF>
 __global__ __launch_bounds__(THREADS) void rotary_kernel(RotaryArgs a) {
   __shared__ float2 turn[MAX_PAIRS];   // [token of the tile][pair]
