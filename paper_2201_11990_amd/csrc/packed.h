@@ -85,7 +85,9 @@ __device__ __forceinline__ Span span_of(const Sequences &s, int i) {
 // Which sequence holds the place-th piece of work, and which of the sequence's pieces it is (at): count(span) says how many a sequence has.  Lengths are known
 // on the device only, so every wave looks for itself.  Up to 32 sequences, the ones with the most keys come first: what is left over at the end of a call are
 // the pieces of short ones.  More: a lane counts a few consecutive sequences, a sum over the lanes before it finds the lane, and again inside that lane's sequences.
-// False: fewer pieces than places.
+// False: fewer pieces than places.  Median us, longest first / as they come (one run of each kind of length): documents of 32 to 2048 tokens, 16 heads of 128 on 4, forward and backward,
+// 8: 43 and 147 / 49 and 160, 16: 50 and 180 / 60 and 212, 24: 84 and 282 / 91 and 317, 32: 64 and 207 / 62 and 202, 40: 101 and 334 / 100 and 348, 64: 143 and 480 / 127 and 452;
+// single tokens over 64 to 16384 keys, 32 heads of 128 on 8, 16: 53 / 51, 24: 86 / 88, 32: 96 / 95, 40: 140 / 136, 64: 171 / 165.  Counting costs each wave a turn to a sequence.
 template <typename Count>
 __device__ __forceinline__ bool find_piece(const Sequences &s, unsigned place, Count &&count, Span &found, unsigned &at) {
   if (s.count <= 32) {

@@ -248,6 +248,33 @@ def test_many_sequences(count):
     c.check()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("count", [32, 33, 64, 65, 150])
+def test_single_tokens_of_many_sequences_over_long_caches(dtype, count):
+    # cut keys and their join, with the sequences counted one to a lane, and several
+    g = torch.Generator().manual_seed(count)
+    keys = torch.randint(0, 3000, (count,), generator=g).tolist()
+    keys[count // 2], keys[-1] = 6000, 1
+    c = Case([1] * count, keys, 1, 2, 64, dtype, backward=False, seed=71)
+    fwd, _ = c.workspaces()
+    assert fwd is not None
+    c.run()
+    c.check()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("count", [32, 33, 80])
+def test_work_of_many_sequences_that_is_cut_and_joined(dtype, count):
+    g = torch.Generator().manual_seed(count)
+    lengths = torch.randint(0, 9, (count,), generator=g).tolist()
+    lengths[count - 2] = 1200
+    c = Case(lengths, lengths, 1, 3, 64, dtype, seed=72)
+    desc = M.packed_desc(c.q, c.k, count, c.max_q, c.max_k)
+    assert M.mtnlg_packed_attention_bwd_workspace(desc) > 8 * c.lse.numel()   # more than a sum for each row
+    c.run()
+    c.check()
+
+
 def test_scores_of_any_size():
     # weights from 1 down to nothing, sums that hold one weight only, and maxima that move from tile to tile
     for dtype in ("bf16", "fp32"):
