@@ -365,6 +365,7 @@ typedef struct {
  * prompt or a document; lq < lk: a prompt continued, a single token; lq > lk: the first queries see none).  a = softmax(scale q k^T) v,
  * lse [heads][q_tokens] float = log sum exp; a query that sees no key: a = 0, lse = -infinity.  Rows of no sequence are neither read nor
  * written; what a query does not see, infinities and NaN included, does not reach its results.
+ * bf16: softmax weights, and backward the gradients of scores, round to bf16 before the products that sum them, at every head size (mtnlg_attention_*: at 64, 128 and 160 only).
  * workspace (nullable, 16-byte aligned): mtnlg_packed_attention_fwd_workspace() bytes of scratch that lets calls of few queries cut long sequences
  * of keys; 0 for calls that have no use for it. */
 size_t mtnlg_packed_attention_fwd_workspace(const mtnlg_packed_desc *desc);

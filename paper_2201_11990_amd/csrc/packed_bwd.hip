@@ -4,16 +4,17 @@
 //   dk = scale sum dS^T q,  dv = sum P^T da
 //
 // Two kernels, in the order of attention_bwd.hip: dq (and D), which owns rows (token, head of the group) as the forward kernel does and streams K and V, and dk / dv, which owns
-// keys and streams Q and dO of one head of the group after the other.  No atomics: where the keys alone leave units idle, the heads of a group are dealt out over workgroups,
-// whose sums packed.hip adds up in their order.  Keys that no query sees get zeros.
+// keys and streams Q and dO of one head of the group after the other.  No atomics: where the keys alone leave units idle, the tiles of a block of keys (of all heads of the group, one
+// head after the other) are dealt out in parts to several workgroups, whose sums packed.hip adds up in their order.  Keys that no query sees get zeros.
 //
-// P and dS round to bf16 before the products that sum them up (2^-8 of each term at most, as each result once more), D and all sums are fp32.  D is worked out from the
-// stored a, which is rounded: forward keeps no other.  All in all dq and dk are off by 0.0025 to 0.0031 of their norm, 0.0017 of that by their own rounding.
+// P and dS round to bf16 before the products that sum them up (2^-8 of each term at most, as each result once more), since as three bf16 parts that keep all bits those products would be three times as long; D and
+// all sums are fp32.  D is worked out from the stored a, which is rounded: forward keeps no other.  All in all dq and dk are off by 0.0025 to 0.0031 of their norm, 0.0017 of that by their own
+// rounding.  (The dense kernels round P and dS at heads of 64, 128 and 160 only, and cut them into parts at others: 1024 keys, heads of 72 to 256, dq off by 0.0018 there and 0.0025 here.)
 //
-// Bound by the matrix pipes, the seven products of which two (S and dP) are taken in both kernels: one kernel for all would add up either dq or dk and dv through atomics, whose
-// order changes results, or through memory (a part of dq to every block of keys).  Four sequences of 384 to 9001 tokens, 32 heads of 128 on 8: dq 1120 us, 1.2 PFLOP/s, pipes
-// busy 72 % of the time; dk / dv 1890 us, 0.95 PFLOP/s, 50 %.  Without its fragments' reads, DMA, exponentials and the exchange that loop took 1332 us of 2020, without one of the
-// first two 1790 to 1850, without one of the others 1870 to 1970: nothing of it stands out.  Eight of 77 to 2048, 16 heads on 4: 96 and 160 us; 2501 and 1589 tokens, 16 heads of 160: 97 and 128 us.
+// Seven products, of which two (S and dP) are taken in both kernels: one kernel for all would add up either dq or dk and dv through atomics, whose
+// order changes results, or through memory (a part of dq to every block of keys).  Four sequences of 384 to 9001 tokens, 32 heads of 128 on 8: dq 1110 us, 1.2 PFLOP/s, bound by the matrix
+// pipes, which are busy 75 % of the time; dk / dv 1850 us, 0.95 PFLOP/s, 53 %, not by one thing alone.  Without its fragments' reads, DMA, exponentials and the exchange that loop took 1332 us of 2020, without one of the
+// first two 1790 to 1850, without one of the others 1870 to 1970: nothing of it stands out.  Eight of 77 to 2048, 16 heads on 4: 98 and 160 us, pipes busy 47 and 41 %; 2501 and 1589 tokens, 16 heads of 160: 98 and 128 us, 46 and 44 %.
 #include "packed.h"
 
 namespace mtnlg {

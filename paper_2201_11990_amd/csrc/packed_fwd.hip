@@ -8,10 +8,11 @@
 // streamed tile as A operand, 32 own rows to a wave as B, P from one product to the next in registers, fragments read a few steps ahead across the end of a tile).
 // Calls of few rows cut the keys into chunks, whose results packed.hip joins.
 //
-// P rounds to bf16 before its product (2^-8 of each term at most, as the result once more); scores, maxima, sums and results are fp32.
+// P rounds to bf16 before its product (2^-8 of each term at most, as the result once more): as three bf16 parts that keep all bits that product would be three times as long.  Scores, maxima, sums and results are fp32.
+// (packed_bwd.hip: where the dense kernels do not round.)
 //
 // Bound by the matrix and vector pipes alike: 64 keys and 128 rows of 128 are 32 MFMAs and 168 vector instructions to a wave, 34 of them exponentials at a quarter of
-// the rate.  Four sequences of 384 to 9001 tokens, 32 heads of 128 on 8: 869 us, 1.04 PFLOP/s of what is not masked, matrix pipes busy 57 % of the time (a large product of the
+// the rate.  Four sequences of 384 to 9001 tokens, 32 heads of 128 on 8: 869 us, 1.04 PFLOP/s of what is not masked, matrix pipes busy 59 % of the time (a large product of the
 // library reaches 1.2 PFLOP/s on this card); eight of 77 to 2048, 16 heads on 4: 73 us, 0.67 PFLOP/s, 39 %, since pieces are short; 2501 and 1589 tokens, 16 heads of 160: 71 us.
 // Single tokens read K and V once: 32 of them over 64 to 15872 keys, 425 MB in 88 us, 4.8 TB/s, and 8 us for the join.
 #include "packed.h"

@@ -1,7 +1,7 @@
 // Attention over packed sequences in the order of its formulas, without a schedule of its own: fp32 on v_mfma_f32_32x32x2_f32 with P and dS in fp32, and bf16
 // of head sizes above 192 (packed_fwd.hip, packed_bwd.hip: the others).
 //
-// fp32 is bound by the matrix pipes, 64 cycles to an instruction: a workgroup alone on a unit takes 6.6 us for 64 keys of 96 columns, 5.1 of them MFMAs.  Small calls by how
+// fp32 instructions take 64 cycles on the matrix pipes: a workgroup alone on a unit takes 6.6 us for 64 keys of 96 columns, 5.1 of them MFMAs.  Small calls are bound by how
 // their pieces come out: 1536 tokens in 4 documents, 8 heads of 96 on 4, in chunks: forward 36 us and 10 for the join, dq 53 and 8, dk / dv 59 and 8, pipes busy 45 to 52 % of the time.
 #include "packed.h"
 
