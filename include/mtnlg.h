@@ -380,6 +380,31 @@ int mtnlg_packed_attention_bwd(const mtnlg_packed_desc *desc, const mtnlg_packed
                                const mtnlg_heads *da, const mtnlg_heads *dq, const mtnlg_heads *dk, const mtnlg_heads *dv,
                                void *workspace, size_t workspace_bytes, void *stream);
 
+/* --- gated feed-forward block: the layer's feed-forward part with two projections, one of which passes an activation and multiplies the other ---- */
+
+enum mtnlg_gate { MTNLG_GATE_SILU = 0, MTNLG_GATE_GELU_TANH = 1, MTNLG_GATE_GELU_ERF = 2 };
+typedef struct {
+  int32_t dtype;    /* MTNLG_F32 or MTNLG_BF16                                                    */
+  int32_t gate;     /* mtnlg_gate                                                               */
+  int64_t tokens;   /* T, <= 2^22 - 64                                                            */
+  int32_t hidden;   /* h, a multiple of 8, <= 32768                                               */
+  int32_t ffn;      /* F, a multiple of 8, <= 2^20                                                */
+  uint32_t flags;   /* backward: MTNLG_ACCUMULATE_WGRAD, MTNLG_WGRAD_FP32                         */
+} mtnlg_gated_desc;
+
+/* z = x w_fc1^T [T,2F];  g = act(z[:, :F]) * z[:, F:] [T,F];  y = g w_fc2^T [T,h], under tensor slicing a row-parallel partial sum as that of
+ * FC2 above.  w_fc1 [2F,h]: the F rows of the gate, then the other projection's; w_fc2 [h,F].  All matrices dense, in the storage type.
+ * z is what backward reads, stored rounded; NULL: it is not kept (a model in use).  g is of z before its rounding; y of g as stored.
+ * workspace (16-byte aligned; nullable where its size is 0): mtnlg_gated_ffn_workspace() bytes for either pass, contents destroyed.  Outputs and workspace lie on no other argument. */
+size_t mtnlg_gated_ffn_workspace(const mtnlg_gated_desc *desc);
+int mtnlg_gated_ffn_fwd(const mtnlg_gated_desc *desc, const void *x, const void *w_fc1, const void *w_fc2, void *z, void *g, void *y,
+                        void *workspace, size_t workspace_bytes, void *stream);
+/* Adjoint, from forward's z and g: dg = dy w_fc2 (not stored);  dz = [dg * z[:, F:] * act'(z[:, :F]), dg * act(z[:, :F])] [T,2F], out, rounded;
+ * dx = dz w_fc1 [T,h];  dw_fc1 = dz^T x;  dw_fc2 = dy^T g, overwritten or (MTNLG_ACCUMULATE_WGRAD) added to, float under MTNLG_WGRAD_FP32.
+ * dx, dw_fc1, dw_fc2: each NULL where it is not wanted.  Run-to-run identical. */
+int mtnlg_gated_ffn_bwd(const mtnlg_gated_desc *desc, const void *x, const void *w_fc1, const void *w_fc2, const void *z, const void *g,
+                        const void *dy, void *dz, void *dx, void *dw_fc1, void *dw_fc2, void *workspace, size_t workspace_bytes, void *stream);
+
 /* --- first and last pipeline stage's extras (the paper names the GPT-2 decoder, Section 3.2, and
  *     prints none of this: token embedding E [V,h] with learned positions P [s,h], final LayerNorm,
  *     output projection tied to E, next-token cross-entropy).  Under the tensor slicing of
@@ -454,6 +479,41 @@ int mtnlg_grad_sqnorm(int64_t count, const float *grad, void *workspace, float *
  * out of range, alignment), MTNLG_HIP_ERROR. */
 int mtnlg_adam_step(const mtnlg_adam_desc *desc, int64_t count, float *master, float *m, float *v,
                     const float *grad, void *weight_bf16, const float *sqnorm, void *stream);
+
+/* --- the same over many tensors at once: one launch for up to 46 of them, gradients in float or bf16, the moments in float or in 8 bits -------- */
+typedef struct {
+  int64_t count;               /* elements, <= 2^39                                                           */
+  float *master;               /* fp32 weight, updated                                                        */
+  void *m, *v;                 /* moments, updated: float [count], or codes [count] (below)                   */
+  float *m_scale, *v_scale;    /* 8 bits: [ceil(count / 256)], updated; else not looked at                    */
+  const void *grad;            /* float or bf16, not modified                                                 */
+  void *weight_bf16;           /* nullable: master rounded to nearest even                                    */
+  int32_t decay;               /* 0: weight_decay does not apply (gains, biases)                              */
+} mtnlg_adam_tensor;
+typedef struct {
+  mtnlg_adam_desc adam;
+  int32_t tensors;             /* <= 2^16                                                                     */
+  int32_t grad_dtype;          /* MTNLG_F32 or MTNLG_BF16                                                     */
+  int32_t state_bits;          /* 32 or 8                                                                     */
+  uint64_t seed;               /* 8 bits: with adam.step, of the random numbers that codes are rounded by     */
+} mtnlg_adam_many_desc;
+
+/* mtnlg_grad_sqnorm over the gradients of all tensors (of `tensors` entries the fields count and grad): one launch up to 16 * 4096
+ * elements, else one per 160 tensors and one more.  Elements are added in a fixed order, in 64 bits.  grad 16-byte aligned (bf16: 8). */
+size_t mtnlg_grad_sqnorm_many_workspace(void);
+int mtnlg_grad_sqnorm_many(int32_t tensors, const mtnlg_adam_tensor *of, int grad_dtype, void *workspace, size_t workspace_bytes, float *sqnorm,
+                           int accumulate, void *stream);
+/* mtnlg_adam_step on every tensor.  sqnorm given and not finite: nothing is changed (the step is left out), decided on the device.
+ * state_bits 8: m is held as e4m3 codes (bias 7, 448 the largest) times a float scale per 256 consecutive elements, sqrt(v) likewise in v
+ * and v_scale (a step squares it, and takes the root of the new v before it rounds).  scale = the block's largest magnitude / 448 (1 where all
+ * are zeros, else 2^-126 at least).  A quotient by the scale becomes the code below or above it: with steps of 2^(e - 3), e the
+ * quotient's exponent or -6 where that is more, floor(quotient / step + u) steps, u in (0, 1) a random number (16 bits and a half) of seed,
+ * adam.step, the block's number among all tensors' blocks and the element's in its block: the same call gives the same codes.  A root that is not zero is one step at
+ * least, so that no update divides by a lost one.  The update itself uses the new moments before they are rounded.  NaN gives the code of NaN; squares of gradients have to be
+ * finite.  Codes of zero with any scale are zero: a program begins with codes 0.
+ * Alignment: master 16 bytes, m and v 16 (codes: 4), grad 16 (bf16: 8), weight_bf16 8.  What is written lies on nothing else of the call (the same tensor twice is
+ * MTNLG_INVALID_ARG). */
+int mtnlg_adam_step_many(const mtnlg_adam_many_desc *desc, const mtnlg_adam_tensor *of, const float *sqnorm, void *stream);
 
 /* --- per-kernel-class timing (optional) --------------------------------------
  * While enabled, the library records a HIP event on the launch stream after each

@@ -21,6 +21,7 @@ GELU_TANH, GELU_ERF = 0, 1
 RECOMPUTE, ACCUMULATE_WGRAD, WGRAD_FP32 = 1, 2, 4
 GEMM_NT, GEMM_NN, GEMM_TN = 0, 1, 2
 EPI_BIAS, EPI_GELU, EPI_RESIDUAL, EPI_ACCUMULATE, EPI_OUT_F32, EPI_GELU_ERF, EPI_GELU_GRAD = 1, 2, 4, 8, 16, 32, 64
+GATE_SILU, GATE_GELU_TANH, GATE_GELU_ERF = 0, 1, 2
 ROTARY_HALF, ROTARY_INTERLEAVED = 0, 1
 ROTARY_UNSCALED, ROTARY_LINEAR, ROTARY_BASE, ROTARY_PARTS = 0, 1, 2, 3
 KERNEL_CLASSES = ("gemm_nt", "gemm_nn", "gemm_tn", "attn_fwd", "attn_bwd", "ln_fwd", "ln_bwd",
@@ -46,6 +47,22 @@ class LayerDesc(ctypes.Structure):
 class AdamDesc(ctypes.Structure):
     _fields_ = [("lr", ctypes.c_float), ("beta1", ctypes.c_float), ("beta2", ctypes.c_float), ("eps", ctypes.c_float),
                 ("weight_decay", ctypes.c_float), ("max_grad_norm", ctypes.c_float), ("step", ctypes.c_int32)]
+
+
+class AdamTensor(ctypes.Structure):
+    _fields_ = [("count", ctypes.c_int64), ("master", ctypes.c_void_p), ("m", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("m_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("weight_bf16", ctypes.c_void_p),
+                ("decay", ctypes.c_int32)]
+
+
+class AdamManyDesc(ctypes.Structure):
+    _fields_ = [("adam", AdamDesc), ("tensors", ctypes.c_int32), ("grad_dtype", ctypes.c_int32), ("state_bits", ctypes.c_int32),
+                ("seed", ctypes.c_uint64)]
+
+
+class GatedDesc(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("gate", ctypes.c_int32), ("tokens", ctypes.c_int64), ("hidden", ctypes.c_int32),
+                ("ffn", ctypes.c_int32), ("flags", ctypes.c_uint32)]
 
 
 class HeadDesc(ctypes.Structure):
@@ -156,6 +173,12 @@ def lib():
             "mtnlg_packed_attention_fwd": (ctypes.c_int, [vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]),
             "mtnlg_packed_attention_bwd_workspace": (sz, [ctypes.POINTER(PackedDesc)]),
             "mtnlg_packed_attention_bwd": (ctypes.c_int, [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]),
+            "mtnlg_gated_ffn_workspace": (sz, [ctypes.POINTER(GatedDesc)]),
+            "mtnlg_gated_ffn_fwd": (ctypes.c_int, [ctypes.POINTER(GatedDesc), vp, vp, vp, vp, vp, vp, vp, sz, vp]),
+            "mtnlg_gated_ffn_bwd": (ctypes.c_int, [ctypes.POINTER(GatedDesc), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]),
+            "mtnlg_grad_sqnorm_many_workspace": (sz, []),
+            "mtnlg_grad_sqnorm_many": (ctypes.c_int, [i32, vp, ctypes.c_int, vp, sz, vp, ctypes.c_int, vp]),
+            "mtnlg_adam_step_many": (ctypes.c_int, [ctypes.POINTER(AdamManyDesc), vp, vp, vp]),
             "mtnlg_calibrate_mfma_operand_bytes": (sz, [ctypes.c_int]),
             "mtnlg_calibrate_mfma_flops": (i64, [ctypes.c_int, ctypes.c_int]),
             "mtnlg_calibrate_mfma": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, vp, vp, vp]),
@@ -182,6 +205,8 @@ EXPORTED = ("mtnlg_version", "mtnlg_status_string", "mtnlg_layer_desc_check", "m
             "mtnlg_rmsnorm_fwd", "mtnlg_rmsnorm_fwd_e4m3", "mtnlg_rmsnorm_bwd_workspace", "mtnlg_rmsnorm_bwd",
             "mtnlg_rotary_fwd", "mtnlg_rotary_bwd", "mtnlg_packed_attention_fwd_workspace", "mtnlg_packed_attention_fwd",
             "mtnlg_packed_attention_bwd_workspace", "mtnlg_packed_attention_bwd",
+            "mtnlg_gated_ffn_workspace", "mtnlg_gated_ffn_fwd", "mtnlg_gated_ffn_bwd",
+            "mtnlg_grad_sqnorm_many_workspace", "mtnlg_grad_sqnorm_many", "mtnlg_adam_step_many",
             "mtnlg_calibrate_mfma_operand_bytes", "mtnlg_calibrate_mfma_flops", "mtnlg_calibrate_mfma",
             "mtnlg_calibrate_copy", "mtnlg_profile_enable", "mtnlg_profile_pause", "mtnlg_profile_read")
 
@@ -686,6 +711,57 @@ def mtnlg_packed_attention_bwd(q, k, v, a, lse, da, dq, dk, dv, q_offsets, k_off
                                             h + 192, h + 224, _dense(workspace), _nbytes(workspace), stream), "mtnlg_packed_attention_bwd")
 
 
+def gated_desc(x, w_fc1, gate=GATE_SILU, flags=0):
+    """Sizes of calls of the gated feed-forward block: x [tokens, hidden], w_fc1 [2 ffn, hidden]."""
+    if x.dim() != 2 or w_fc1.dim() != 2 or w_fc1.shape[0] % 2 or w_fc1.shape[1] != x.shape[1]:
+        raise ValueError("x: [tokens, hidden], w_fc1: [2 ffn, hidden]")
+    return GatedDesc(_dtype_code(x), gate, x.shape[0], x.shape[1], w_fc1.shape[0] // 2, flags)
+
+
+def mtnlg_gated_ffn_workspace(desc):
+    return lib().mtnlg_gated_ffn_workspace(ctypes.byref(desc))
+
+
+def _gated(desc, x, w_fc1, w_fc2):
+    """Storage type, tokens, hidden and ffn of a call whose inputs are what the descriptor says."""
+    dtype, T, h, F = x.dtype, desc.tokens, desc.hidden, desc.ffn
+    if _dtype_code(x) != desc.dtype:
+        raise ValueError("x: of another type than the descriptor's")
+    _like(x, dtype, (T, h), "x")
+    _like(w_fc1, dtype, (2 * F, h), "w_fc1")
+    _like(w_fc2, dtype, (h, F), "w_fc2")
+    return dtype, T, h, F
+
+
+def mtnlg_gated_ffn_fwd(desc, x, w_fc1, w_fc2, z, g, y, workspace=None):
+    """x, y: [T, h]; w_fc1: [2 F, h]; w_fc2: [h, F]; z (nullable): [T, 2 F]; g: [T, F]."""
+    stream = _device_stream(x, w_fc1, w_fc2, z, g, y, workspace)
+    dtype, T, h, F = _gated(desc, x, w_fc1, w_fc2)
+    if z is not None:
+        _like(z, dtype, (T, 2 * F), "z")
+    _like(g, dtype, (T, F), "g")
+    _like(y, dtype, (T, h), "y")
+    _check(lib().mtnlg_gated_ffn_fwd(ctypes.byref(desc), _dense(x), _dense(w_fc1), _dense(w_fc2), _dense(z), _dense(g), _dense(y),
+                                     _dense(workspace), _nbytes(workspace) if workspace is not None else 0, stream), "mtnlg_gated_ffn_fwd")
+
+
+def mtnlg_gated_ffn_bwd(desc, x, w_fc1, w_fc2, z, g, dy, dz, dx, dw_fc1, dw_fc2, workspace=None):
+    """As forward; dz: [T, 2 F], dx (nullable): [T, h], dw_fc1, dw_fc2 (nullable): as the weights, fp32 under WGRAD_FP32."""
+    stream = _device_stream(x, w_fc1, w_fc2, z, g, dy, dz, dx, dw_fc1, dw_fc2, workspace)
+    dtype, T, h, F = _gated(desc, x, w_fc1, w_fc2)
+    _like(z, dtype, (T, 2 * F), "z")
+    _like(g, dtype, (T, F), "g")
+    _like(dy, dtype, (T, h), "dy")
+    _like(dz, dtype, (T, 2 * F), "dz")
+    wide = torch.float32 if desc.flags & WGRAD_FP32 else dtype
+    for t, kind, shape, what in ((dx, dtype, (T, h), "dx"), (dw_fc1, wide, (2 * F, h), "dw_fc1"), (dw_fc2, wide, (h, F), "dw_fc2")):
+        if t is not None:
+            _like(t, kind, shape, what)
+    _check(lib().mtnlg_gated_ffn_bwd(ctypes.byref(desc), _dense(x), _dense(w_fc1), _dense(w_fc2), _dense(z), _dense(g), _dense(dy), _dense(dz),
+                                     _dense(dx), _dense(dw_fc1), _dense(dw_fc2), _dense(workspace),
+                                     _nbytes(workspace) if workspace is not None else 0, stream), "mtnlg_gated_ffn_bwd")
+
+
 def mtnlg_grad_sqnorm_workspace():
     return lib().mtnlg_grad_sqnorm_workspace()
 
@@ -707,6 +783,76 @@ def mtnlg_adam_step(master, m, v, grad, weight_bf16=None, sqnorm=None, *, lr, st
     d = AdamDesc(lr, beta1, beta2, eps, weight_decay, max_grad_norm, step)
     _check(lib().mtnlg_adam_step(ctypes.byref(d), master.numel(), _p(master), _p(m), _p(v), _p(grad), _p(weight_bf16),
                                  _p(sqnorm), _stream()), "mtnlg_adam_step")
+
+
+class AdamTensors:
+    """Marshalled table of the tensors of mtnlg_grad_sqnorm_many and mtnlg_adam_step_many, built once and reused per step.
+
+    Each a dict: "master" fp32, "grad" fp32 or bf16 (the same in all), "m" and "v" fp32, or float8_e4m3fn (in all) with "m_scale" and "v_scale",
+    fp32 of one element to 256; "weight_bf16" (optional), "decay" (default true): whether weight decay applies.  For the norm alone "grad" is enough."""
+
+    def __init__(self, tensors):
+        if not tensors:
+            raise ValueError("no tensors")
+        first = tensors[0]
+        self.grad_dtype, self.device = _dtype_code(first["grad"]), first["grad"].get_device()
+        eight = first.get("m") is not None and first["m"].dtype == torch.float8_e4m3fn
+        self.state_bits = 8 if eight else 32
+        self.steps = all(t.get(k) is not None for t in tensors for k in ("master", "m", "v"))
+        self.table = (AdamTensor * len(tensors))()
+        for row, t in zip(self.table, tensors):
+            n = t["grad"].numel()
+            kinds = {"grad": first["grad"].dtype}
+            if self.steps:
+                state = torch.float8_e4m3fn if eight else torch.float32
+                kinds.update(master=torch.float32, m=state, v=state)
+                if eight:
+                    kinds.update(m_scale=torch.float32, v_scale=torch.float32)
+                if t.get("weight_bf16") is not None:
+                    kinds["weight_bf16"] = torch.bfloat16
+            row.count, row.decay = n, int(bool(t.get("decay", True)))
+            for name, dtype in kinds.items():
+                x = t[name]
+                count = -(-n // 256) if name.endswith("_scale") else n
+                if x.dtype != dtype or x.numel() != count or not x.is_cuda or x.get_device() != self.device:
+                    raise ValueError(f"{name}: expected {count} elements of {dtype} on device {self.device}, got {x.numel()} of {x.dtype} on {x.device}")
+                setattr(row, name, _dense(x))
+        self._keep = [dict(t) for t in tensors]
+
+    def __len__(self):
+        return len(self.table)
+
+
+def _adam_tensors(tensors):
+    t = tensors if isinstance(tensors, AdamTensors) else AdamTensors(tensors)
+    if t.device != torch.cuda.current_device():
+        raise ValueError("tensors handed to the library must be on the current device")
+    return t
+
+
+def mtnlg_grad_sqnorm_many_workspace():
+    return lib().mtnlg_grad_sqnorm_many_workspace()
+
+
+def mtnlg_grad_sqnorm_many(tensors, sqnorm, workspace, accumulate=False):
+    """tensors: AdamTensors, or a list of its dicts; sqnorm: fp32 device tensor of one element."""
+    t = _adam_tensors(tensors)
+    stream = _device_stream(sqnorm, workspace)
+    _like(sqnorm, torch.float32, (1,), "sqnorm")
+    _check(lib().mtnlg_grad_sqnorm_many(len(t), t.table, t.grad_dtype, _dense(workspace), _nbytes(workspace), _dense(sqnorm),
+                                        int(bool(accumulate)), stream), "mtnlg_grad_sqnorm_many")
+
+
+def mtnlg_adam_step_many(tensors, sqnorm=None, *, lr, step, beta1=0.9, beta2=0.95, eps=1e-8, weight_decay=0.1, max_grad_norm=1.0, seed=0):
+    """In-place Adam update of many tensors (AdamTensors, or a list of its dicts); seed: of the rounding of states in 8 bits."""
+    t = _adam_tensors(tensors)
+    if not t.steps:
+        raise ValueError("every tensor needs master, m and v")
+    stream = _device_stream(sqnorm)
+    if sqnorm is not None:
+        _like(sqnorm, torch.float32, (1,), "sqnorm")
+    d = AdamManyDesc(AdamDesc(lr, beta1, beta2, eps, weight_decay, max_grad_norm, step), len(t), t.grad_dtype, t.state_bits, seed)
+    _check(lib().mtnlg_adam_step_many(ctypes.byref(d), t.table, _dense(sqnorm), stream), "mtnlg_adam_step_many")
 
 
 def mtnlg_calibrate_mfma_operand_bytes(workgroups):

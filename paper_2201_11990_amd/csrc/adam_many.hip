@@ -1,0 +1,411 @@
+// The optimizer step over many tensors at once, with the moments in fp32 or in 8 bits, and the squared norm of all their gradients.
+//
+// A model's parameters are a few large tensors and many small ones (gains, biases), and a launch for each is what the small ones cost.
+// Here the addresses and sizes of up to kStepTensors tensors travel in the launch's arguments (no table in device memory, nothing to copy before the
+// call), every tensor is cut into chunks of 4096 elements, and a workgroup finds its chunk's tensor by a binary search through uniform values.
+//
+// States in 8 bits: e4m3 codes of m and of r = sqrt(v), with one fp32 scale each to a block of 256 elements, which is what a wave takes at 4
+// elements a lane, so that a block's largest magnitude is one reduction over the wave.  r and not v: a code's range (2^-9 .. 448 times the scale) then spans
+// 10 decades of v, and a step is at most 1/8 of r as it is of m.  Codes are rounded up with the probability of the part of a step that is left: rounded to
+// nearest, a moment whose change in a step is below half a code (beta2 = 0.95 takes 5 % of v, 2.5 % of r; a code is 6 to 12 % wide) would never move.
+#include <algorithm>
+#include <new>
+
+#include "adam.h"
+
+namespace mtnlg {
+
+namespace {
+
+constexpr int kBlock = 256;                // elements that share a scale
+constexpr int kChunk = 4096;               // elements of a workgroup's turn: 4 vectors of 4 a thread
+constexpr int kTurns = kChunk / 1024;
+constexpr int kStepTensors = 46, kNormTensors = 160;   // per launch: what 4 KB of arguments hold
+constexpr int kNormBlocks = 2048;          // partial sums at most
+constexpr uint32_t kOnce = 16;             // chunks up to which one workgroup takes all
+constexpr int32_t kMostTensors = 1 << 16;
+
+struct StepTensor {
+  float *p;
+  void *m, *v;
+  float *m_scale, *v_scale;
+  const void *g;
+  bf16 *w;
+  int64_t count;
+  uint32_t first_chunk, first_block;   // of this launch; of the call
+  float wd;
+  uint32_t pad;
+};
+struct StepArgs {
+  AdamArgs a;
+  uint32_t key_lo, key_hi, chunks;
+  int32_t tensors;
+  const float *sqnorm;
+  StepTensor of[kStepTensors];
+};
+static_assert(sizeof(StepArgs) <= 4096, "arguments of a launch");
+
+struct NormTensor {
+  const void *g;
+  int64_t count;
+  uint32_t first_chunk, pad;
+};
+struct NormArgs {
+  uint32_t chunks;
+  int32_t tensors;
+  NormTensor of[kNormTensors];
+};
+static_assert(sizeof(NormArgs) + 32 <= 4096, "arguments of a launch");
+
+// the tensor that chunk c is of: the last one that begins at it or before
+template <typename A>
+__device__ __forceinline__ int tensor_of(const A &a, uint32_t c) {
+  int lo = 0, hi = a.tensors;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (a.of[mid].first_chunk <= c) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+
+// elements i .. i + 3 of n (zeros beyond), aligned for one access
+template <typename E>
+__device__ __forceinline__ f32x4 load_some(const E *p, int64_t i, int64_t n) {
+  if (i + 4 <= n) return load4(p + i);
+  f32x4 r = {};
+#pragma unroll
+  for (int e = 0; e < 3; ++e)
+    if (i + e < n) r[e] = to_f32(p[i + e]);
+  return r;
+}
+template <typename E>
+__device__ __forceinline__ void store_some(E *p, int64_t i, int64_t n, f32x4 x) {
+  if (i + 4 <= n) {
+    if constexpr (sizeof(E) == 4) *reinterpret_cast<f32x4 *>(p + i) = x;
+    else *reinterpret_cast<bf16x4 *>(p + i) = bf16x4{(bf16)x[0], (bf16)x[1], (bf16)x[2], (bf16)x[3]};
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < 3; ++e)
+    if (i + e < n) p[i + e] = from_f32<E>(x[e]);
+}
+// four codes
+__device__ __forceinline__ uint32_t load_codes(const uint8_t *p, int64_t i, int64_t n) {
+  if (i + 4 <= n) return *reinterpret_cast<const uint32_t *>(p + i);
+  uint32_t r = 0;
+#pragma unroll
+  for (int e = 0; e < 3; ++e)
+    if (i + e < n) r |= (uint32_t)p[i + e] << (8 * e);
+  return r;
+}
+__device__ __forceinline__ void store_codes(uint8_t *p, int64_t i, int64_t n, uint32_t x) {
+  if (i + 4 <= n) {
+    *reinterpret_cast<uint32_t *>(p + i) = x;
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < 3; ++e)
+    if (i + e < n) p[i + e] = (uint8_t)(x >> (8 * e));
+}
+__device__ __forceinline__ f32x4 decode(uint32_t codes, float scale) {
+  const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, true);
+  return f32x4{lo[0] * scale, lo[1] * scale, hi[0] * scale, hi[1] * scale};
+}
+
+// 32 random bits for element e of a block: products, shifts and exclusive ors on the step's two words, the block's number and e.
+__device__ __forceinline__ uint32_t block_key(uint32_t block, uint32_t lo, uint32_t hi) {
+  uint32_t k = block * 0x9E3779B1u + lo;
+  k = (k ^ (k >> 15)) * 0x510E527Fu;
+  return (k ^ (k >> 13)) ^ hi;
+}
+__device__ __forceinline__ uint32_t element_bits(uint32_t key, uint32_t e) {
+  uint32_t h = key + e * 0x3C6EF373u;
+  h = (h ^ (h >> 16)) * 0x6A09E667u;
+  h = (h ^ (h >> 15)) * 0xBB67AE85u;
+  return h ^ (h >> 16);
+}
+
+// The code of x * inv (inv: the reciprocal of the block's scale), rounded up where the part of a step that is left and u = (r + 1/2) / 2^16 make a whole
+// one.  From 2^-6 on a code is the upper bits of the fp32 value, whose other 20 bits are that part; below, codes are multiples of 2^-9, and
+// adding 2^-6 brings the value to where they are the upper bits too.
+template <int LEAST>
+__device__ __forceinline__ uint32_t encode(float x, float inv, uint32_t r) {
+  const float y = fabsf(x) * inv, most = fminf(y, 448.0f);
+  const bool low = most < 0x1p-6f;
+  const uint32_t bits = __builtin_bit_cast(uint32_t, low ? most + 0x1p-6f : most) + (r * 16 + 8);
+  uint32_t code = (bits >> 20) - (low ? 968u : 960u);   // exponents: 127 there, 7 here
+  if (LEAST > 0) code = x != 0.0f && code < (uint32_t)LEAST ? (uint32_t)LEAST : code;
+  code = y == y ? code : 0x7Fu;
+  return code | ((__builtin_bit_cast(uint32_t, x) >> 24) & 0x80u);
+}
+// scale of a block with this largest magnitude
+__device__ __forceinline__ float scale_of(float most) { return most > 0.0f ? fmaxf(most / 448.0f, 0x1p-126f) : 1.0f; }
+
+template <bool EIGHT, typename G>
+__global__ __launch_bounds__(256) void adam_many_kernel(StepArgs s) {
+  float coef = 1.0f;
+  if (s.sqnorm != nullptr) {
+    const float sq = s.sqnorm[0];
+    if (!(fabsf(sq) < INFINITY)) return;   // a gradient that is not finite: the step is left out
+    if (s.a.max_norm > 0.0f) coef = fminf(1.0f, s.a.max_norm / (sqrtf(sq) + 1e-6f));
+  }
+  for (uint32_t c = blockIdx.x; c < s.chunks; c += gridDim.x) {
+    const StepTensor &t = s.of[tensor_of(s, c)];
+    const int64_t n = t.count, first = (int64_t)(c - t.first_chunk) * kChunk + threadIdx.x * 4;
+    AdamArgs a = s.a;
+    a.wd = t.wd;
+#pragma unroll
+    for (int u = 0; u < kTurns; ++u) {
+      const int64_t i = first + u * 1024;
+      f32x4 p = load_some(t.p, i, n), g = load_some(static_cast<const G *>(t.g), i, n), m, v;
+      if constexpr (EIGHT) {
+        if (i - (threadIdx.x & 63) * 4 >= n) break;   // (the whole wave)
+        const int64_t b = i / kBlock;
+        m = decode(load_codes(static_cast<const uint8_t *>(t.m), i, n), t.m_scale[b]);
+        v = decode(load_codes(static_cast<const uint8_t *>(t.v), i, n), t.v_scale[b]);
+        v *= v;
+      } else {
+        m = load_some(static_cast<const float *>(t.m), i, n);
+        v = load_some(static_cast<const float *>(t.v), i, n);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float pe = p[e], me = m[e], ve = v[e];
+        adam_one(a, coef, g[e], pe, me, ve);
+        p[e] = pe;
+        m[e] = me;
+        v[e] = ve;
+      }
+      store_some(t.p, i, n, p);
+      if (t.w != nullptr) store_some(t.w, i, n, p);
+      if constexpr (EIGHT) {
+        const int64_t b = i / kBlock;
+        float mm = 0.0f, rm = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          v[e] = sqrtf(v[e]);
+          mm = fmaxf(mm, fabsf(m[e]));
+          rm = fmaxf(rm, v[e]);
+        }
+        const float ms = scale_of(wave_max(mm)), rs = scale_of(wave_max(rm)), mi = 1.0f / ms, ri = 1.0f / rs;
+        const uint32_t key = block_key(t.first_block + (uint32_t)b, s.key_lo, s.key_hi);
+        uint32_t mc = 0, rc = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t h = element_bits(key, (threadIdx.x & 63) * 4 + e);
+          mc |= encode<0>(m[e], mi, h & 0xFFFFu) << (8 * e);
+          rc |= encode<1>(v[e], ri, h >> 16) << (8 * e);
+        }
+        store_codes(static_cast<uint8_t *>(t.m), i, n, mc);
+        store_codes(static_cast<uint8_t *>(t.v), i, n, rc);
+        if ((threadIdx.x & 63) == 0) {
+          t.m_scale[b] = ms;
+          t.v_scale[b] = rs;
+        }
+      } else {
+        store_some(static_cast<float *>(t.m), i, n, m);
+        store_some(static_cast<float *>(t.v), i, n, v);
+      }
+    }
+  }
+}
+
+// Squares of a chunk's elements, this thread's share
+template <typename G>
+__device__ __forceinline__ double chunk_squares(const NormArgs &s, uint32_t c, int threads) {
+  const NormTensor &t = s.of[tensor_of(s, c)];
+  const int64_t lo = (int64_t)(c - t.first_chunk) * kChunk;
+  double sum = 0.0;
+  for (int64_t i = lo + threadIdx.x * 4; i < lo + kChunk; i += threads * 4) {
+    const f32x4 g = load_some(static_cast<const G *>(t.g), i, t.count);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum += (double)g[e] * g[e];
+  }
+  return sum;
+}
+// partial[block] = the squares of chunks block, block + grid, ..., added to what launches before left in the first `have`
+template <typename G>
+__global__ __launch_bounds__(256) void norm_many_kernel(NormArgs s, double *__restrict__ partial, int have) {
+  double sum = 0.0;
+  for (uint32_t c = blockIdx.x; c < s.chunks; c += gridDim.x) sum += chunk_squares<G>(s, c, 256);
+  sum = workgroup_sum<256>(sum);
+  if (threadIdx.x == 0) partial[blockIdx.x] = (int)blockIdx.x < have ? partial[blockIdx.x] + sum : sum;
+}
+__global__ __launch_bounds__(256) void norm_many_sum(int blocks, const double *__restrict__ partial, float *__restrict__ out, int accumulate) {
+  double s = 0.0;
+#pragma unroll
+  for (int i = 0; i < kNormBlocks / 256; ++i) {
+    const int b = i * 256 + threadIdx.x;
+    s += b < blocks ? partial[b] : 0.0;
+  }
+  s = workgroup_sum<256>(s);
+  if (threadIdx.x == 0) out[0] = (float)(accumulate ? (double)out[0] + s : s);
+}
+// Few elements: the launches are the time, so there is one
+template <typename G>
+__global__ __launch_bounds__(1024) void norm_many_once(NormArgs s, float *__restrict__ out, int accumulate) {
+  double sum = 0.0;
+  for (uint32_t c = 0; c < s.chunks; ++c) sum += chunk_squares<G>(s, c, 1024);
+  sum = workgroup_sum<1024>(sum);
+  if (threadIdx.x == 0) out[0] = (float)(accumulate ? (double)out[0] + sum : sum);
+}
+
+// Bytes that a call reads or writes.
+struct Span {
+  uintptr_t from, to;
+  bool written;
+};
+// Whether no byte that is written is of two spans
+bool spans_apart(Span *s, int64_t n) {
+  std::sort(s, s + n, [](const Span &a, const Span &b) { return a.from < b.from; });
+  uintptr_t any = 0, written = 0;   // ends of the spans so far, of the written ones
+  for (int64_t i = 0; i < n; ++i) {
+    if (s[i].from < (s[i].written ? any : written)) return false;
+    any = std::max(any, s[i].to);
+    if (s[i].written) written = std::max(written, s[i].to);
+  }
+  return true;
+}
+
+int64_t blocks_of(int64_t count) { return (count + kBlock - 1) / kBlock; }
+
+// Which elements a tensor may have: their blocks are counted in 32 bits
+bool count_ok(int64_t count) { return count > 0 && count <= (int64_t)1 << 39; }
+
+// Two words of random numbers' key
+void step_keys(uint64_t seed, int32_t step, uint32_t *lo, uint32_t *hi) {
+  uint64_t s = seed * 0x9E3779B97F4A7C15ull + (uint64_t)step;
+  s = (s ^ (s >> 32)) * 0xBB67AE8584CAA73Bull;
+  s = (s ^ (s >> 29)) * 0x6A09E667F3BCC909ull;
+  s ^= s >> 32;
+  *lo = (uint32_t)s;
+  *hi = (uint32_t)(s >> 32);
+}
+
+}  // namespace
+
+}  // namespace mtnlg
+
+using namespace mtnlg;
+
+extern "C" {
+
+size_t mtnlg_grad_sqnorm_many_workspace(void) { return kNormBlocks * sizeof(double); }
+
+int mtnlg_grad_sqnorm_many(int32_t tensors, const mtnlg_adam_tensor *of, int grad_dtype, void *workspace, size_t workspace_bytes, float *sqnorm,
+                           int accumulate, void *stream) {
+  if (!of || !workspace || !sqnorm) return MTNLG_NULL_POINTER;
+  if (tensors <= 0 || (grad_dtype != MTNLG_F32 && grad_dtype != MTNLG_BF16)) return MTNLG_INVALID_ARG;
+  if (tensors > kMostTensors) return MTNLG_UNSUPPORTED_SHAPE;
+  if (((uintptr_t)workspace & 7) || ((uintptr_t)sqnorm & 3)) return MTNLG_INVALID_ARG;
+  if (workspace_bytes < mtnlg_grad_sqnorm_many_workspace()) return MTNLG_WORKSPACE_TOO_SMALL;
+  const bool f32 = grad_dtype == MTNLG_F32;
+  for (int32_t i = 0; i < tensors; ++i) {
+    if (!of[i].grad) return MTNLG_NULL_POINTER;
+    if (of[i].count <= 0 || ((uintptr_t)of[i].grad & (f32 ? 15 : 7))) return MTNLG_INVALID_ARG;
+    if (!count_ok(of[i].count)) return MTNLG_UNSUPPORTED_SHAPE;
+  }
+  hipStream_t st = (hipStream_t)stream;
+  LaunchScope scope(MTNLG_K_ELEMENTWISE, st);
+  int have = 0;
+  for (int32_t i = 0; i < tensors;) {
+    NormArgs s;
+    uint64_t chunks = 0;
+    int32_t k = 0;
+    for (; i + k < tensors && k < kNormTensors && chunks < ((uint64_t)1 << 31); ++k) {
+      s.of[k] = NormTensor{of[i + k].grad, of[i + k].count, (uint32_t)chunks, 0};
+      chunks += (uint64_t)(of[i + k].count + kChunk - 1) / kChunk;
+    }
+    s.chunks = (uint32_t)chunks;   // (a tensor has up to 2^27)
+    s.tensors = k;
+    if (i == 0 && k == tensors && chunks <= kOnce) {
+      if (f32) norm_many_once<float><<<1, 1024, 0, st>>>(s, sqnorm, accumulate ? 1 : 0);
+      else norm_many_once<bf16><<<1, 1024, 0, st>>>(s, sqnorm, accumulate ? 1 : 0);
+      return check_launch();
+    }
+    const int grid = chunks < kNormBlocks ? (int)chunks : kNormBlocks;
+    if (f32) norm_many_kernel<float><<<grid, 256, 0, st>>>(s, (double *)workspace, have);
+    else norm_many_kernel<bf16><<<grid, 256, 0, st>>>(s, (double *)workspace, have);
+    MTNLG_TRY(check_launch());
+    have = std::max(have, grid);
+    i += k;
+  }
+  norm_many_sum<<<1, 256, 0, st>>>(have, (const double *)workspace, sqnorm, accumulate ? 1 : 0);
+  return check_launch();
+}
+
+int mtnlg_adam_step_many(const mtnlg_adam_many_desc *desc, const mtnlg_adam_tensor *of, const float *sqnorm, void *stream) {
+  if (!desc || !of) return MTNLG_NULL_POINTER;
+  const bool eight = desc->state_bits == 8, f32 = desc->grad_dtype == MTNLG_F32;
+  if (desc->tensors <= 0 || !adam_desc_ok(desc->adam) || (!eight && desc->state_bits != 32) || (!f32 && desc->grad_dtype != MTNLG_BF16))
+    return MTNLG_INVALID_ARG;
+  if (desc->tensors > kMostTensors) return MTNLG_UNSUPPORTED_SHAPE;
+  if ((uintptr_t)sqnorm & 3) return MTNLG_INVALID_ARG;
+  uint64_t blocks = 0;
+  for (int32_t i = 0; i < desc->tensors; ++i) {
+    const mtnlg_adam_tensor &t = of[i];
+    if (!t.master || !t.m || !t.v || !t.grad || (eight && (!t.m_scale || !t.v_scale))) return MTNLG_NULL_POINTER;
+    const uintptr_t states = (uintptr_t)t.m | (uintptr_t)t.v;
+    if (t.count <= 0 || ((uintptr_t)t.master & 15) || ((uintptr_t)t.grad & (f32 ? 15 : 7)) || ((uintptr_t)t.weight_bf16 & 7) ||
+        (states & (eight ? 3 : 15)) || (eight && (((uintptr_t)t.m_scale | (uintptr_t)t.v_scale) & 3)))
+      return MTNLG_INVALID_ARG;
+    if (!count_ok(t.count)) return MTNLG_UNSUPPORTED_SHAPE;
+    blocks += (uint64_t)blocks_of(t.count);
+  }
+  if (blocks > 0xFFFFFFFFull) return MTNLG_UNSUPPORTED_SHAPE;
+  {
+    Span *spans = new (std::nothrow) Span[(size_t)desc->tensors * 7 + 1];
+    if (!spans) return MTNLG_HIP_ERROR;
+    int64_t n = 0;
+    auto add = [&](const void *p, int64_t bytes, bool written) {
+      if (p) spans[n++] = Span{(uintptr_t)p, (uintptr_t)p + (uintptr_t)bytes, written};
+    };
+    for (int32_t i = 0; i < desc->tensors; ++i) {
+      const mtnlg_adam_tensor &t = of[i];
+      add(t.master, t.count * 4, true);
+      add(t.m, t.count * (eight ? 1 : 4), true);
+      add(t.v, t.count * (eight ? 1 : 4), true);
+      add(t.weight_bf16, t.count * 2, true);
+      add(t.grad, t.count * (f32 ? 4 : 2), false);
+      if (eight) {
+        add(t.m_scale, blocks_of(t.count) * 4, true);
+        add(t.v_scale, blocks_of(t.count) * 4, true);
+      }
+    }
+    add(sqnorm, 4, false);
+    const bool apart = spans_apart(spans, n);
+    delete[] spans;
+    if (!apart) return MTNLG_INVALID_ARG;
+  }
+  hipStream_t st = (hipStream_t)stream;
+  LaunchScope scope(MTNLG_K_ELEMENTWISE, st);
+  StepArgs s;
+  s.a = adam_args(desc->adam);
+  s.sqnorm = sqnorm;
+  step_keys(desc->seed, desc->adam.step, &s.key_lo, &s.key_hi);
+  uint32_t block = 0;
+  for (int32_t i = 0; i < desc->tensors;) {
+    uint64_t chunks = 0;
+    int32_t k = 0;
+    for (; i + k < desc->tensors && k < kStepTensors && chunks < ((uint64_t)1 << 31); ++k) {
+      const mtnlg_adam_tensor &t = of[i + k];
+      s.of[k] = StepTensor{t.master, t.m, t.v, t.m_scale, t.v_scale, t.grad, (bf16 *)t.weight_bf16, t.count, (uint32_t)chunks, block,
+                           t.decay ? desc->adam.weight_decay : 0.0f, 0};
+      chunks += (uint64_t)(t.count + kChunk - 1) / kChunk;
+      block += (uint32_t)blocks_of(t.count);
+    }
+    s.chunks = (uint32_t)chunks;
+    s.tensors = k;
+    const unsigned grid = (unsigned)std::min<uint64_t>(chunks, 1u << 20);
+    if (eight && f32) adam_many_kernel<true, float><<<grid, 256, 0, st>>>(s);
+    else if (eight) adam_many_kernel<true, bf16><<<grid, 256, 0, st>>>(s);
+    else if (f32) adam_many_kernel<false, float><<<grid, 256, 0, st>>>(s);
+    else adam_many_kernel<false, bf16><<<grid, 256, 0, st>>>(s);
+    MTNLG_TRY(check_launch());
+    i += k;
+  }
+  return MTNLG_OK;
+}
+
+}  // extern "C"

@@ -9,9 +9,7 @@
 //                            forward pass (14 bytes); the clipping factor comes from a device
 //                            scalar so that nothing synchronises with the host.
 // Every lane moves 16 bytes per access, lanes on consecutive addresses.
-#include <math.h>
-
-#include "common.h"
+#include "adam.h"
 
 namespace mtnlg {
 
@@ -48,20 +46,6 @@ __device__ __forceinline__ double square_sum(const float *__restrict__ g, int64_
   }
   return (s[0] + s[1]) + (s[2] + s[3]);
 }
-// the sum over the workgroup, in thread 0: a fixed tree
-template <int THREADS>
-__device__ __forceinline__ double workgroup_sum(double s) {
-  __shared__ double red[THREADS / 64];
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) s += __shfl_xor(s, off, 64);
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
-  __syncthreads();
-  s = red[0];
-#pragma unroll
-  for (int w = 1; w < THREADS / 64; ++w) s += red[w];
-  return s;
-}
-
 __global__ __launch_bounds__(256) void sqnorm_stage1(int64_t count, int64_t chunk, const float *__restrict__ g, double *__restrict__ partial) {
   // block b owns the contiguous range [b * chunk, (b + 1) * chunk), chunk a multiple of 4
   const int64_t lo = blockIdx.x * chunk, hi = lo + chunk < count ? lo + chunk : count;
@@ -84,19 +68,6 @@ __global__ __launch_bounds__(256) void sqnorm_stage2(int blocks, const double *_
 __global__ __launch_bounds__(1024) void sqnorm_once(int64_t count, const float *__restrict__ g, float *__restrict__ out, int accumulate) {
   const double s = workgroup_sum<1024>(square_sum<1024>(g, 0, count));
   if (threadIdx.x == 0) out[0] = (float)(accumulate ? (double)out[0] + s : s);
-}
-
-struct AdamArgs {
-  float lr, beta1, beta2, eps, wd, max_norm;
-  float inv_c1, inv_c2;   // 1 / (1 - beta1^t), 1 / (1 - beta2^t)
-};
-
-__device__ __forceinline__ void adam_one(const AdamArgs &a, float coef, float g, float &p, float &m, float &v) {
-  g *= coef;
-  m = a.beta1 * m + (1.0f - a.beta1) * g;
-  v = a.beta2 * v + (1.0f - a.beta2) * g * g;
-  const float mh = m * a.inv_c1, vh = v * a.inv_c2;
-  p = p - a.lr * (mh / (sqrtf(vh) + a.eps) + a.wd * p);
 }
 
 __global__ __launch_bounds__(256) void adam_kernel(AdamArgs a, int64_t count, float *__restrict__ p, float *__restrict__ m,
@@ -172,20 +143,10 @@ int mtnlg_grad_sqnorm(int64_t count, const float *grad, void *workspace, float *
 int mtnlg_adam_step(const mtnlg_adam_desc *desc, int64_t count, float *master, float *m, float *v, const float *grad,
                     void *weight_bf16, const float *sqnorm, void *stream) {
   if (!desc || !master || !m || !v || !grad) return MTNLG_NULL_POINTER;
-  if (count <= 0 || desc->step < 1) return MTNLG_INVALID_ARG;
-  if (!(desc->beta1 >= 0.0f && desc->beta1 < 1.0f && desc->beta2 >= 0.0f && desc->beta2 < 1.0f && desc->eps > 0.0f))
-    return MTNLG_INVALID_ARG;
+  if (count <= 0 || !adam_desc_ok(*desc)) return MTNLG_INVALID_ARG;
   if (((uintptr_t)master | (uintptr_t)m | (uintptr_t)v | (uintptr_t)grad) & 15) return MTNLG_INVALID_ARG;
   if ((uintptr_t)weight_bf16 & 7) return MTNLG_INVALID_ARG;
-  AdamArgs a;
-  a.lr = desc->lr;
-  a.beta1 = desc->beta1;
-  a.beta2 = desc->beta2;
-  a.eps = desc->eps;
-  a.wd = desc->weight_decay;
-  a.max_norm = desc->max_grad_norm;
-  a.inv_c1 = (float)(1.0 / (1.0 - pow((double)desc->beta1, (double)desc->step)));
-  a.inv_c2 = (float)(1.0 / (1.0 - pow((double)desc->beta2, (double)desc->step)));
+  const AdamArgs a = adam_args(*desc);
   hipStream_t st = (hipStream_t)stream;
   int64_t blocks = (count + 1023) / 1024;
   if (blocks > 8192) blocks = 8192;   // grid-stride beyond: 32 workgroups per CU
