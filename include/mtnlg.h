@@ -388,7 +388,7 @@ typedef struct {
   int32_t gate;     /* mtnlg_gate                                                               */
   int64_t tokens;   /* T, <= 2^22 - 64                                                            */
   int32_t hidden;   /* h, a multiple of 8, <= 32768                                               */
-  int32_t ffn;      /* F, a multiple of 8, <= 2^20                                                */
+  int32_t ffn;      /* F, a multiple of 8, <= 2^20; h F <= 2^31 - 2^23, float 2^30 - 2^22          */
   uint32_t flags;   /* backward: MTNLG_ACCUMULATE_WGRAD, MTNLG_WGRAD_FP32                         */
 } mtnlg_gated_desc;
 

@@ -83,11 +83,20 @@ void saved_layout(const Shape &S, mtnlg_saved_layout *L) {
 bool fp32_in_parts(int dtype, int layout, int64_t M, int64_t N, int64_t K) {
   return dtype == MTNLG_F32 && gemm_parts_time(M, N, K) < std::min(gemm_generic_time(layout, M, N, K), gemm_direct_time(M, N, K));
 }
+
+}  // namespace
+
+namespace mtnlg {
+
 // estimated microseconds of a product on the kernels that do not split K over waves
 double gemm_time(int dtype, int layout, int64_t M, int64_t N, int64_t K, size_t ws_bytes) {
   if (dtype == MTNLG_BF16) return gemm_mfma_time(layout, M, N, K, ws_bytes);
   return std::min(gemm_parts_time(M, N, K), std::min(gemm_generic_time(layout, M, N, K), gemm_direct_time(M, N, K)));
 }
+
+}  // namespace mtnlg
+
+namespace {
 
 // Scratch carved from the caller's workspace.
 struct Work {

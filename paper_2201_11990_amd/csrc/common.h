@@ -332,6 +332,7 @@ inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 int heads_check(const mtnlg_heads *m, int64_t tokens, int groups, int heads, int d, int dtype);
 
 // internal launchers shared between translation units
+double gemm_time(int dtype, int layout, int64_t M, int64_t N, int64_t K, size_t ws_bytes);   // estimated microseconds of mtnlg_gemm without the kernels of gemm_wave.hip
 constexpr int64_t GEMM_GENERIC_MAX_ROWS = 65535 * 64;
 int gemm_generic(int dtype, int layout, int64_t M, int64_t N, int64_t K, const void *A,
                  const void *B, void *C, const void *bias, void *aux, uint32_t epi,
@@ -361,7 +362,8 @@ struct ColumnSums {
 // have to be taken; sums: how many matrices, of how many rows and columns
 int gemm_wave_group_tile(int dtype, const GemmCall &nn, const GemmCall &tn, int sums, int64_t sum_rows, int64_t sum_cols, double separate_nn,
                          double separate_tn);
-int gemm_wave_group(int dtype, const GemmCall &nn, const GemmCall &tn, const ColumnSums &sums, int tile, hipStream_t stream);
+int gemm_wave_group(int dtype, const GemmCall &nn, const GemmCall &tn, const ColumnSums &sums, int tile, hipStream_t stream,
+                    bool gate = false);   // gate: nn with the gate's backward (gate.h: GATE_BWD)
 // LayerNorm backward without the sums over rows; left: what is to be added up afterwards, over so many rows at most
 int layernorm_bwd_rows(int dtype, int64_t T, int64_t h, const void *x, const void *gamma, const float *mean, const float *rstd,
                        const void *dout, const void *dres, void *dx, void *dgamma, void *dbeta, void *colsum_dx, int grad_f32,

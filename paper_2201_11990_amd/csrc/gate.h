@@ -1,0 +1,104 @@
+// The gate of the gated feed-forward block: an activation of fp32 values, and its slope.
+#pragma once
+#include "common.h"
+
+namespace mtnlg {
+
+// FAST: hardware exp2 and reciprocal (1 ulp each), a few 1e-7 of relative error, for results that round to bf16: silu(x) = x s, s = 1 / (1 + exp(-x)), silu' = s + x s (1 - s) with 1 - s =
+// exp(-x) s, the exponent clamped so that exp(-x) s stays finite; GeLU's tanh form likewise (gelu_sigmoid_f).
+template <bool FAST, int KIND>
+__device__ __forceinline__ void gate_one(float x, float &a, float &slope) {
+  if constexpr (KIND == MTNLG_GATE_SILU) {
+    if constexpr (FAST) {
+      const float e = __builtin_amdgcn_exp2f(fminf(x * -1.4426950408889634f, 115.0f)), s = __builtin_amdgcn_rcpf(1.0f + e);
+      a = x * s;
+      slope = s + a * (e * s);
+    } else {
+      const float s = 1.0f / (1.0f + expf(-x));
+      a = x * s;
+      slope = s + a * (1.0f - s);
+    }
+  } else if constexpr (KIND == MTNLG_GATE_GELU_TANH) {
+    if constexpr (FAST) {
+      constexpr float D1 = 2.0f * 0.79788456080286536f, D3 = D1 * 3.0f * 0.044715f;
+      const float x2 = x * x;
+      float e;
+      const float s = gelu_sigmoid_f(x, x2, e);
+      a = x * s;
+      slope = s + (x * (D1 + D3 * x2)) * (e * s) * s;
+    } else {
+      a = gelu_f(x, false);
+      slope = gelu_grad_f(x, false);
+    }
+  } else {
+    a = gelu_f(x, true);
+    slope = gelu_grad_f(x, true);
+  }
+}
+// a[i] = act(x[i]), slope[i] = act'(x[i]); the kind is the same in all lanes and is looked at once for the N values
+template <bool FAST, int N>
+__device__ __forceinline__ void gate_of(int kind, const float (&x)[N], float (&a)[N], float (&slope)[N]) {
+  if (kind == MTNLG_GATE_SILU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) gate_one<FAST, MTNLG_GATE_SILU>(x[i], a[i], slope[i]);
+  } else if (kind == MTNLG_GATE_GELU_TANH) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) gate_one<FAST, MTNLG_GATE_GELU_TANH>(x[i], a[i], slope[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) gate_one<FAST, MTNLG_GATE_GELU_ERF>(x[i], a[i], slope[i]);
+  }
+}
+
+// What a product of the block does with its results, in the place of the other epilogues (EpiArgs: aux is z [M, 2 F], flags the kind):
+//   GATE_FWD  N = 2 F columns of z, in fours (gate, gate, other, other): act(gate) * other to C [M, F], z to aux (nullable)
+//   GATE_BWD  N = F columns of dg: with z from aux, dz to C [M, 2 F]
+enum gate_mode { GATE_NONE = 0, GATE_FWD = 1, GATE_BWD = 2 };
+// Row of w_fc1 [2 F, h] that column n of GATE_FWD's product takes: so every lane of a matrix instruction's result holds both parts of two columns
+__device__ __forceinline__ int64_t gate_row(int64_t n, int64_t F) { return (n >> 2) * 2 + (n & 1) + ((n & 2) ? F : 0); }
+
+template <typename E>
+__device__ __forceinline__ void put4(E *p, f32x4 x) {
+  if constexpr (sizeof(E) == 4) *reinterpret_cast<f32x4 *>(p) = x;
+  else *reinterpret_cast<bf16x4 *>(p) = bf16x4{(bf16)x[0], (bf16)x[1], (bf16)x[2], (bf16)x[3]};
+}
+typedef __attribute__((ext_vector_type(2))) float gate_f32x2;
+template <typename E>
+__device__ __forceinline__ void put2(E *p, float x, float y) {
+  if constexpr (sizeof(E) == 4) *reinterpret_cast<gate_f32x2 *>(p) = gate_f32x2{x, y};
+  else *reinterpret_cast<bf16x2 *>(p) = bf16x2{(bf16)x, (bf16)y};
+}
+// Four consecutive columns of row m at column n of such a product
+template <typename E, int MODE>
+__device__ __forceinline__ void gate_epilogue4(const EpiArgs &ea, void *C, int64_t N, int64_t m, int64_t n, f32x4 v) {
+  constexpr bool FAST = sizeof(E) == 2;
+  if constexpr (MODE == GATE_FWD) {
+    const int64_t F = N / 2, c = n / 2;
+    if (ea.aux != nullptr) {
+      E *z = static_cast<E *>(ea.aux) + m * N + c;
+      put2(z, v[0], v[1]);
+      put2(z + F, v[2], v[3]);
+    }
+    const float x[2] = {v[0], v[1]};
+    float a[2], slope[2];
+    gate_of<FAST>((int)ea.flags, x, a, slope);
+    put2(static_cast<E *>(C) + m * F + c, a[0] * v[2], a[1] * v[3]);
+  } else {
+    const E *z = static_cast<const E *>(ea.aux) + m * 2 * N + n;
+    const f32x4 g = load4(z), u = load4(z + N);
+    const float x[4] = {g[0], g[1], g[2], g[3]};
+    float a[4], slope[4];
+    gate_of<FAST>((int)ea.flags, x, a, slope);
+    f32x4 da, db;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      da[e] = v[e] * u[e] * slope[e];
+      db[e] = v[e] * a[e];
+    }
+    E *dz = static_cast<E *>(C) + m * 2 * N + n;
+    put4(dz, da);
+    put4(dz + N, db);
+  }
+}
+
+}  // namespace mtnlg

@@ -1,0 +1,18 @@
+// Launchers of the gated feed-forward block's products that carry its activation (gate.h: what they do with their results).
+#pragma once
+#include "gate.h"
+
+namespace mtnlg {
+
+int gated_mfma_fwd(int kind, int64_t T, int64_t h, int64_t F, const void *x, const void *w_fc1, void *z, void *g, void *ws, size_t ws_bytes,
+                   hipStream_t stream);
+int gated_mfma_bwd(int kind, int64_t T, int64_t h, int64_t F, const void *dy, const void *w_fc2, const void *z, void *dz, void *ws, size_t ws_bytes,
+                   hipStream_t stream);
+
+// mode: GATE_FWD (A x, B w_fc1, C g) or GATE_BWD (A dy, B w_fc2, C dz); tile: 32 or 64
+bool gated_wave_takes(int dtype, int64_t h, int64_t F);
+int gated_wave(int dtype, int mode, int kind, int64_t T, int64_t h, int64_t F, const void *A, const void *B, void *z, void *C, int tile,
+               hipStream_t stream);
+int gated_parts(int mode, int kind, int64_t T, int64_t h, int64_t F, const void *A, const void *B, void *z, void *C, hipStream_t stream);
+
+}  // namespace mtnlg

@@ -1,70 +1,20 @@
-// Gated feed-forward block: z = x w_fc1^T, g = act(z_a) * z_b, y = g w_fc2^T and its adjoint.
+// Gated feed-forward block: z = x w_fc1^T, g = act(z_a) * z_b, y = g w_fc2^T and its adjoint, as matrix products that carry the activation:
+//   forward   x w_fc1^T (act(gate) * other in the epilogue), g w_fc2^T
+//   backward  dw_fc2 = dy^T g, dy w_fc2 (the activation's backward in the epilogue: dz), dx = dz w_fc1, dw_fc1 = dz^T x
+// Bound by the matrix pipes from some hundred tokens on: 6 T h F operations forward and 12 backward, with z written and read once.  In small calls
+// the products of one weight matrix's backward are one launch (gemm_wave.hip), so a step of 61 tokens is four.
 #include <algorithm>
 
-#include "common.h"
+#include "gated.h"
 
 namespace mtnlg {
 
 namespace {
 
-// The activation of fp32 x and its slope
-__device__ __forceinline__ void gate_of(int kind, float x, float &a, float &da) {
-  if (kind == MTNLG_GATE_SILU) {
-    const float s = 1.0f / (1.0f + expf(-x));
-    a = x * s;
-    da = s * (1.0f + x * (1.0f - s));
-  } else {
-    a = gelu_f(x, kind == MTNLG_GATE_GELU_ERF);
-    da = gelu_grad_f(x, kind == MTNLG_GATE_GELU_ERF);
-  }
-}
-
-template <typename E>
-__global__ __launch_bounds__(256) void gate_fwd_kernel(int64_t T, int64_t F, int kind, const float *__restrict__ zf, E *__restrict__ z, E *__restrict__ g) {
-  const int64_t n = T * (F / 8);
-  for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < n; i += gridDim.x * 256ll) {
-    const int64_t t = i / (F / 8), c = i % (F / 8) * 8;
-    float a[8], b[8];
-    load8(zf + t * 2 * F + c, a);
-    load8(zf + t * 2 * F + F + c, b);
-    if (z != nullptr) {
-      store8(z + t * 2 * F + c, a);
-      store8(z + t * 2 * F + F + c, b);
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      float v, d;
-      gate_of(kind, a[e], v, d);
-      a[e] = v * b[e];
-    }
-    store8(g + t * F + c, a);
-  }
-}
-template <typename E>
-__global__ __launch_bounds__(256) void gate_bwd_kernel(int64_t T, int64_t F, int kind, const E *__restrict__ z, const float *__restrict__ dg, E *__restrict__ dz) {
-  const int64_t n = T * (F / 8);
-  for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < n; i += gridDim.x * 256ll) {
-    const int64_t t = i / (F / 8), c = i % (F / 8) * 8;
-    float a[8], b[8], d[8];
-    load8(z + t * 2 * F + c, a);
-    load8(z + t * 2 * F + F + c, b);
-    load8(dg + t * F + c, d);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      float v, s;
-      gate_of(kind, a[e], v, s);
-      a[e] = d[e] * b[e] * s;
-      b[e] = d[e] * v;
-    }
-    store8(dz + t * 2 * F + c, a);
-    store8(dz + t * 2 * F + F + c, b);
-  }
-}
-
 struct Sizes {
   int64_t T, h, F;
   int dtype, gate;
-  size_t es, gemm_ws, inner;
+  size_t es, gemm_ws;
 };
 int sizes_of(const mtnlg_gated_desc *d, Sizes *s) {
   if (!d) return MTNLG_NULL_POINTER;
@@ -72,7 +22,9 @@ int sizes_of(const mtnlg_gated_desc *d, Sizes *s) {
       d->hidden <= 0 || d->ffn <= 0 || (d->flags & ~(MTNLG_ACCUMULATE_WGRAD | MTNLG_WGRAD_FP32)))
     return MTNLG_INVALID_ARG;
   if (d->tokens > GEMM_GENERIC_MAX_ROWS || d->hidden % 8 || d->hidden > 32768 || d->ffn % 8 || d->ffn > (1 << 20)) return MTNLG_UNSUPPORTED_SHAPE;
-  *s = Sizes{d->tokens, d->hidden, d->ffn, d->dtype, d->gate, d->dtype == MTNLG_F32 ? (size_t)4 : 2, 0, 0};
+  // 32-bit offsets reach both halves of w_fc1 from a tile's first row
+  if ((int64_t)d->hidden * d->ffn > (d->dtype == MTNLG_F32 ? ((int64_t)1 << 30) - (1 << 22) : ((int64_t)1 << 31) - (1 << 23))) return MTNLG_UNSUPPORTED_SHAPE;
+  *s = Sizes{d->tokens, d->hidden, d->ffn, d->dtype, d->gate, d->dtype == MTNLG_F32 ? (size_t)4 : 2, 0};
   auto need = [&](int layout, int64_t M, int64_t N, int64_t K) { s->gemm_ws = std::max(s->gemm_ws, mtnlg_gemm_workspace(s->dtype, layout, M, N, K)); };
   need(MTNLG_GEMM_NT, s->T, 2 * s->F, s->h);
   need(MTNLG_GEMM_NT, s->T, s->h, s->F);
@@ -81,7 +33,6 @@ int sizes_of(const mtnlg_gated_desc *d, Sizes *s) {
   need(MTNLG_GEMM_TN, 2 * s->F, s->h, s->T);
   need(MTNLG_GEMM_TN, s->h, s->F, s->T);
   s->gemm_ws = align_up(s->gemm_ws, 256);
-  s->inner = align_up((size_t)(s->T * 2 * s->F) * 4, 256);
   return MTNLG_OK;
 }
 
@@ -101,7 +52,21 @@ bool lies_apart(const Bytes *out, int outs, const Bytes *in, int ins) {
   return true;
 }
 
-unsigned grid_of(const Sizes &s) { return (unsigned)std::min<int64_t>((s.T * (s.F / 8) + 255) / 256, 8192); }
+// One of the two products that carry the activation, on the kernel that is estimated to be the fastest
+double gated_time(const Sizes &s, int mode) {
+  const int layout = mode == GATE_FWD ? MTNLG_GEMM_NT : MTNLG_GEMM_NN;
+  const int64_t N = mode == GATE_FWD ? 2 * s.F : s.F;
+  return s.dtype == MTNLG_F32 ? gemm_parts_time(s.T, N, s.h) : gemm_mfma_time(layout, s.T, N, s.h, s.gemm_ws);
+}
+int gated_product(const Sizes &s, int mode, const void *A, const void *B, void *z, void *C, void *ws, hipStream_t st) {
+  const int layout = mode == GATE_FWD ? MTNLG_GEMM_NT : MTNLG_GEMM_NN;
+  const int64_t N = mode == GATE_FWD ? 2 * s.F : s.F;
+  if (const int tile = gemm_wave_pick(s.dtype, layout, s.T, N, s.h, gated_time(s, mode)))
+    return gated_wave(s.dtype, mode, s.gate, s.T, s.h, s.F, A, B, z, C, tile, st);
+  if (s.dtype == MTNLG_F32) return gated_parts(mode, s.gate, s.T, s.h, s.F, A, B, z, C, st);
+  return mode == GATE_FWD ? gated_mfma_fwd(s.gate, s.T, s.h, s.F, A, B, z, C, ws, s.gemm_ws, st)
+                          : gated_mfma_bwd(s.gate, s.T, s.h, s.F, A, B, z, C, ws, s.gemm_ws, st);
+}
 
 }  // namespace
 
@@ -113,7 +78,7 @@ extern "C" {
 
 size_t mtnlg_gated_ffn_workspace(const mtnlg_gated_desc *desc) {
   Sizes s;
-  return sizes_of(desc, &s) == MTNLG_OK ? s.gemm_ws + s.inner : 0;
+  return sizes_of(desc, &s) == MTNLG_OK ? s.gemm_ws : 0;
 }
 
 int mtnlg_gated_ffn_fwd(const mtnlg_gated_desc *desc, const void *x, const void *w_fc1, const void *w_fc2, void *z, void *g, void *y,
@@ -128,14 +93,7 @@ int mtnlg_gated_ffn_fwd(const mtnlg_gated_desc *desc, const void *x, const void 
   if (!lies_apart(out, 4, in, 3)) return MTNLG_INVALID_ARG;
   if (workspace_bytes < need) return MTNLG_WORKSPACE_TOO_SMALL;
   hipStream_t st = (hipStream_t)stream;
-  float *zf = (float *)((char *)workspace + s.gemm_ws);
-  MTNLG_TRY(mtnlg_gemm(s.dtype, MTNLG_GEMM_NT, s.T, 2 * s.F, s.h, x, w_fc1, zf, nullptr, nullptr, MTNLG_EPI_OUT_F32, workspace, s.gemm_ws, stream));
-  {
-    LaunchScope scope(MTNLG_K_GELU, st);
-    if (s.dtype == MTNLG_F32) gate_fwd_kernel<float><<<grid_of(s), 256, 0, st>>>(s.T, s.F, s.gate, zf, (float *)z, (float *)g);
-    else gate_fwd_kernel<bf16><<<grid_of(s), 256, 0, st>>>(s.T, s.F, s.gate, zf, (bf16 *)z, (bf16 *)g);
-    MTNLG_TRY(check_launch());
-  }
+  MTNLG_TRY(gated_product(s, GATE_FWD, x, w_fc1, z, g, workspace, st));
   return mtnlg_gemm(s.dtype, MTNLG_GEMM_NT, s.T, s.h, s.F, g, w_fc2, y, nullptr, nullptr, 0, workspace, s.gemm_ws, stream);
 }
 
@@ -156,17 +114,24 @@ int mtnlg_gated_ffn_bwd(const mtnlg_gated_desc *desc, const void *x, const void 
   if (workspace_bytes < need) return MTNLG_WORKSPACE_TOO_SMALL;
   hipStream_t st = (hipStream_t)stream;
   const uint32_t epi = ((desc->flags & MTNLG_ACCUMULATE_WGRAD) ? (uint32_t)MTNLG_EPI_ACCUMULATE : 0u) | (wide ? (uint32_t)MTNLG_EPI_OUT_F32 : 0u);
-  float *dg = (float *)((char *)workspace + s.gemm_ws);
-  MTNLG_TRY(mtnlg_gemm(s.dtype, MTNLG_GEMM_NN, s.T, s.F, s.h, dy, w_fc2, dg, nullptr, nullptr, MTNLG_EPI_OUT_F32, workspace, s.gemm_ws, stream));
-  {
-    LaunchScope scope(MTNLG_K_GELU, st);
-    if (s.dtype == MTNLG_F32) gate_bwd_kernel<float><<<grid_of(s), 256, 0, st>>>(s.T, s.F, s.gate, (const float *)z, dg, (float *)dz);
-    else gate_bwd_kernel<bf16><<<grid_of(s), 256, 0, st>>>(s.T, s.F, s.gate, (const bf16 *)z, dg, (bf16 *)dz);
-    MTNLG_TRY(check_launch());
+  auto gemm = [&](int layout, const GemmCall &c) {
+    return mtnlg_gemm(s.dtype, layout, c.M, c.N, c.K, c.A, c.B, c.C, nullptr, nullptr, c.epi, workspace, s.gemm_ws, stream);
+  };
+  auto time = [&](int layout, const GemmCall &c) { return gemm_time(s.dtype, layout, c.M, c.N, c.K, s.gemm_ws); };
+  const GemmCall to_dz{s.T, s.F, s.h, dy, w_fc2, dz, const_cast<void *>(z), (uint32_t)s.gate}, to_dw2{s.h, s.F, s.T, dy, g, dw_fc2, nullptr, epi};
+  const int tile2 = dw_fc2 ? gemm_wave_group_tile(s.dtype, to_dz, to_dw2, 0, 0, 0, gated_time(s, GATE_BWD), time(MTNLG_GEMM_TN, to_dw2)) : 0;
+  if (tile2) {
+    MTNLG_TRY(gemm_wave_group(s.dtype, to_dz, to_dw2, ColumnSums{}, tile2, st, true));
+  } else {
+    if (dw_fc2) MTNLG_TRY(gemm(MTNLG_GEMM_TN, to_dw2));
+    MTNLG_TRY(gated_product(s, GATE_BWD, dy, w_fc2, const_cast<void *>(z), dz, workspace, st));
   }
-  if (dw_fc2) MTNLG_TRY(mtnlg_gemm(s.dtype, MTNLG_GEMM_TN, s.h, s.F, s.T, dy, g, dw_fc2, nullptr, nullptr, epi, workspace, s.gemm_ws, stream));
-  if (dx) MTNLG_TRY(mtnlg_gemm(s.dtype, MTNLG_GEMM_NN, s.T, s.h, 2 * s.F, dz, w_fc1, dx, nullptr, nullptr, 0, workspace, s.gemm_ws, stream));
-  if (dw_fc1) MTNLG_TRY(mtnlg_gemm(s.dtype, MTNLG_GEMM_TN, 2 * s.F, s.h, s.T, dz, x, dw_fc1, nullptr, nullptr, epi, workspace, s.gemm_ws, stream));
+  const GemmCall to_dx{s.T, s.h, 2 * s.F, dz, w_fc1, dx, nullptr, 0}, to_dw1{2 * s.F, s.h, s.T, dz, x, dw_fc1, nullptr, epi};
+  if (dx && dw_fc1)
+    if (const int tile = gemm_wave_group_tile(s.dtype, to_dx, to_dw1, 0, 0, 0, time(MTNLG_GEMM_NN, to_dx), time(MTNLG_GEMM_TN, to_dw1)))
+      return gemm_wave_group(s.dtype, to_dx, to_dw1, ColumnSums{}, tile, st);
+  if (dx) MTNLG_TRY(gemm(MTNLG_GEMM_NN, to_dx));
+  if (dw_fc1) MTNLG_TRY(gemm(MTNLG_GEMM_TN, to_dw1));
   return MTNLG_OK;
 }
 

@@ -7,7 +7,7 @@
 // TN 58 / 65 / 50; 2048 x 2048 x 4096 NT 242 / 208 / 179.  Those two cut a value once a wave, two to eight times a workgroup, and with the
 // operands in LDS as fp32 values and the cutting behind the reads the same tiles took 66 us at 1024 x 4096 x 1024 NT; leaving the cutting out
 // altogether, 45.  What bounds it now: the MFMAs (0.97 to 1.2 PFLOP/s of products of parts), then LDS: 147 KB read and 48 KB written a slab.
-#include "common.h"
+#include "gated.h"
 
 namespace mtnlg {
 
@@ -35,8 +35,9 @@ typedef __attribute__((ext_vector_type(2))) float f32x2;
 struct Pair {
   float v[2][8];
   // first: element (first row of the blocks, k = 0), row row0 of the operand; slabs past the last one: zeros
+  // half: rows of the weights in pairs of both halves (gate.h), so many rows apart; 0: as they lie
   template <bool ROWC>
-  __device__ __forceinline__ void load(const float *first, int64_t ld, int64_t rows_left, int64_t row0, int64_t k0, int64_t K, int lane) {
+  __device__ __forceinline__ void load(const float *first, int64_t ld, int64_t rows_left, int64_t row0, int64_t k0, int64_t K, int lane, int64_t half) {
     const int g = lane >> 4, r = lane & 15;
     if constexpr (!ROWC) {
       const __amdgpu_buffer_rsrc_t rs = rsrc(first + k0, RECORDS);
@@ -44,7 +45,7 @@ struct Pair {
       for (int b = 0; b < 2; ++b)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const uint32_t off = (uint32_t)((16 * b + r) * ld * 4 + (16 * h + 4 * g) * 4);
+          const uint32_t off = (uint32_t)((half ? gate_row(16 * b + r, half) : 16 * b + r) * ld * 4 + (16 * h + 4 * g) * 4);
           const f32x4 t = __builtin_bit_cast(
               f32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, 16 * b + r < rows_left && k0 + 16 * h + 4 * g < K ? off : OUTSIDE, 0, 0));
 #pragma unroll
@@ -73,7 +74,7 @@ struct Pair {
 template <int V>
 struct Num { static constexpr int value = V; };
 
-template <bool AT, bool BT>
+template <bool AT, bool BT, int GATE>
 __global__ __launch_bounds__(64 * WAVES, 2) void gemm_parts_kernel(PartsArgs a) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
@@ -90,7 +91,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void gemm_parts_kernel(PartsArgs a) 
   // Waves 0-3 bring A, 4-7 B, 32 rows each.
   const bool is_a = wave < 4;
   const int64_t row0 = (is_a ? m0 : n0) + 32 * (wave & 3), rows_left = (is_a ? a.M : a.N) - row0, ld = is_a ? a.lda : a.ldb;
-  const float *first = (is_a ? a.A : a.B) + ((is_a ? AT : BT) ? row0 : row0 * ld);
+  static_assert(GATE != GATE_FWD || !BT, "rows of the weights in pairs");
+  const int64_t half = GATE == GATE_FWD && !is_a ? a.N / 2 : 0;
+  const float *first = (is_a ? a.A : a.B) + ((is_a ? AT : BT) ? row0 : (half ? row0 / 2 : row0) * ld);
   const int nk = (int)((a.K + SLAB_K - 1) / SLAB_K);
   Pair raw[2];   // [slab % 2]
   auto put = [&](auto slot, int stage) {   // the wave's blocks in parts
@@ -118,7 +121,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void gemm_parts_kernel(PartsArgs a) 
   // One body for each way of loading: where the two kinds meet in one, the compiler waits for all loads at their first use.
   auto run = [&](auto rowc) {
     auto load = [&](auto slot, int s) {
-      raw[decltype(slot)::value].template load<decltype(rowc)::value != 0>(first, ld, rows_left, row0, (int64_t)s * SLAB_K, a.K, lane);
+      raw[decltype(slot)::value].template load<decltype(rowc)::value != 0>(first, ld, rows_left, row0, (int64_t)s * SLAB_K, a.K, lane, half);
     };
     load(Num<0>{}, 0);
     load(Num<1>{}, 1);
@@ -186,8 +189,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void gemm_parts_kernel(PartsArgs a) 
       for (int j = 0; j < 2; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 1
     for (int s = 0; s < nk; ++s) {   // the same blocks as fp32 values: elements 0-3 in the place of the first part, 4-7 of the second
-      if (is_a) raw[0].load<AT>(first, ld, rows_left, row0, (int64_t)s * SLAB_K, a.K, lane);
-      else raw[0].load<BT>(first, ld, rows_left, row0, (int64_t)s * SLAB_K, a.K, lane);
+      if (is_a) raw[0].load<AT>(first, ld, rows_left, row0, (int64_t)s * SLAB_K, a.K, lane, half);
+      else raw[0].load<BT>(first, ld, rows_left, row0, (int64_t)s * SLAB_K, a.K, lane, half);
       __syncthreads();
 #pragma unroll
       for (int b = 0; b < 2; ++b)
@@ -231,21 +234,24 @@ __global__ __launch_bounds__(64 * WAVES, 2) void gemm_parts_kernel(PartsArgs a) 
         for (int e = 0; e < 4; ++e) o[e] = acc[i][(4 * v + e) & 1][(4 * v + e) >> 1];
       }
       const int64_t m = m0 + 64 * wm + 32 * (i >> 1) + (AT ? 2 * r + (i & 1) : 16 * (i & 1) + r), n = n0 + 32 * wn + (BT ? 8 * g + 4 * v : 16 * v + 4 * g);
-      if (m < a.M && n < a.N) epilogue4<float>(a.ea, a.C, a.N, m, n, o);
+      if (m < a.M && n < a.N) {
+        if constexpr (GATE == GATE_NONE) epilogue4<float>(a.ea, a.C, a.N, m, n, o);
+        else gate_epilogue4<float, GATE>(a.ea, a.C, a.N, m, n, o);
+      }
     }
 }
 
-template <bool AT, bool BT>
+template <bool AT, bool BT, int GATE = GATE_NONE>
 int launch(const PartsArgs &a, hipStream_t st) {
   constexpr int smem = STAGES * STAGE;
   static unsigned long long attr_done = 0;
   int device;
   if (!attr_is_set(attr_done, &device)) {
-    if (hipFuncSetAttribute((const void *)gemm_parts_kernel<AT, BT>, hipFuncAttributeMaxDynamicSharedMemorySize, smem) != hipSuccess)
+    if (hipFuncSetAttribute((const void *)gemm_parts_kernel<AT, BT, GATE>, hipFuncAttributeMaxDynamicSharedMemorySize, smem) != hipSuccess)
       return MTNLG_HIP_ERROR;
     attr_mark_set(attr_done, device);
   }
-  gemm_parts_kernel<AT, BT><<<dim3((unsigned)(((int64_t)a.tiles_m * a.tiles_n + 7) / 8 * 8)), 64 * WAVES, smem, st>>>(a);
+  gemm_parts_kernel<AT, BT, GATE><<<dim3((unsigned)(((int64_t)a.tiles_m * a.tiles_n + 7) / 8 * 8)), 64 * WAVES, smem, st>>>(a);
   return check_launch();
 }
 
@@ -270,6 +276,18 @@ int gemm_parts(int layout, int64_t M, int64_t N, int64_t K, const void *A, const
   if (layout == MTNLG_GEMM_NT) return launch<false, false>(a, stream);
   if (layout == MTNLG_GEMM_NN) return launch<false, true>(a, stream);
   return launch<true, true>(a, stream);
+}
+
+// The products with the gate's epilogues (gated_wave_takes holds)
+int gated_parts(int mode, int kind, int64_t T, int64_t h, int64_t F, const void *A, const void *B, void *z, void *C, hipStream_t stream) {
+  const int layout = mode == GATE_FWD ? MTNLG_GEMM_NT : MTNLG_GEMM_NN;
+  const int64_t N = mode == GATE_FWD ? 2 * F : F, tm = (T + TILE - 1) / TILE, tn = (N + TILE - 1) / TILE;
+  if (!gated_wave_takes(MTNLG_F32, h, F) || !gemm_wave_takes(MTNLG_F32, layout, T, N, h, A, B, C, nullptr, z) || tm * tn > (1 << 28))
+    return MTNLG_UNSUPPORTED_SHAPE;
+  const PartsArgs a{T, N, h, h, mode == GATE_FWD ? h : F, static_cast<const float *>(A), static_cast<const float *>(B), static_cast<float *>(C),
+                    EpiArgs{nullptr, z, (uint32_t)kind}, (int)tm, (int)tn};
+  LaunchScope scope(MTNLG_K_GEMM_NT + layout, stream);
+  return mode == GATE_FWD ? launch<false, false, GATE_FWD>(a, stream) : launch<false, true, GATE_BWD>(a, stream);
 }
 
 }  // namespace mtnlg

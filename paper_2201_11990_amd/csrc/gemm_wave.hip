@@ -11,7 +11,7 @@
 // fp32: values in three bf16 parts (common.h: Parts), bound by the MFMAs and the vector instructions that make the parts.
 #include <math.h>
 
-#include "common.h"
+#include "gated.h"
 
 namespace mtnlg {
 
@@ -52,12 +52,13 @@ struct Slab {
   static __device__ __forceinline__ int place(int k) { return ES == 4 && TB == 32 ? k ^ ((k >> 2) & 1) : k; }   // (its own inverse)
 
   uint32_t off[NI];   // byte offsets of this lane's units from the slab's first element; rows past the edge lie outside
-  __device__ __forceinline__ Slab(int64_t ld, int64_t rows_left, int lane) {
+  // half: rows of the weights in pairs of both halves (gate.h), so many rows apart; 0: as they lie
+  __device__ __forceinline__ Slab(int64_t ld, int64_t rows_left, int lane, int64_t half = 0) {
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
       if constexpr (!ROWC) {
         const int row = 8 * i + (lane >> 3), c = (lane & 7) ^ (lane >> 3);
-        off[i] = row < rows_left ? (uint32_t)(row * ld * ES + c * 16) : OUTSIDE;
+        off[i] = row < rows_left ? (uint32_t)((half ? gate_row(row, half) : row) * ld * ES + c * 16) : OUTSIDE;
       } else {
         const int q = 64 * i + lane, k = place(q / UPR), u = (q % UPR) ^ mask(k);
         off[i] = u * EPU < rows_left ? (uint32_t)(k * ld * ES + u * 16) : OUTSIDE;
@@ -139,8 +140,8 @@ struct Frag32 {
   }
 };
 
-// The tile of workgroup `block` of a problem's grid.
-template <typename E, int TB, bool AT, bool BT>
+// The tile of workgroup `block` of a problem's grid.  GATE: gate.h
+template <typename E, int TB, bool AT, bool BT, int GATE = GATE_NONE>
 __device__ __forceinline__ void wave_tile(const WaveGemmArgs &a, int block, char *smem) {
   using SA = Slab<E, TB, AT>;
   using SB = Slab<E, TB, BT>;
@@ -157,9 +158,11 @@ __device__ __forceinline__ void wave_tile(const WaveGemmArgs &a, int block, char
   const int gsz = a.tiles_m - first_m < 8 ? a.tiles_m - first_m : 8;
   const int64_t m0 = (int64_t)(first_m + (pid % per_group) % gsz) * TB, n0 = (int64_t)((pid % per_group) / gsz) * TB;
 
-  const E *A = static_cast<const E *>(a.A) + (AT ? m0 : m0 * a.lda), *B = static_cast<const E *>(a.B) + (BT ? n0 : n0 * a.ldb);
+  static_assert(GATE != GATE_FWD || !BT, "rows of the weights in pairs");
+  const E *A = static_cast<const E *>(a.A) + (AT ? m0 : m0 * a.lda);
+  const E *B = static_cast<const E *>(a.B) + (BT ? n0 : (GATE == GATE_FWD ? n0 / 2 : n0) * a.ldb);
   const SA sa(a.lda, a.M - m0, lane);
-  const SB sb(a.ldb, a.N - n0, lane);
+  const SB sb(a.ldb, a.N - n0, lane, GATE == GATE_FWD ? a.N / 2 : 0);
   char *const stage = smem + wave * STAGE;
   const uint32_t lds = lds_address(stage);
   const int slabs = (int)((a.K + SK - 1) / SK);
@@ -279,14 +282,17 @@ __device__ __forceinline__ void wave_tile(const WaveGemmArgs &a, int block, char
     for (int w = 1; w < WAVES; ++w) s += red[w * PITCH + t * 64 + lane];
     const int i = t / NB, v = t % NB;
     const int64_t m = m0 + (ROWS_BY_LANE ? NB * r + i : 16 * i + r), n = n0 + (COLS_BY_LANE ? 4 * NB * g + 4 * v : 16 * v + 4 * g);
-    if (m < a.M && n < a.N) epilogue4<E>(a.ea, a.C, a.N, m, n, s);
+    if (m < a.M && n < a.N) {
+      if constexpr (GATE == GATE_NONE) epilogue4<E>(a.ea, a.C, a.N, m, n, s);
+      else gate_epilogue4<E, GATE>(a.ea, a.C, a.N, m, n, s);
+    }
   }
 }
 
-template <typename E, int TB, bool AT, bool BT>
+template <typename E, int TB, bool AT, bool BT, int GATE>
 __global__ __launch_bounds__(64 * WAVES, 2) void gemm_wave_kernel(WaveGemmArgs a) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
-  wave_tile<E, TB, AT, BT>(a, blockIdx.x, smem);
+  wave_tile<E, TB, AT, BT, GATE>(a, blockIdx.x, smem);
 }
 
 // Sums over the rows of a matrix, 64 columns to a workgroup: eight lanes take a row's columns, so a wave has eight rows and a pass of
@@ -347,11 +353,11 @@ struct GroupArgs {
   ColumnSums sums;
   int blocks_sum;             // for each of them
 };
-template <typename E, int TB>
+template <typename E, int TB, int GATE>
 __global__ __launch_bounds__(64 * WAVES, 2) void gemm_wave_group_kernel(GroupArgs a) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
   int block = blockIdx.x;
-  if (block < a.blocks_nn) return wave_tile<E, TB, false, true>(a.nn, block, smem);
+  if (block < a.blocks_nn) return wave_tile<E, TB, false, true, GATE>(a.nn, block, smem);
   block -= a.blocks_nn;
   if (block < a.blocks_tn) return wave_tile<E, TB, true, true>(a.tn, block, smem);
   block -= a.blocks_tn;
@@ -361,32 +367,34 @@ __global__ __launch_bounds__(64 * WAVES, 2) void gemm_wave_group_kernel(GroupArg
   else column_sums<bf16>(s, a.sums.rows, a.sums.C, block, a.sums.out_f32, a.sums.accumulate, smem);
 }
 
-template <typename E, int TB, bool AT, bool BT>
+template <typename E, int TB, bool AT, bool BT, int GATE = GATE_NONE>
 int launch(WaveGemmArgs a, hipStream_t st) {
   constexpr int smem = WAVES * 2 * TB * 128;
   static unsigned long long attr_done = 0;
   int device;
   if (!attr_is_set(attr_done, &device)) {
-    if (hipFuncSetAttribute((const void *)gemm_wave_kernel<E, TB, AT, BT>, hipFuncAttributeMaxDynamicSharedMemorySize, smem) != hipSuccess)
+    if (hipFuncSetAttribute((const void *)gemm_wave_kernel<E, TB, AT, BT, GATE>, hipFuncAttributeMaxDynamicSharedMemorySize, smem) != hipSuccess)
       return MTNLG_HIP_ERROR;
     attr_mark_set(attr_done, device);
   }
-  gemm_wave_kernel<E, TB, AT, BT><<<dim3((unsigned)(((int64_t)a.tiles_m * a.tiles_n + 7) / 8 * 8)), 64 * WAVES, smem, st>>>(a);
+  gemm_wave_kernel<E, TB, AT, BT, GATE><<<dim3((unsigned)(((int64_t)a.tiles_m * a.tiles_n + 7) / 8 * 8)), 64 * WAVES, smem, st>>>(a);
   return check_launch();
 }
 
 template <typename E, int TB>
-int launch_layout(int layout, WaveGemmArgs a, hipStream_t st) {
+int launch_layout(int layout, WaveGemmArgs a, hipStream_t st, int gate = GATE_NONE) {
   const int64_t tm = (a.M + TB - 1) / TB, tn = (a.N + TB - 1) / TB;
   if (tm * tn > (1 << 28)) return MTNLG_UNSUPPORTED_SHAPE;
   a.tiles_m = (int)tm;
   a.tiles_n = (int)tn;
+  if (gate == GATE_FWD) return launch<E, TB, false, false, GATE_FWD>(a, st);
+  if (gate == GATE_BWD) return launch<E, TB, false, true, GATE_BWD>(a, st);
   if (layout == MTNLG_GEMM_NT) return launch<E, TB, false, false>(a, st);
   if (layout == MTNLG_GEMM_NN) return launch<E, TB, false, true>(a, st);
   return launch<E, TB, true, true>(a, st);
 }
 
-template <typename E, int TB>
+template <typename E, int TB, int GATE>
 int launch_group(GroupArgs a, hipStream_t st) {
   auto blocks = [](WaveGemmArgs &p) {
     p.tiles_m = (int)((p.M + TB - 1) / TB);
@@ -399,11 +407,11 @@ int launch_group(GroupArgs a, hipStream_t st) {
   static unsigned long long attr_done = 0;
   int device;
   if (!attr_is_set(attr_done, &device)) {
-    if (hipFuncSetAttribute((const void *)gemm_wave_group_kernel<E, TB>, hipFuncAttributeMaxDynamicSharedMemorySize, smem) != hipSuccess)
+    if (hipFuncSetAttribute((const void *)gemm_wave_group_kernel<E, TB, GATE>, hipFuncAttributeMaxDynamicSharedMemorySize, smem) != hipSuccess)
       return MTNLG_HIP_ERROR;
     attr_mark_set(attr_done, device);
   }
-  gemm_wave_group_kernel<E, TB><<<dim3((unsigned)(a.blocks_nn + a.blocks_tn + a.sums.count * a.blocks_sum)), 64 * WAVES, smem, st>>>(a);
+  gemm_wave_group_kernel<E, TB, GATE><<<dim3((unsigned)(a.blocks_nn + a.blocks_tn + a.sums.count * a.blocks_sum)), 64 * WAVES, smem, st>>>(a);
   return check_launch();
 }
 
@@ -499,14 +507,31 @@ int gemm_wave_group_tile(int dtype, const GemmCall &nn, const GemmCall &tn, int 
   return pick_group(dtype, nn, tn, sums ? sum_rows : 0, separate);
 }
 
-int gemm_wave_group(int dtype, const GemmCall &nn, const GemmCall &tn, const ColumnSums &sums, int tile, hipStream_t stream) {
+// The products with the gate's epilogues: whether these kernels can take them, and their launch
+bool gated_wave_takes(int dtype, int64_t h, int64_t F) { return (F + 64) * h * (dtype == MTNLG_F32 ? 4 : 2) < (int64_t)RECORDS - 256; }
+int gated_wave(int dtype, int mode, int kind, int64_t T, int64_t h, int64_t F, const void *A, const void *B, void *z, void *C, int tile,
+               hipStream_t stream) {
+  const int layout = mode == GATE_FWD ? MTNLG_GEMM_NT : MTNLG_GEMM_NN;
+  const int64_t N = mode == GATE_FWD ? 2 * F : F;
+  if (!gated_wave_takes(dtype, h, F) || !gemm_wave_takes(dtype, layout, T, N, h, A, B, C, nullptr, z)) return MTNLG_UNSUPPORTED_SHAPE;
+  const WaveGemmArgs a{T, N, h, h, mode == GATE_FWD ? h : F, A, B, C, EpiArgs{nullptr, z, (uint32_t)kind}, 0, 0};
+  LaunchScope scope(MTNLG_K_GEMM_NT + layout, stream);
+  if (dtype == MTNLG_F32) return tile == 32 ? launch_layout<float, 32>(layout, a, stream, mode) : launch_layout<float, 64>(layout, a, stream, mode);
+  return tile == 32 ? launch_layout<bf16, 32>(layout, a, stream, mode) : launch_layout<bf16, 64>(layout, a, stream, mode);
+}
+
+int gemm_wave_group(int dtype, const GemmCall &nn, const GemmCall &tn, const ColumnSums &sums, int tile, hipStream_t stream, bool gate) {
   if (tile != 32 && (tile != 64 || dtype == MTNLG_F32)) return MTNLG_INVALID_ARG;
   const GroupArgs a{{nn.M, nn.N, nn.K, nn.K, nn.N, nn.A, nn.B, nn.C, EpiArgs{nullptr, nn.aux, nn.epi}, 0, 0},
                     {tn.M, tn.N, tn.K, tn.M, tn.N, tn.A, tn.B, tn.C, EpiArgs{nullptr, tn.aux, tn.epi}, 0, 0},
                     0, 0, sums, (int)((sums.C + 63) / 64)};
   LaunchScope scope(MTNLG_K_GEMM_NN, stream, MTNLG_K_GEMM_TN);   // the two products have the same number of operations
-  if (dtype == MTNLG_F32) return launch_group<float, 32>(a, stream);
-  return tile == 32 ? launch_group<bf16, 32>(a, stream) : launch_group<bf16, 64>(a, stream);
+  if (gate) {
+    if (dtype == MTNLG_F32) return launch_group<float, 32, GATE_BWD>(a, stream);
+    return tile == 32 ? launch_group<bf16, 32, GATE_BWD>(a, stream) : launch_group<bf16, 64, GATE_BWD>(a, stream);
+  }
+  if (dtype == MTNLG_F32) return launch_group<float, 32, GATE_NONE>(a, stream);
+  return tile == 32 ? launch_group<bf16, 32, GATE_NONE>(a, stream) : launch_group<bf16, 64, GATE_NONE>(a, stream);
 }
 
 }  // namespace mtnlg

@@ -33,7 +33,8 @@ def call_gated(desc, backward, ws=BIG, **kw):
 @pytest.mark.parametrize("bad,status", [(dict(dtype=2), INVALID), (dict(gate=-1), INVALID), (dict(gate=3), INVALID), (dict(tokens=0), INVALID),
                                         (dict(tokens=-5), INVALID), (dict(hidden=0), INVALID), (dict(ffn=0), INVALID), (dict(flags=1), INVALID),
                                         (dict(flags=8), INVALID), (dict(hidden=60), SHAPE), (dict(ffn=4), SHAPE), (dict(hidden=32776), SHAPE),
-                                        (dict(ffn=(1 << 20) + 8), SHAPE), (dict(tokens=(1 << 22) - 63), SHAPE)])
+                                        (dict(ffn=(1 << 20) + 8), SHAPE), (dict(tokens=(1 << 22) - 63), SHAPE),
+                                        (dict(hidden=32768, ffn=(1 << 16) - 248), SHAPE), (dict(dtype=B.F32, hidden=32768, ffn=(1 << 15) - 120), SHAPE)])
 def test_gated_descriptors_that_are_refused(bad, status, backward):
     assert call_gated(gated(**bad), backward) == status
     assert M.mtnlg_gated_ffn_workspace(gated(**bad)) == 0

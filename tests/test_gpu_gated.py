@@ -92,6 +92,8 @@ def check_backward(kind, s, rows=slice(None), dx=True):
 
 def check_weights(s, got1, got2, turns=1, start=0.0):
     for got, (want, e), what in ((got1, product(s["dz"].T, s["x"].T), "dw_fc1"), (got2, product(s["dy"].T, s["g"].T), "dw_fc2")):
+        if got is None:
+            continue
         u = HALF_STEP[got.dtype]
         within(got, turns * want + start, turns * (e + 2 * u * (turns * want.abs() + abs(start) + e)), what)
 
@@ -155,13 +157,15 @@ def test_gradients_that_are_not_wanted(dtype, T):
     ws = room(desc)
     forward(desc, s, ws)
     backward(desc, s, ws)
-    want = {k: s[k].clone() for k in ("dz", "dx", "dw_fc1", "dw_fc2")}
+    outs = ("dz", "dx", "dw_fc1", "dw_fc2")
     for left_out in (("dx",), ("dw_fc1",), ("dw_fc2",), ("dw_fc1", "dw_fc2"), ("dx", "dw_fc1", "dw_fc2")):
-        for k in want:
+        for k in outs:
             s[k].fill_(float("nan"))
         backward(desc, s, ws, **{k: None for k in left_out})
-        for k in want:
-            assert torch.isnan(s[k]).all() if k in left_out else torch.equal(s[k], want[k]), (left_out, k)
+        assert all(torch.isnan(s[k]).all() for k in left_out)
+        # (not bit for bit what all of them give: products that are one launch together may be other kernels alone, with sums in another order)
+        check_backward("silu", s, dx="dx" not in left_out)
+        check_weights(s, s["dw_fc1"] if "dw_fc1" not in left_out else None, s["dw_fc2"] if "dw_fc2" not in left_out else None)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
