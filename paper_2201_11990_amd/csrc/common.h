@@ -362,8 +362,7 @@ struct ColumnSums {
 // have to be taken; sums: how many matrices, of how many rows and columns
 int gemm_wave_group_tile(int dtype, const GemmCall &nn, const GemmCall &tn, int sums, int64_t sum_rows, int64_t sum_cols, double separate_nn,
                          double separate_tn);
-int gemm_wave_group(int dtype, const GemmCall &nn, const GemmCall &tn, const ColumnSums &sums, int tile, hipStream_t stream,
-                    bool gate = false);   // gate: nn with the gate's backward (gate.h: GATE_BWD)
+int gemm_wave_group(int dtype, const GemmCall &nn, const GemmCall &tn, const ColumnSums &sums, int tile, hipStream_t stream);
 // LayerNorm backward without the sums over rows; left: what is to be added up afterwards, over so many rows at most
 int layernorm_bwd_rows(int dtype, int64_t T, int64_t h, const void *x, const void *gamma, const float *mean, const float *rstd,
                        const void *dout, const void *dres, void *dx, void *dgamma, void *dbeta, void *colsum_dx, int grad_f32,

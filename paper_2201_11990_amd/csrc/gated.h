@@ -13,6 +13,7 @@ int gated_mfma_bwd(int kind, int64_t T, int64_t h, int64_t F, const void *dy, co
 bool gated_wave_takes(int dtype, int64_t h, int64_t F);
 int gated_wave(int dtype, int mode, int kind, int64_t T, int64_t h, int64_t F, const void *A, const void *B, void *z, void *C, int tile,
                hipStream_t stream);
+int gated_wave_group(int dtype, const GemmCall &nn, const GemmCall &tn, int tile, hipStream_t stream);   // nn: the one with the gate's backward
 int gated_parts(int mode, int kind, int64_t T, int64_t h, int64_t F, const void *A, const void *B, void *z, void *C, hipStream_t stream);
 
 }  // namespace mtnlg

@@ -121,7 +121,7 @@ int mtnlg_gated_ffn_bwd(const mtnlg_gated_desc *desc, const void *x, const void 
   const GemmCall to_dz{s.T, s.F, s.h, dy, w_fc2, dz, const_cast<void *>(z), (uint32_t)s.gate}, to_dw2{s.h, s.F, s.T, dy, g, dw_fc2, nullptr, epi};
   const int tile2 = dw_fc2 ? gemm_wave_group_tile(s.dtype, to_dz, to_dw2, 0, 0, 0, gated_time(s, GATE_BWD), time(MTNLG_GEMM_TN, to_dw2)) : 0;
   if (tile2) {
-    MTNLG_TRY(gemm_wave_group(s.dtype, to_dz, to_dw2, ColumnSums{}, tile2, st, true));
+    MTNLG_TRY(gated_wave_group(s.dtype, to_dz, to_dw2, tile2, st));
   } else {
     if (dw_fc2) MTNLG_TRY(gemm(MTNLG_GEMM_TN, to_dw2));
     MTNLG_TRY(gated_product(s, GATE_BWD, dy, w_fc2, const_cast<void *>(z), dz, workspace, st));

@@ -35,8 +35,8 @@ typedef __attribute__((ext_vector_type(2))) float f32x2;
 struct Pair {
   float v[2][8];
   // first: element (first row of the blocks, k = 0), row row0 of the operand; slabs past the last one: zeros
-  // half: rows of the weights in pairs of both halves (gate.h), so many rows apart; 0: as they lie
-  template <bool ROWC>
+  // PAIRED: rows of the weights in pairs of both halves (gate.h), `half` rows apart, unless that is 0
+  template <bool ROWC, bool PAIRED>
   __device__ __forceinline__ void load(const float *first, int64_t ld, int64_t rows_left, int64_t row0, int64_t k0, int64_t K, int lane, int64_t half) {
     const int g = lane >> 4, r = lane & 15;
     if constexpr (!ROWC) {
@@ -45,7 +45,7 @@ struct Pair {
       for (int b = 0; b < 2; ++b)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const uint32_t off = (uint32_t)((half ? gate_row(16 * b + r, half) : 16 * b + r) * ld * 4 + (16 * h + 4 * g) * 4);
+          const uint32_t off = (uint32_t)((PAIRED && half ? gate_row(16 * b + r, half) * ld : (16 * b + r) * ld) * 4 + (16 * h + 4 * g) * 4);
           const f32x4 t = __builtin_bit_cast(
               f32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, 16 * b + r < rows_left && k0 + 16 * h + 4 * g < K ? off : OUTSIDE, 0, 0));
 #pragma unroll
@@ -121,7 +121,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void gemm_parts_kernel(PartsArgs a) 
   // One body for each way of loading: where the two kinds meet in one, the compiler waits for all loads at their first use.
   auto run = [&](auto rowc) {
     auto load = [&](auto slot, int s) {
-      raw[decltype(slot)::value].template load<decltype(rowc)::value != 0>(first, ld, rows_left, row0, (int64_t)s * SLAB_K, a.K, lane, half);
+      raw[decltype(slot)::value].template load<decltype(rowc)::value != 0, GATE == GATE_FWD>(first, ld, rows_left, row0, (int64_t)s * SLAB_K, a.K, lane, half);
     };
     load(Num<0>{}, 0);
     load(Num<1>{}, 1);
@@ -189,8 +189,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void gemm_parts_kernel(PartsArgs a) 
       for (int j = 0; j < 2; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 1
     for (int s = 0; s < nk; ++s) {   // the same blocks as fp32 values: elements 0-3 in the place of the first part, 4-7 of the second
-      if (is_a) raw[0].load<AT>(first, ld, rows_left, row0, (int64_t)s * SLAB_K, a.K, lane, half);
-      else raw[0].load<BT>(first, ld, rows_left, row0, (int64_t)s * SLAB_K, a.K, lane, half);
+      if (is_a) raw[0].load<AT, GATE == GATE_FWD>(first, ld, rows_left, row0, (int64_t)s * SLAB_K, a.K, lane, half);
+      else raw[0].load<BT, GATE == GATE_FWD>(first, ld, rows_left, row0, (int64_t)s * SLAB_K, a.K, lane, half);
       __syncthreads();
 #pragma unroll
       for (int b = 0; b < 2; ++b)

@@ -38,7 +38,8 @@ typedef __attribute__((address_space(3))) i16x4 *lds_i16x4_ptr;
 //   Row-contiguous ([k][row] in memory): [k][TB rows], the units of a k-row permuted so that the reads below spread over the banks:
 //     bf16 (transposing reads: 16 lanes take 4 k-rows x 32 bytes) by bits 1 and 3 of k; fp32, 32 rows: neighbouring k-rows
 //     swap places where bit 2 of k is set; fp32, 64 rows: 256-byte k-rows need nothing.
-template <typename E, int TB, bool ROWC>
+// PAIRED: rows of the weights in pairs of both halves (gate.h), `half` rows apart.
+template <typename E, int TB, bool ROWC, bool PAIRED = false>
 struct Slab {
   static constexpr int ES = sizeof(E), EPU = 16 / ES, SK = 128 / ES;   // element size, elements of a unit, k of a slab
   static constexpr int NI = TB / 8;          // DMA instructions (1 KB each)
@@ -52,13 +53,12 @@ struct Slab {
   static __device__ __forceinline__ int place(int k) { return ES == 4 && TB == 32 ? k ^ ((k >> 2) & 1) : k; }   // (its own inverse)
 
   uint32_t off[NI];   // byte offsets of this lane's units from the slab's first element; rows past the edge lie outside
-  // half: rows of the weights in pairs of both halves (gate.h), so many rows apart; 0: as they lie
   __device__ __forceinline__ Slab(int64_t ld, int64_t rows_left, int lane, int64_t half = 0) {
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
       if constexpr (!ROWC) {
         const int row = 8 * i + (lane >> 3), c = (lane & 7) ^ (lane >> 3);
-        off[i] = row < rows_left ? (uint32_t)((half ? gate_row(row, half) : row) * ld * ES + c * 16) : OUTSIDE;
+        off[i] = row < rows_left ? (uint32_t)((PAIRED ? gate_row(row, half) * ld : row * ld) * ES + c * 16) : OUTSIDE;
       } else {
         const int q = 64 * i + lane, k = place(q / UPR), u = (q % UPR) ^ mask(k);
         off[i] = u * EPU < rows_left ? (uint32_t)(k * ld * ES + u * 16) : OUTSIDE;
@@ -144,7 +144,7 @@ struct Frag32 {
 template <typename E, int TB, bool AT, bool BT, int GATE = GATE_NONE>
 __device__ __forceinline__ void wave_tile(const WaveGemmArgs &a, int block, char *smem) {
   using SA = Slab<E, TB, AT>;
-  using SB = Slab<E, TB, BT>;
+  using SB = Slab<E, TB, BT, GATE == GATE_FWD>;
   constexpr int NB = TB / 16, NV = NB * NB, STAGE = SA::BYTES + SB::BYTES, SK = SA::SK;
   static_assert(NV * 1024 <= STAGE, "a wave's partial tile fits its stage");
   const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
@@ -162,7 +162,7 @@ __device__ __forceinline__ void wave_tile(const WaveGemmArgs &a, int block, char
   const E *A = static_cast<const E *>(a.A) + (AT ? m0 : m0 * a.lda);
   const E *B = static_cast<const E *>(a.B) + (BT ? n0 : (GATE == GATE_FWD ? n0 / 2 : n0) * a.ldb);
   const SA sa(a.lda, a.M - m0, lane);
-  const SB sb(a.ldb, a.N - n0, lane, GATE == GATE_FWD ? a.N / 2 : 0);
+  const SB sb(a.ldb, a.N - n0, lane, a.N / 2);
   char *const stage = smem + wave * STAGE;
   const uint32_t lds = lds_address(stage);
   const int slabs = (int)((a.K + SK - 1) / SK);
@@ -520,18 +520,21 @@ int gated_wave(int dtype, int mode, int kind, int64_t T, int64_t h, int64_t F, c
   return tile == 32 ? launch_layout<bf16, 32>(layout, a, stream, mode) : launch_layout<bf16, 64>(layout, a, stream, mode);
 }
 
-int gemm_wave_group(int dtype, const GemmCall &nn, const GemmCall &tn, const ColumnSums &sums, int tile, hipStream_t stream, bool gate) {
+template <int GATE>
+static int launch_group(int dtype, const GemmCall &nn, const GemmCall &tn, const ColumnSums &sums, int tile, hipStream_t stream) {
   if (tile != 32 && (tile != 64 || dtype == MTNLG_F32)) return MTNLG_INVALID_ARG;
   const GroupArgs a{{nn.M, nn.N, nn.K, nn.K, nn.N, nn.A, nn.B, nn.C, EpiArgs{nullptr, nn.aux, nn.epi}, 0, 0},
                     {tn.M, tn.N, tn.K, tn.M, tn.N, tn.A, tn.B, tn.C, EpiArgs{nullptr, tn.aux, tn.epi}, 0, 0},
                     0, 0, sums, (int)((sums.C + 63) / 64)};
   LaunchScope scope(MTNLG_K_GEMM_NN, stream, MTNLG_K_GEMM_TN);   // the two products have the same number of operations
-  if (gate) {
-    if (dtype == MTNLG_F32) return launch_group<float, 32, GATE_BWD>(a, stream);
-    return tile == 32 ? launch_group<bf16, 32, GATE_BWD>(a, stream) : launch_group<bf16, 64, GATE_BWD>(a, stream);
-  }
-  if (dtype == MTNLG_F32) return launch_group<float, 32, GATE_NONE>(a, stream);
-  return tile == 32 ? launch_group<bf16, 32, GATE_NONE>(a, stream) : launch_group<bf16, 64, GATE_NONE>(a, stream);
+  if (dtype == MTNLG_F32) return launch_group<float, 32, GATE>(a, stream);
+  return tile == 32 ? launch_group<bf16, 32, GATE>(a, stream) : launch_group<bf16, 64, GATE>(a, stream);
+}
+int gemm_wave_group(int dtype, const GemmCall &nn, const GemmCall &tn, const ColumnSums &sums, int tile, hipStream_t stream) {
+  return launch_group<GATE_NONE>(dtype, nn, tn, sums, tile, stream);
+}
+int gated_wave_group(int dtype, const GemmCall &nn, const GemmCall &tn, int tile, hipStream_t stream) {
+  return launch_group<GATE_BWD>(dtype, nn, tn, ColumnSums{}, tile, stream);
 }
 
 }  // namespace mtnlg
