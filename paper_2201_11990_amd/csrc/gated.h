@@ -16,4 +16,9 @@ int gated_wave(int dtype, int mode, int kind, int64_t T, int64_t h, int64_t F, c
 int gated_wave_group(int dtype, const GemmCall &nn, const GemmCall &tn, int tile, hipStream_t stream);   // nn: the one with the gate's backward
 int gated_parts(int mode, int kind, int64_t T, int64_t h, int64_t F, const void *A, const void *B, void *z, void *C, hipStream_t stream);
 
+// few tokens, bf16: forward's products (N, K: rows and columns of the weights)
+bool gated_tokens_takes(int64_t T, int64_t N, int64_t K);
+int gated_tokens_fwd(int kind, int64_t T, int64_t h, int64_t F, const void *x, const void *w_fc1, void *z, void *g, hipStream_t stream);
+int gated_tokens_out(int64_t T, int64_t h, int64_t F, const void *g, const void *w_fc2, void *y, hipStream_t stream);
+
 }  // namespace mtnlg

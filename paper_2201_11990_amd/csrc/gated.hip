@@ -61,6 +61,7 @@ double gated_time(const Sizes &s, int mode) {
 int gated_product(const Sizes &s, int mode, const void *A, const void *B, void *z, void *C, void *ws, hipStream_t st) {
   const int layout = mode == GATE_FWD ? MTNLG_GEMM_NT : MTNLG_GEMM_NN;
   const int64_t N = mode == GATE_FWD ? 2 * s.F : s.F;
+  if (s.dtype == MTNLG_BF16 && mode == GATE_FWD && gated_tokens_takes(s.T, N, s.h)) return gated_tokens_fwd(s.gate, s.T, s.h, s.F, A, B, z, C, st);
   if (const int tile = gemm_wave_pick(s.dtype, layout, s.T, N, s.h, gated_time(s, mode)))
     return gated_wave(s.dtype, mode, s.gate, s.T, s.h, s.F, A, B, z, C, tile, st);
   if (s.dtype == MTNLG_F32) return gated_parts(mode, s.gate, s.T, s.h, s.F, A, B, z, C, st);
@@ -94,6 +95,7 @@ int mtnlg_gated_ffn_fwd(const mtnlg_gated_desc *desc, const void *x, const void 
   if (workspace_bytes < need) return MTNLG_WORKSPACE_TOO_SMALL;
   hipStream_t st = (hipStream_t)stream;
   MTNLG_TRY(gated_product(s, GATE_FWD, x, w_fc1, z, g, workspace, st));
+  if (s.dtype == MTNLG_BF16 && gated_tokens_takes(s.T, s.h, s.F)) return gated_tokens_out(s.T, s.h, s.F, g, w_fc2, y, st);
   return mtnlg_gemm(s.dtype, MTNLG_GEMM_NT, s.T, s.h, s.F, g, w_fc2, y, nullptr, nullptr, 0, workspace, s.gemm_ws, stream);
 }
 
