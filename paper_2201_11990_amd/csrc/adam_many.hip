@@ -10,6 +10,7 @@
 // nearest, a moment whose change in a step is below half a code (beta2 = 0.95 takes 5 % of v, 2.5 % of r; a code is 6 to 12 % wide) would never move.
 #include <algorithm>
 #include <new>
+#include <type_traits>
 
 #include "adam.h"
 
@@ -69,19 +70,19 @@ __device__ __forceinline__ int tensor_of(const A &a, uint32_t c) {
   return lo;
 }
 
-// elements i .. i + 3 of n (zeros beyond), aligned for one access
-template <typename E>
+// elements i .. i + 3 of n (zeros beyond), aligned for one access; WHOLE: all of them are there
+template <bool WHOLE, typename E>
 __device__ __forceinline__ f32x4 load_some(const E *p, int64_t i, int64_t n) {
-  if (i + 4 <= n) return load4(p + i);
+  if (WHOLE || i + 4 <= n) return load4(p + i);
   f32x4 r = {};
 #pragma unroll
   for (int e = 0; e < 3; ++e)
     if (i + e < n) r[e] = to_f32(p[i + e]);
   return r;
 }
-template <typename E>
+template <bool WHOLE, typename E>
 __device__ __forceinline__ void store_some(E *p, int64_t i, int64_t n, f32x4 x) {
-  if (i + 4 <= n) {
+  if (WHOLE || i + 4 <= n) {
     if constexpr (sizeof(E) == 4) *reinterpret_cast<f32x4 *>(p + i) = x;
     else *reinterpret_cast<bf16x4 *>(p + i) = bf16x4{(bf16)x[0], (bf16)x[1], (bf16)x[2], (bf16)x[3]};
     return;
@@ -91,16 +92,18 @@ __device__ __forceinline__ void store_some(E *p, int64_t i, int64_t n, f32x4 x) 
     if (i + e < n) p[i + e] = from_f32<E>(x[e]);
 }
 // four codes
+template <bool WHOLE>
 __device__ __forceinline__ uint32_t load_codes(const uint8_t *p, int64_t i, int64_t n) {
-  if (i + 4 <= n) return *reinterpret_cast<const uint32_t *>(p + i);
+  if (WHOLE || i + 4 <= n) return *reinterpret_cast<const uint32_t *>(p + i);
   uint32_t r = 0;
 #pragma unroll
   for (int e = 0; e < 3; ++e)
     if (i + e < n) r |= (uint32_t)p[i + e] << (8 * e);
   return r;
 }
+template <bool WHOLE>
 __device__ __forceinline__ void store_codes(uint8_t *p, int64_t i, int64_t n, uint32_t x) {
-  if (i + 4 <= n) {
+  if (WHOLE || i + 4 <= n) {
     *reinterpret_cast<uint32_t *>(p + i) = x;
     return;
   }
@@ -108,9 +111,9 @@ __device__ __forceinline__ void store_codes(uint8_t *p, int64_t i, int64_t n, ui
   for (int e = 0; e < 3; ++e)
     if (i + e < n) p[i + e] = (uint8_t)(x >> (8 * e));
 }
-__device__ __forceinline__ f32x4 decode(uint32_t codes, float scale) {
+__device__ __forceinline__ f32x4 decode(uint32_t codes) {
   const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, true);
-  return f32x4{lo[0] * scale, lo[1] * scale, hi[0] * scale, hi[1] * scale};
+  return f32x4{lo[0], lo[1], hi[0], hi[1]};
 }
 
 // 32 random bits for element e of a block: products, shifts and exclusive ors on the step's two words, the block's number and e.
@@ -126,21 +129,113 @@ __device__ __forceinline__ uint32_t element_bits(uint32_t key, uint32_t e) {
   return h ^ (h >> 16);
 }
 
-// The code of x * inv (inv: the reciprocal of the block's scale), rounded up where the part of a step that is left and u = (r + 1/2) / 2^16 make a whole
-// one.  From 2^-6 on a code is the upper bits of the fp32 value, whose other 20 bits are that part; below, codes are multiples of 2^-9, and
-// adding 2^-6 brings the value to where they are the upper bits too.
-template <int LEAST>
-__device__ __forceinline__ uint32_t encode(float x, float inv, uint32_t r) {
-  const float y = fabsf(x) * inv, most = fminf(y, 448.0f);
-  const bool low = most < 0x1p-6f;
-  const uint32_t bits = __builtin_bit_cast(uint32_t, low ? most + 0x1p-6f : most) + (r * 16 + 8);
-  uint32_t code = (bits >> 20) - (low ? 968u : 960u);   // exponents: 127 there, 7 here
-  if (LEAST > 0) code = x != 0.0f && code < (uint32_t)LEAST ? (uint32_t)LEAST : code;
-  code = y == y ? code : 0x7Fu;
-  return code | ((__builtin_bit_cast(uint32_t, x) >> 24) & 0x80u);
+// Codes of four quotients, rounded up where the part of a step that is left and u make a whole one: the conversion instruction adds the upper 20 bits of a
+// random word to what the code leaves of the value, below 2^-6 too, where a step is 2^-9.  Those bits are of u = (16 random bits + 1/2) / 2^16.
+__device__ __forceinline__ uint32_t encode(const float (&y)[4], const uint32_t (&u)[4]) {
+  int w = __builtin_amdgcn_cvt_sr_fp8_f32(y[0], (int)u[0], 0, 0);
+  w = __builtin_amdgcn_cvt_sr_fp8_f32(y[1], (int)u[1], w, 1);
+  w = __builtin_amdgcn_cvt_sr_fp8_f32(y[2], (int)u[2], w, 2);
+  return (uint32_t)__builtin_amdgcn_cvt_sr_fp8_f32(y[3], (int)u[3], w, 3);
 }
-// scale of a block with this largest magnitude
-__device__ __forceinline__ float scale_of(float most) { return most > 0.0f ? fmaxf(most / 448.0f, 0x1p-126f) : 1.0f; }
+// the largest of 64 lanes' values that are not negative, in all of them: within rows of 16 lanes, from row to row, from the last lane
+__device__ __forceinline__ float wave_most(float x) {
+  auto step = [&](auto ctrl) {
+    x = fmaxf(x, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value, 0xF, 0xF, false)));
+  };
+  step(std::integral_constant<int, 0x111>{});   // row_shr 1, 2, 4, 8
+  step(std::integral_constant<int, 0x112>{});
+  step(std::integral_constant<int, 0x114>{});
+  step(std::integral_constant<int, 0x118>{});
+  step(std::integral_constant<int, 0x142>{});   // row_bcast 15, 31
+  step(std::integral_constant<int, 0x143>{});
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
+}
+// scale of a block with this largest magnitude, and what its values are multiplied with: less than the reciprocal by 2^-22, more than roundings can make
+// up for, so that no quotient passes 448
+__device__ __forceinline__ float scale_of(float most) { return most > 0.0f ? fmaxf(most * (1.0f / 448.0f), 0x1p-126f) : 1.0f; }
+__device__ __forceinline__ float inverse_of(float scale) { return __builtin_amdgcn_rcpf(scale) * (1.0f - 0x1p-22f); }
+
+// The four elements of a thread at i
+template <bool EIGHT, typename G, bool WHOLE>
+struct Turn {
+  f32x4 p, g, m, v;
+  uint32_t mc, vc;
+  float ms, vs;
+  __device__ __forceinline__ void load(const StepTensor &t, int64_t i) {
+    p = load_some<WHOLE>(t.p, i, t.count);
+    g = load_some<WHOLE>(static_cast<const G *>(t.g), i, t.count);
+    if constexpr (EIGHT) {
+      mc = load_codes<WHOLE>(static_cast<const uint8_t *>(t.m), i, t.count);
+      vc = load_codes<WHOLE>(static_cast<const uint8_t *>(t.v), i, t.count);
+      ms = t.m_scale[i / kBlock];
+      vs = t.v_scale[i / kBlock];
+    } else {
+      m = load_some<WHOLE>(static_cast<const float *>(t.m), i, t.count);
+      v = load_some<WHOLE>(static_cast<const float *>(t.v), i, t.count);
+    }
+  }
+  __device__ __forceinline__ void step(const StepArgs &s, const StepTensor &t, float coef, int64_t i) {
+    if constexpr (EIGHT) {
+      // adam_one with the root of v taken once, for the update and for the state, by the hardware's root and reciprocal (1 ulp each)
+      const AdamArgs &a = s.a;
+      const float root_c2 = sqrtf(a.inv_c2), m_old = ms * a.beta1, r_old = vs * sqrtf(a.beta2);
+      f32x4 r = decode(vc);
+      m = decode(mc);
+      float mm = 0.0f, rm = 0.0f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float ge = g[e] * coef;
+        m[e] = m[e] * m_old + (1.0f - a.beta1) * ge;
+        r[e] *= r_old;
+        r[e] = __builtin_amdgcn_sqrtf(r[e] * r[e] + (1.0f - a.beta2) * ge * ge);
+        const float update = m[e] * a.inv_c1 * __builtin_amdgcn_rcpf(r[e] * root_c2 + a.eps);
+        p[e] = p[e] - a.lr * (update + t.wd * p[e]);
+        mm = fmaxf(mm, fabsf(m[e]));
+        rm = fmaxf(rm, r[e]);
+      }
+      const int64_t b = i / kBlock;
+      ms = scale_of(wave_most(mm));
+      vs = scale_of(wave_most(rm));
+      const float mi = inverse_of(ms), ri = inverse_of(vs);
+      const uint32_t key = block_key(__builtin_amdgcn_readfirstlane(t.first_block + (uint32_t)b), s.key_lo, s.key_hi);
+      float ym[4], yr[4];
+      uint32_t um[4], ur[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t h = element_bits(key, (threadIdx.x & 63) * 4 + e);
+        um[e] = (h << 16) | 0x8000u;
+        ur[e] = (h & 0xFFFF0000u) | 0x8000u;
+        ym[e] = m[e] * mi;
+        // one step at least of a root that is not zero: what lies below it has the code of it, however it is rounded
+        const float y = r[e] * ri, least = r[e] > 0.0f ? 0x1p-9f : 0.0f;
+        yr[e] = y < least ? least : y;
+      }
+      mc = encode(ym, um);
+      vc = encode(yr, ur);
+      store_codes<WHOLE>(static_cast<uint8_t *>(t.m), i, t.count, mc);
+      store_codes<WHOLE>(static_cast<uint8_t *>(t.v), i, t.count, vc);
+      if ((threadIdx.x & 63) == 0) {
+        t.m_scale[b] = ms;
+        t.v_scale[b] = vs;
+      }
+    } else {
+      AdamArgs a = s.a;
+      a.wd = t.wd;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float pe = p[e], me = m[e], ve = v[e];
+        adam_one(a, coef, g[e], pe, me, ve);
+        p[e] = pe;
+        m[e] = me;
+        v[e] = ve;
+      }
+      store_some<WHOLE>(static_cast<float *>(t.m), i, t.count, m);
+      store_some<WHOLE>(static_cast<float *>(t.v), i, t.count, v);
+    }
+    store_some<WHOLE>(t.p, i, t.count, p);
+    if (t.w != nullptr) store_some<WHOLE>(t.w, i, t.count, p);
+  }
+};
 
 template <bool EIGHT, typename G>
 __global__ __launch_bounds__(256) void adam_many_kernel(StepArgs s) {
@@ -152,83 +247,52 @@ __global__ __launch_bounds__(256) void adam_many_kernel(StepArgs s) {
   }
   for (uint32_t c = blockIdx.x; c < s.chunks; c += gridDim.x) {
     const StepTensor &t = s.of[tensor_of(s, c)];
-    const int64_t n = t.count, first = (int64_t)(c - t.first_chunk) * kChunk + threadIdx.x * 4;
-    AdamArgs a = s.a;
-    a.wd = t.wd;
+    const int64_t base = (int64_t)(c - t.first_chunk) * kChunk, first = base + threadIdx.x * 4;
+    if (base + kChunk <= t.count) {   // all loads of a chunk at once
+      Turn<EIGHT, G, true> turn[kTurns];
 #pragma unroll
-    for (int u = 0; u < kTurns; ++u) {
-      const int64_t i = first + u * 1024;
-      f32x4 p = load_some(t.p, i, n), g = load_some(static_cast<const G *>(t.g), i, n), m, v;
-      if constexpr (EIGHT) {
-        if (i - (threadIdx.x & 63) * 4 >= n) break;   // (the whole wave)
-        const int64_t b = i / kBlock;
-        m = decode(load_codes(static_cast<const uint8_t *>(t.m), i, n), t.m_scale[b]);
-        v = decode(load_codes(static_cast<const uint8_t *>(t.v), i, n), t.v_scale[b]);
-        v *= v;
-      } else {
-        m = load_some(static_cast<const float *>(t.m), i, n);
-        v = load_some(static_cast<const float *>(t.v), i, n);
-      }
+      for (int u = 0; u < kTurns; ++u) turn[u].load(t, first + u * 1024);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        float pe = p[e], me = m[e], ve = v[e];
-        adam_one(a, coef, g[e], pe, me, ve);
-        p[e] = pe;
-        m[e] = me;
-        v[e] = ve;
-      }
-      store_some(t.p, i, n, p);
-      if (t.w != nullptr) store_some(t.w, i, n, p);
-      if constexpr (EIGHT) {
-        const int64_t b = i / kBlock;
-        float mm = 0.0f, rm = 0.0f;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          v[e] = sqrtf(v[e]);
-          mm = fmaxf(mm, fabsf(m[e]));
-          rm = fmaxf(rm, v[e]);
-        }
-        const float ms = scale_of(wave_max(mm)), rs = scale_of(wave_max(rm)), mi = 1.0f / ms, ri = 1.0f / rs;
-        const uint32_t key = block_key(t.first_block + (uint32_t)b, s.key_lo, s.key_hi);
-        uint32_t mc = 0, rc = 0;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const uint32_t h = element_bits(key, (threadIdx.x & 63) * 4 + e);
-          mc |= encode<0>(m[e], mi, h & 0xFFFFu) << (8 * e);
-          rc |= encode<1>(v[e], ri, h >> 16) << (8 * e);
-        }
-        store_codes(static_cast<uint8_t *>(t.m), i, n, mc);
-        store_codes(static_cast<uint8_t *>(t.v), i, n, rc);
-        if ((threadIdx.x & 63) == 0) {
-          t.m_scale[b] = ms;
-          t.v_scale[b] = rs;
-        }
-      } else {
-        store_some(static_cast<float *>(t.m), i, n, m);
-        store_some(static_cast<float *>(t.v), i, n, v);
+      for (int u = 0; u < kTurns; ++u) turn[u].step(s, t, coef, first + u * 1024);
+    } else {
+#pragma unroll 1
+      for (int u = 0; u < kTurns; ++u) {
+        const int64_t i = first + u * 1024;
+        if (i - (threadIdx.x & 63) * 4 >= t.count) break;   // (the whole wave)
+        Turn<EIGHT, G, false> turn;
+        turn.load(t, i);
+        turn.step(s, t, coef, i);
       }
     }
   }
 }
 
 // Squares of a chunk's elements, this thread's share
-template <typename G>
-__device__ __forceinline__ double chunk_squares(const NormArgs &s, uint32_t c, int threads) {
+template <typename G, int THREADS>
+__device__ __forceinline__ double chunk_squares(const NormArgs &s, uint32_t c) {
   const NormTensor &t = s.of[tensor_of(s, c)];
-  const int64_t lo = (int64_t)(c - t.first_chunk) * kChunk;
-  double sum = 0.0;
-  for (int64_t i = lo + threadIdx.x * 4; i < lo + kChunk; i += threads * 4) {
-    const f32x4 g = load_some(static_cast<const G *>(t.g), i, t.count);
+  const int64_t base = (int64_t)(c - t.first_chunk) * kChunk, first = base + threadIdx.x * 4;
+  constexpr int TURNS = kChunk / (4 * THREADS);
+  f32x4 g[TURNS];
+  if (base + kChunk <= t.count) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) sum += (double)g[e] * g[e];
+    for (int u = 0; u < TURNS; ++u) g[u] = load_some<true>(static_cast<const G *>(t.g), first + u * 4 * THREADS, t.count);
+  } else {
+#pragma unroll
+    for (int u = 0; u < TURNS; ++u) g[u] = load_some<false>(static_cast<const G *>(t.g), first + u * 4 * THREADS, t.count);
   }
+  double sum = 0.0;
+#pragma unroll
+  for (int u = 0; u < TURNS; ++u)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum += (double)g[u][e] * g[u][e];
   return sum;
 }
 // partial[block] = the squares of chunks block, block + grid, ..., added to what launches before left in the first `have`
 template <typename G>
 __global__ __launch_bounds__(256) void norm_many_kernel(NormArgs s, double *__restrict__ partial, int have) {
   double sum = 0.0;
-  for (uint32_t c = blockIdx.x; c < s.chunks; c += gridDim.x) sum += chunk_squares<G>(s, c, 256);
+  for (uint32_t c = blockIdx.x; c < s.chunks; c += gridDim.x) sum += chunk_squares<G, 256>(s, c);
   sum = workgroup_sum<256>(sum);
   if (threadIdx.x == 0) partial[blockIdx.x] = (int)blockIdx.x < have ? partial[blockIdx.x] + sum : sum;
 }
@@ -246,7 +310,7 @@ __global__ __launch_bounds__(256) void norm_many_sum(int blocks, const double *_
 template <typename G>
 __global__ __launch_bounds__(1024) void norm_many_once(NormArgs s, float *__restrict__ out, int accumulate) {
   double sum = 0.0;
-  for (uint32_t c = 0; c < s.chunks; ++c) sum += chunk_squares<G>(s, c, 1024);
+  for (uint32_t c = 0; c < s.chunks; ++c) sum += chunk_squares<G, 1024>(s, c);
   sum = workgroup_sum<1024>(sum);
   if (threadIdx.x == 0) out[0] = (float)(accumulate ? (double)out[0] + sum : sum);
 }
