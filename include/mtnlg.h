@@ -480,7 +480,7 @@ int mtnlg_grad_sqnorm(int64_t count, const float *grad, void *workspace, float *
 int mtnlg_adam_step(const mtnlg_adam_desc *desc, int64_t count, float *master, float *m, float *v,
                     const float *grad, void *weight_bf16, const float *sqnorm, void *stream);
 
-/* --- the same over many tensors at once: one launch for up to 46 of them, gradients in float or bf16, the moments in float or in 8 bits -------- */
+/* --- the same over many tensors at once: one launch for up to 55 of them, gradients in float or bf16, the moments in float or in 8 bits -------- */
 typedef struct {
   int64_t count;               /* elements, <= 2^39                                                           */
   float *master;               /* fp32 weight, updated                                                        */
@@ -498,7 +498,7 @@ typedef struct {
   uint64_t seed;               /* 8 bits: with adam.step, of the random numbers that codes are rounded by     */
 } mtnlg_adam_many_desc;
 
-/* mtnlg_grad_sqnorm over the gradients of all tensors (of `tensors` entries the fields count and grad): one launch up to 16 * 4096
+/* mtnlg_grad_sqnorm over the gradients of all tensors (of `tensors` entries the fields count and grad): one launch up to 32 chunks of 4096
  * elements, else one per 160 tensors and one more.  Elements are added in a fixed order, in 64 bits.  grad 16-byte aligned (bf16: 8). */
 size_t mtnlg_grad_sqnorm_many_workspace(void);
 int mtnlg_grad_sqnorm_many(int32_t tensors, const mtnlg_adam_tensor *of, int grad_dtype, void *workspace, size_t workspace_bytes, float *sqnorm,
