@@ -480,7 +480,7 @@ int mtnlg_grad_sqnorm(int64_t count, const float *grad, void *workspace, float *
 int mtnlg_adam_step(const mtnlg_adam_desc *desc, int64_t count, float *master, float *m, float *v,
                     const float *grad, void *weight_bf16, const float *sqnorm, void *stream);
 
-/* --- the same over many tensors at once: one launch for up to 55 of them, gradients in float or bf16, the moments in float or in 8 bits -------- */
+/* --- the same over many tensors at once: one launch for up to 56 of them, gradients in float or bf16, the moments in float or in 8 bits -------- */
 typedef struct {
   int64_t count;               /* elements, <= 2^39                                                           */
   float *master;               /* fp32 weight, updated                                                        */

@@ -21,7 +21,7 @@ namespace {
 constexpr int kBlock = 256;                // elements that share a scale
 constexpr int kChunk = 4096;               // elements of a workgroup's turn: 4 vectors of 4 a thread
 constexpr int kTurns = kChunk / 1024;
-constexpr int kStepTensors = 55, kNormTensors = 160;   // per launch: what 4 KB of arguments hold
+constexpr int kStepTensors = 56, kNormTensors = 160;   // per launch: what 4 KB of arguments hold
 constexpr int kNormBlocks = 2048;          // partial sums at most
 constexpr uint32_t kOnce = 32;             // chunks up to which one workgroup takes all, two to a wave
 constexpr int32_t kMostTensors = 1 << 16;

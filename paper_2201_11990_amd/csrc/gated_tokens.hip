@@ -52,7 +52,7 @@ __global__ __launch_bounds__(64 * WAVES) void gated_tokens_kernel(TokenArgs a) {
   // slab s into a stage; past the last one zeros, which no memory is read for (the wait below counts every stage's DMAs)
   auto fetch = [&](int s, int stage) {
     const int64_t k0 = (int64_t)(s < slabs ? s : slabs) * SK;
-    sw.fetch(W, a.K, n0, k0, a.K, lds + stage * STAGE, lane);
+    sw.template fetch<true>(W, a.K, n0, k0, a.K, lds + stage * STAGE, lane);
     sx.fetch(a.x, a.K, 0, k0, a.K, lds + stage * STAGE + SW::BYTES, lane);
   };
   f32x4 acc[MB][NB];

@@ -46,13 +46,18 @@ struct Slab {
       }
     }
   }
+  // ONCE: past the caches
   // the slab at k0 into LDS; first: element (first row of the tile, k = 0); what lies past K arrives as zeros
+  template <bool ONCE = false>
   __device__ __forceinline__ void fetch(const E *first, int64_t ld, int64_t row0, int64_t k0, int64_t K, uint32_t lds, int lane) const {
     if constexpr (!ROWC) {
       const dma_rsrc_t rs = dma_rsrc(first + k0, RECORDS);
       const bool inside = k0 + ((lane & 7) ^ (lane >> 3)) * EPU < K;
 #pragma unroll
-      for (int i = 0; i < NI; ++i) dma16(rs, lds + i * 1024, inside ? off[i] : OUTSIDE);
+      for (int i = 0; i < NI; ++i) {
+        if constexpr (ONCE) dma16_once(rs, lds + i * 1024, inside ? off[i] : OUTSIDE);
+        else dma16(rs, lds + i * 1024, inside ? off[i] : OUTSIDE);
+      }
     } else {
       const int64_t left = ((K - k0) * ld - row0) * ES;   // to the end of the matrix
       const dma_rsrc_t rs = dma_rsrc(first + k0 * ld, left < RECORDS ? (uint32_t)left : RECORDS);
