@@ -21,4 +21,9 @@ bool gated_tokens_takes(int64_t T, int64_t N, int64_t K);
 int gated_tokens_fwd(int kind, int64_t T, int64_t h, int64_t F, const void *x, const void *w_fc1, void *z, void *g, hipStream_t stream);
 int gated_tokens_out(int64_t T, int64_t h, int64_t F, const void *g, const void *w_fc2, void *y, hipStream_t stream);
 
+// C = A B^T (NT) or A B (NN), bf16, on 128 x 128 tiles that are split along K where they leave compute units idle
+size_t gated_split_workspace(int64_t M, int64_t N, int64_t K);
+double gated_split_time(int64_t M, int64_t N, int64_t K, size_t ws_bytes);
+int gated_split(int layout, int64_t M, int64_t N, int64_t K, const void *A, const void *B, void *C, void *ws, size_t ws_bytes, hipStream_t stream);
+
 }  // namespace mtnlg

@@ -32,8 +32,22 @@ int sizes_of(const mtnlg_gated_desc *d, Sizes *s) {
   need(MTNLG_GEMM_NN, s->T, s->h, 2 * s->F);
   need(MTNLG_GEMM_TN, 2 * s->F, s->h, s->T);
   need(MTNLG_GEMM_TN, s->h, s->F, s->T);
+  if (s->dtype == MTNLG_BF16) s->gemm_ws = std::max({s->gemm_ws, gated_split_workspace(s->T, s->h, s->F), gated_split_workspace(s->T, s->h, 2 * s->F)});
   s->gemm_ws = align_up(s->gemm_ws, 256);
   return MTNLG_OK;
+}
+
+// C = A B^T (NT) or A B (NN) without the activation: mtnlg_gemm, or tiles cut along K where that is estimated to be faster
+int plain_product(const Sizes &s, int layout, int64_t M, int64_t N, int64_t K, const void *A, const void *B, void *C, void *ws, hipStream_t st) {
+  if (s.dtype == MTNLG_BF16) {
+    const double split = gated_split_time(M, N, K, ws ? s.gemm_ws : 0);
+    // (rows that do not begin at whole lines cost the 32 and 64 tiles a third more than their estimate)
+    if (split < gemm_time(s.dtype, layout, M, N, K, s.gemm_ws) && !gemm_wave_pick(s.dtype, layout, M, N, K, split / (K % 64 ? 1.35 : 1.0))) {
+      const int status = gated_split(layout, M, N, K, A, B, C, ws, s.gemm_ws, st);
+      if (status != MTNLG_UNSUPPORTED_SHAPE) return status;
+    }
+  }
+  return mtnlg_gemm(s.dtype, layout, M, N, K, A, B, C, nullptr, nullptr, 0, ws, s.gemm_ws, st);
 }
 
 struct Bytes {
@@ -96,7 +110,7 @@ int mtnlg_gated_ffn_fwd(const mtnlg_gated_desc *desc, const void *x, const void 
   hipStream_t st = (hipStream_t)stream;
   MTNLG_TRY(gated_product(s, GATE_FWD, x, w_fc1, z, g, workspace, st));
   if (s.dtype == MTNLG_BF16 && gated_tokens_takes(s.T, s.h, s.F)) return gated_tokens_out(s.T, s.h, s.F, g, w_fc2, y, st);
-  return mtnlg_gemm(s.dtype, MTNLG_GEMM_NT, s.T, s.h, s.F, g, w_fc2, y, nullptr, nullptr, 0, workspace, s.gemm_ws, stream);
+  return plain_product(s, MTNLG_GEMM_NT, s.T, s.h, s.F, g, w_fc2, y, workspace, st);
 }
 
 int mtnlg_gated_ffn_bwd(const mtnlg_gated_desc *desc, const void *x, const void *w_fc1, const void *w_fc2, const void *z, const void *g,
@@ -132,7 +146,7 @@ int mtnlg_gated_ffn_bwd(const mtnlg_gated_desc *desc, const void *x, const void 
   if (dx && dw_fc1)
     if (const int tile = gemm_wave_group_tile(s.dtype, to_dx, to_dw1, 0, 0, 0, time(MTNLG_GEMM_NN, to_dx), time(MTNLG_GEMM_TN, to_dw1)))
       return gemm_wave_group(s.dtype, to_dx, to_dw1, ColumnSums{}, tile, st);
-  if (dx) MTNLG_TRY(gemm(MTNLG_GEMM_NN, to_dx));
+  if (dx) MTNLG_TRY(plain_product(s, MTNLG_GEMM_NN, s.T, s.h, 2 * s.F, dz, w_fc1, dx, workspace, st));
   if (dw_fc1) MTNLG_TRY(gemm(MTNLG_GEMM_TN, to_dw1));
   return MTNLG_OK;
 }

@@ -881,8 +881,8 @@ bool tile_reaches(bool at, bool bt, int64_t M, int64_t N, int64_t K, int bm, int
   return reach(at, M, bm) <= (int64_t)RAG_RECORDS && reach(bt, N, bn) <= (int64_t)RAG_RECORDS;
 }
 
-// Streaming kernel.  Without RAG: M a multiple of BM, N of BN, K of 64.  Only 256 x 256 tiles split a last round along K.
-template <int BM, int BN, int WGM, int WGN, int DEEP, bool AT, bool BT, bool RAG, int EPI = EPI_FLAGS>
+// Streaming kernel.  Without RAG: M a multiple of BM, N of BN, K of 64.  SPLIT: a last round that leaves compute units idle is split along K.
+template <int BM, int BN, int WGM, int WGN, int DEEP, bool AT, bool BT, bool RAG, int EPI = EPI_FLAGS, bool SPLIT = BM == 256 && BN == 256>
 int launch_stream(const GemmArgs &in, void *ws, size_t ws_bytes, hipStream_t st) {
   GemmArgs g = in;
   if (!RAG && (g.M % BM || g.N % BN || g.K % BK)) return MTNLG_UNSUPPORTED_SHAPE;
@@ -891,7 +891,7 @@ int launch_stream(const GemmArgs &in, void *ws, size_t ws_bytes, hipStream_t st)
   if (EPI == EPI_GATE_FWD && (g.N / 2 + BN / 2) * g.K * 2 > (int64_t)RAG_RECORDS) return MTNLG_UNSUPPORTED_SHAPE;
   unsigned grid;
   SplitPlan plan;
-  MTNLG_TRY((plan_launch<BM, BN>(g, ws, ws_bytes, BM == 256 && BN == 256, &grid, &plan)));
+  MTNLG_TRY((plan_launch<BM, BN>(g, ws, ws_bytes, SPLIT, &grid, &plan)));
   constexpr int smem = DEEP ? DEEP * (BM + BN) * BK * 2 : (2 * BM + stream_ring_b(BN) * BN) * BK * 2;
   static unsigned long long attr_done = 0;
   int device;

@@ -16,7 +16,7 @@ F = 2.0 ** -23
 GATES = {"silu": M.GATE_SILU, "gelu_tanh": M.GATE_GELU_TANH, "gelu_erf": M.GATE_GELU_ERF}
 # tokens, hidden, ffn: one token to many, widths that no tile divides, whole tiles of every kernel, and rows on either side of where the kernels change
 SIZES = [(1, 8, 8), (1, 2048, 1024), (2, 64, 40), (5, 1032, 520), (16, 512, 1368), (17, 520, 344), (24, 2560, 1024), (32, 776, 264), (33, 1024, 2048), (61, 520, 344),
-         (64, 2048, 776), (65, 264, 128), (130, 264, 136), (128, 4096, 256), (256, 512, 1024), (300, 2048, 1000), (257, 1024, 776), (512, 640, 1280),
+         (64, 2048, 776), (65, 264, 128), (130, 264, 136), (128, 4096, 256), (256, 512, 1024), (300, 2048, 1000), (130, 1032, 5464), (777, 2048, 5464), (200, 4096, 4104), (257, 1024, 776), (512, 640, 1280),
          (1024, 2048, 2048), (2048, 1280, 2560)]
 
 
