@@ -706,7 +706,8 @@ __global__ __launch_bounds__(64 * WGM * WGN, WGM * WGN == 8 ? 1 : 2) void gemm_s
         }
       }
     };
-    // The gate's backward reads two values a position, one pass ahead.
+    // The gate's backward reads two values a position, one pass ahead and past the caches, which keep more of dz for the products that follow (8192 tokens, h 2048,
+    // F 8192: this product and dw_fc2 510 -> 491 us).
     constexpr bool BWD = EPI == EPI_GATE_BWD;
     bf16x8 zg[BWD ? NP : 1][NRD], zu[BWD ? NP : 1][NRD];
     auto preload_z = [&](auto P) {
@@ -718,8 +719,8 @@ __global__ __launch_bounds__(64 * WGM * WGN, WGM * WGN == 8 ? 1 : 2) void gemm_s
           const int q = t * 64 + elane, row = q / SEG, cv = q % SEG;
           const int64_t m = m0 + ewm * WM + p * RP + row, n = n0 + ewn * WN + cv * 8;
           const int64_t off = RAG && (m >= g.M || n >= g.N) ? 0 : m * g.ldc + n;
-          zg[p][t] = *reinterpret_cast<const bf16x8 *>(z + off);
-          zu[p][t] = *reinterpret_cast<const bf16x8 *>(z + off + g.N);
+          zg[p][t] = __builtin_bit_cast(bf16x8, __builtin_nontemporal_load(reinterpret_cast<const f32x4 *>(z + off)));
+          zu[p][t] = __builtin_bit_cast(bf16x8, __builtin_nontemporal_load(reinterpret_cast<const f32x4 *>(z + off + g.N)));
         }
       }
     };
