@@ -504,13 +504,14 @@ size_t mtnlg_grad_sqnorm_many_workspace(void);
 int mtnlg_grad_sqnorm_many(int32_t tensors, const mtnlg_adam_tensor *of, int grad_dtype, void *workspace, size_t workspace_bytes, float *sqnorm,
                            int accumulate, void *stream);
 /* mtnlg_adam_step on every tensor.  sqnorm given and not finite: nothing is changed (the step is left out), decided on the device.
- * state_bits 8: m is held as e4m3 codes (bias 7, 448 the largest) times a float scale per 256 consecutive elements, sqrt(v) likewise in v
- * and v_scale (a step squares it, and takes the root of the new v before it rounds).  scale = the block's largest magnitude / 448 (1 where all
- * are zeros, else 2^-126 at least).  A quotient by the scale becomes the code below or above it: with steps of 2^(e - 3), e the
- * quotient's exponent or -6 where that is more, floor(quotient / step + u) steps, u in (0, 1) a random number (16 bits and a half) of seed,
- * adam.step, the block's number among all tensors' blocks and the element's in its block: the same call gives the same codes.  A root that is not zero is one step at
- * least, so that no update divides by a lost one.  The update itself uses the new moments before they are rounded.  NaN gives the code of NaN; squares of gradients have to be
- * finite.  Codes of zero with any scale are zero: a program begins with codes 0.
+ * state_bits 8: m is held as e4m3 codes (bias 7, 448 the largest) times a float scale per 256 consecutive elements, r = sqrt(v) likewise in v and v_scale.
+ * A step decodes (code * scale), updates (m = m beta1 + g' (1 - beta1), r = sqrt(r r beta2 + g' (1 - beta2) g'), every operation rounded to float; the
+ * weight's update uses these moments as they are), and encodes: scale = the block's largest magnitude * float(1/448) (1 where all are zeros, else 2^-126
+ * at least); y = magnitude * (1 / scale), 448 at most; with steps of 2^(e - 3), e the exponent of y or -6 where that is more, the code is of floor(y / step + u)
+ * steps, u in (0, 1) a random number of 16 bits (and a half) that follows from seed, adam.step, the block's number among all tensors' blocks and the element's
+ * in its block.  So rounding has no bias, which moments need that change by less than a code in a step, and the same call gives the same codes.  A root that is not zero is one step at
+ * least, so that no update divides by a lost one.  NaN gives the code of NaN; squares of gradients have to be finite.  Codes of zero are zero with any
+ * finite scale: a program begins with codes and scales of 0.
  * Alignment: master 16 bytes, m and v 16 (codes: 4), grad 16 (bf16: 8), weight_bf16 8.  What is written lies on nothing else of the call (the same tensor twice is
  * MTNLG_INVALID_ARG). */
 int mtnlg_adam_step_many(const mtnlg_adam_many_desc *desc, const mtnlg_adam_tensor *of, const float *sqnorm, void *stream);

@@ -785,6 +785,9 @@ def mtnlg_adam_step(master, m, v, grad, weight_bf16=None, sqnorm=None, *, lr, st
                                  _p(sqnorm), _stream()), "mtnlg_adam_step")
 
 
+_ADAM_TENSOR = struct.Struct("q7Qi4x")   # an AdamTensor
+
+
 class AdamTensors:
     """Marshalled table of the tensors of mtnlg_grad_sqnorm_many and mtnlg_adam_step_many, built once and reused per step.
 
@@ -794,29 +797,32 @@ class AdamTensors:
     def __init__(self, tensors):
         if not tensors:
             raise ValueError("no tensors")
-        first = tensors[0]
-        self.grad_dtype, self.device = _dtype_code(first["grad"]), first["grad"].get_device()
-        eight = first.get("m") is not None and first["m"].dtype == torch.float8_e4m3fn
-        self.state_bits = 8 if eight else 32
-        self.steps = all(t.get(k) is not None for t in tensors for k in ("master", "m", "v"))
-        self.table = (AdamTensor * len(tensors))()
-        for row, t in zip(self.table, tensors):
+        first = tensors[0]["grad"]
+        kind, device = first.dtype, first.get_device()
+        m = tensors[0].get("m")
+        eight = m is not None and m.dtype == torch.float8_e4m3fn
+        state = torch.float8_e4m3fn if eight else torch.float32
+        self.grad_dtype, self.device, self.state_bits = _dtype_code(first), device, 8 if eight else 32
+        self.steps = all(t.get("master") is not None and t.get("m") is not None and t.get("v") is not None for t in tensors)
+
+        def at(t, name, dtype, count):
+            x = t[name]
+            if x.dtype != dtype or x.numel() != count or x.get_device() != device or device < 0:
+                raise ValueError(f"{name}: expected {count} elements of {dtype} on device {device}, got {x.numel()} of {x.dtype} on {x.device}")
+            return _dense(x)
+
+        rows = bytearray(_ADAM_TENSOR.size * len(tensors))
+        for i, t in enumerate(tensors):
             n = t["grad"].numel()
-            kinds = {"grad": first["grad"].dtype}
+            grad, master, m, v, m_scale, v_scale, weight = at(t, "grad", kind, n), 0, 0, 0, 0, 0, 0
             if self.steps:
-                state = torch.float8_e4m3fn if eight else torch.float32
-                kinds.update(master=torch.float32, m=state, v=state)
+                master, m, v = at(t, "master", torch.float32, n), at(t, "m", state, n), at(t, "v", state, n)
                 if eight:
-                    kinds.update(m_scale=torch.float32, v_scale=torch.float32)
+                    m_scale, v_scale = at(t, "m_scale", torch.float32, -(-n // 256)), at(t, "v_scale", torch.float32, -(-n // 256))
                 if t.get("weight_bf16") is not None:
-                    kinds["weight_bf16"] = torch.bfloat16
-            row.count, row.decay = n, int(bool(t.get("decay", True)))
-            for name, dtype in kinds.items():
-                x = t[name]
-                count = -(-n // 256) if name.endswith("_scale") else n
-                if x.dtype != dtype or x.numel() != count or not x.is_cuda or x.get_device() != self.device:
-                    raise ValueError(f"{name}: expected {count} elements of {dtype} on device {self.device}, got {x.numel()} of {x.dtype} on {x.device}")
-                setattr(row, name, _dense(x))
+                    weight = at(t, "weight_bf16", torch.bfloat16, n)
+            _ADAM_TENSOR.pack_into(rows, i * _ADAM_TENSOR.size, n, master, m, v, m_scale, v_scale, grad, weight, bool(t.get("decay", True)))
+        self.table = (AdamTensor * len(tensors)).from_buffer(rows)
         self._keep = [dict(t) for t in tensors]
 
     def __len__(self):

@@ -162,10 +162,8 @@ __device__ __forceinline__ float wave_most(float x) {
   step(std::integral_constant<int, 0x143>{});
   return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
 }
-// scale of a block with this largest magnitude, and what its values are multiplied with: less than the reciprocal by 2^-22, more than roundings can make
-// up for, so that no quotient passes 448
+// scale of a block with this largest magnitude
 __device__ __forceinline__ float scale_of(float most) { return most > 0.0f ? fmaxf(most * (1.0f / 448.0f), 0x1p-126f) : 1.0f; }
-__device__ __forceinline__ float inverse_of(float scale) { return __builtin_amdgcn_rcpf(scale) * (1.0f - 0x1p-22f); }
 
 // The four elements of a thread at i
 template <bool EIGHT, typename G, bool WHOLE>
@@ -192,27 +190,28 @@ struct Turn {
   __device__ __forceinline__ void step(const StepArgs &s, const StepTensor &t, int64_t n, float wd, float coef, int64_t i) {
     if (!any(i, n)) return;
     if constexpr (EIGHT) {
-      // adam_one with the root of v taken once, for the update and for the state, by the hardware's root and reciprocal (1 ulp each)
+      // What leads to codes and scales rounds operation by operation, so that a state follows from its inputs alone, whatever is contracted or
+      // approximated elsewhere; the update takes the same root and the hardware's reciprocal (1 ulp).
+#pragma clang fp contract(off)
       const AdamArgs &a = s.a;
-      const float root_c2 = sqrtf(a.inv_c2), m_old = ms * a.beta1, r_old = vs * sqrtf(a.beta2);
+      const float root_c2 = sqrtf(a.inv_c2), new_m = 1.0f - a.beta1, new_v = 1.0f - a.beta2;
       f32x4 r = decode(vc);
       m = decode(mc);
       float mm = 0.0f, rm = 0.0f;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float ge = g[e] * coef;
-        m[e] = m[e] * m_old + (1.0f - a.beta1) * ge;
-        r[e] *= r_old;
-        r[e] = __builtin_amdgcn_sqrtf(r[e] * r[e] + (1.0f - a.beta2) * ge * ge);
-        const float update = m[e] * a.inv_c1 * __builtin_amdgcn_rcpf(r[e] * root_c2 + a.eps);
-        p[e] = p[e] - a.lr * (update + wd * p[e]);
+        const float ge = g[e] * coef, old = r[e] * vs;
+        m[e] = (m[e] * ms) * a.beta1 + ge * new_m;
+        r[e] = sqrtf((old * old) * a.beta2 + (ge * new_v) * ge);
+        const float update = m[e] * a.inv_c1 * __builtin_amdgcn_rcpf(__builtin_fmaf(r[e], root_c2, a.eps));
+        p[e] = __builtin_fmaf(-a.lr, __builtin_fmaf(wd, p[e], update), p[e]);
         mm = fmaxf(mm, fabsf(m[e]));
         rm = fmaxf(rm, r[e]);
       }
       const int64_t b = i / kBlock;
       ms = scale_of(wave_most(mm));
       vs = scale_of(wave_most(rm));
-      const float mi = inverse_of(ms), ri = inverse_of(vs);
+      const float mi = 1.0f / ms, ri = 1.0f / vs;
       const uint32_t key = block_key(__builtin_amdgcn_readfirstlane(t.first_block + (uint32_t)b), s.key_lo, s.key_hi);
       float ym[4], yr[4];
       uint32_t um[4], ur[4];
@@ -221,10 +220,11 @@ struct Turn {
         const uint32_t h = element_bits(key, (threadIdx.x & 63) * 4 + e);
         um[e] = (h << 16) | 0x8000u;
         ur[e] = (h & 0xFFFF0000u) | 0x8000u;
-        ym[e] = m[e] * mi;
+        const float y = m[e] * mi;   // (comparisons that let NaN through)
+        ym[e] = y > 448.0f ? 448.0f : y < -448.0f ? -448.0f : y;
         // one step at least of a root that is not zero: what lies below it has the code of it, however it is rounded
-        const float y = r[e] * ri, least = r[e] > 0.0f ? 0x1p-9f : 0.0f;
-        yr[e] = y < least ? least : y;
+        const float q = r[e] * ri, least = r[e] > 0.0f ? 0x1p-9f : 0.0f;
+        yr[e] = q < least ? least : q > 448.0f ? 448.0f : q;
       }
       mc = encode(ym, um);
       vc = encode(yr, ur);

@@ -171,6 +171,38 @@ def test_three_steps(bits, grads, which):
         check(before, rows, bits, float(sq), step, seed=step * 77, clip=clip)
 
 
+@pytest.mark.parametrize("grads", ["fp32", "bf16"])
+@pytest.mark.parametrize("clip", [0.0, 1e-2])
+def test_codes_and_scales_bit_by_bit(grads, clip):
+    # every operation rounds once to fp32, here as there
+    rows = with_states(model(COUNTS["small"] + [50_001, 4096 * 3], grads, 3), 8, 4)
+    before = [{k: (v.cpu() if isinstance(v, torch.Tensor) else v) for k, v in t.items()} for t in rows]
+    sq, _ = run_norm(rows)
+    M.mtnlg_adam_step_many(rows, sq, lr=1e-3, step=12, max_grad_norm=clip, seed=987654321987654321)
+    f = torch.tensor([0.9, 0.95, 1e-6, clip], dtype=torch.float32)
+    b1, b2, one = f[0], f[1], torch.ones((), dtype=torch.float32)
+    root = lambda x: x.double().sqrt().float()   # noqa: E731  (of 53 bits to 24: the same as rounding once)
+    coef = torch.minimum(one, f[3] / (root(sq.cpu()) + f[2])) if clip > 0 else one
+    block = 0
+    for old, new in zip(before, rows):
+        n = old["master"].numel()
+        wide = lambda s: s.repeat_interleave(BLOCK)[:n]   # noqa: E731
+        g = old["grad"].float() * coef
+        m = (old["m"].float() * wide(old["m_scale"])) * b1 + g * (one - b1)
+        r = old["v"].float() * wide(old["v_scale"])
+        r = root((r * r) * b2 + (g * (one - b2)) * g)
+        for k, x, u, least in zip("mv", (m, r), numbers(987654321987654321, 12, block, n), (0, 1)):
+            most = torch.nn.functional.pad(x.abs(), (0, -n % BLOCK)).view(-1, BLOCK).amax(1)
+            scale = torch.where(most > 0, (most * (one / 448)).clamp(min=2.0 ** -126), one)
+            assert torch.equal(new[k + "_scale"].cpu(), scale), k
+            y = (x.abs() * wide(one / scale)).clamp(max=448).double()
+            step = torch.exp2((torch.frexp(y).exponent - 1).clamp(min=-6).double() - 3)
+            steps = torch.floor(y / step + u.cpu())
+            codes = torch.copysign(torch.where(x != 0, steps.clamp(min=least), 0.0) * step, x.double()).float().to(E4M3)
+            assert torch.equal(new[k].cpu().view(torch.uint8), codes.view(torch.uint8)), k
+        block += -(-n // BLOCK)
+
+
 @pytest.mark.parametrize("bits", [32, 8])
 def test_first_step_from_nothing_and_without_a_norm(bits):
     rows = with_states(model(COUNTS["small"], "fp32"), bits, zero=True)
