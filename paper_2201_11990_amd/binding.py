@@ -178,7 +178,7 @@ def lib():
             "mtnlg_gated_ffn_bwd": (ctypes.c_int, [ctypes.POINTER(GatedDesc), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]),
             "mtnlg_grad_sqnorm_many_workspace": (sz, []),
             "mtnlg_grad_sqnorm_many": (ctypes.c_int, [i32, vp, ctypes.c_int, vp, sz, vp, ctypes.c_int, vp]),
-            "mtnlg_adam_step_many": (ctypes.c_int, [ctypes.POINTER(AdamManyDesc), vp, vp, vp]),
+            "mtnlg_adam_step_many": (ctypes.c_int, [vp, vp, vp, vp]),
             "mtnlg_calibrate_mfma_operand_bytes": (sz, [ctypes.c_int]),
             "mtnlg_calibrate_mfma_flops": (i64, [ctypes.c_int, ctypes.c_int]),
             "mtnlg_calibrate_mfma": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, vp, vp, vp]),
@@ -785,7 +785,7 @@ def mtnlg_adam_step(master, m, v, grad, weight_bf16=None, sqnorm=None, *, lr, st
                                  _p(sqnorm), _stream()), "mtnlg_adam_step")
 
 
-_ADAM_TENSOR = struct.Struct("q7Qi4x")   # an AdamTensor
+_ADAM_TENSOR, _ADAM_MANY = struct.Struct("q7Qi4x"), struct.Struct("6f4iQ")   # an AdamTensor, an AdamManyDesc
 
 
 class AdamTensors:
@@ -857,8 +857,8 @@ def mtnlg_adam_step_many(tensors, sqnorm=None, *, lr, step, beta1=0.9, beta2=0.9
     stream = _device_stream(sqnorm)
     if sqnorm is not None:
         _like(sqnorm, torch.float32, (1,), "sqnorm")
-    d = AdamManyDesc(AdamDesc(lr, beta1, beta2, eps, weight_decay, max_grad_norm, step), len(t), t.grad_dtype, t.state_bits, seed)
-    _check(lib().mtnlg_adam_step_many(ctypes.byref(d), t.table, _dense(sqnorm), stream), "mtnlg_adam_step_many")
+    s = _Structs(_ADAM_MANY, lr, beta1, beta2, eps, weight_decay, max_grad_norm, step, len(t), t.grad_dtype, t.state_bits, seed)
+    _check(lib().mtnlg_adam_step_many(s.at, t.table, _dense(sqnorm), stream), "mtnlg_adam_step_many")
 
 
 def mtnlg_calibrate_mfma_operand_bytes(workgroups):

@@ -277,47 +277,54 @@ __global__ __launch_bounds__(256) void adam_many_kernel(StepArgs s) {
   }
 }
 
-// Squares of a chunk's elements, this thread's share; THREADS take the chunk, 16 bytes a load
+// A chunk's elements, this thread's share of THREADS, 16 bytes a load (of bf16 whose alignment is 8: a load of four dwords needs no more than a dword's)
 template <typename G, int THREADS>
-__device__ __forceinline__ double chunk_squares(const NormArgs &s, uint32_t c) {
-  const NormTensor &t = s.of[tensor_of<kNormTensors>(s, c)];
-  const G *p = static_cast<const G *>(t.g);
-  const int64_t n = t.count, base = (int64_t)(c - t.first_chunk) * kChunk;
-  constexpr int W = 16 / sizeof(G), TURNS = kChunk / (W * THREADS);
-  const int64_t first = base + threadIdx.x % THREADS * W;
+struct Squares {
+  static constexpr int W = 16 / sizeof(G), TURNS = kChunk / (W * THREADS);
   f32x4 g[TURNS][W / 4];
-  if (base + kChunk <= n) {
+  __device__ __forceinline__ void load(const NormArgs &s, uint32_t c) {
+    const NormTensor &t = s.of[tensor_of<kNormTensors>(s, c)];
+    const G *p = static_cast<const G *>(t.g);
+    const int64_t n = t.count, base = (int64_t)(c - t.first_chunk) * kChunk, first = base + threadIdx.x % THREADS * W;
+    if (base + kChunk <= n) {
 #pragma unroll
-    for (int u = 0; u < TURNS; ++u) {
-      const int64_t i = first + u * W * THREADS;
-      if constexpr (sizeof(G) == 4) {
-        g[u][0] = stream4(p + i);
-      } else {
-        const bf16x8 x = __builtin_bit_cast(bf16x8, __builtin_nontemporal_load(reinterpret_cast<const f32x4 *>(p + i)));
+      for (int u = 0; u < TURNS; ++u) {
+        const int64_t i = first + u * W * THREADS;
+        if constexpr (sizeof(G) == 4) {
+          g[u][0] = stream4(p + i);
+        } else {
+          const bf16x8 x = __builtin_bit_cast(bf16x8, __builtin_nontemporal_load(reinterpret_cast<const f32x4 *>(p + i)));
 #pragma unroll
-        for (int e = 0; e < 8; ++e) g[u][e / 4][e % 4] = (float)x[e];
+          for (int e = 0; e < 8; ++e) g[u][e / 4][e % 4] = (float)x[e];
+        }
       }
+    } else {
+#pragma unroll
+      for (int u = 0; u < TURNS; ++u)
+#pragma unroll
+        for (int o = 0; o < W / 4; ++o) g[u][o] = load_some<false>(p, first + u * W * THREADS + 4 * o, n);
     }
-  } else {
+  }
+  __device__ __forceinline__ double sum() const {
+    double s = 0.0;
 #pragma unroll
     for (int u = 0; u < TURNS; ++u)
 #pragma unroll
-      for (int o = 0; o < W / 4; ++o) g[u][o] = load_some<false>(p, first + u * W * THREADS + 4 * o, n);
+      for (int o = 0; o < W / 4; ++o)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s += (double)g[u][o][e] * g[u][o][e];
+    return s;
   }
-  double sum = 0.0;
-#pragma unroll
-  for (int u = 0; u < TURNS; ++u)
-#pragma unroll
-    for (int o = 0; o < W / 4; ++o)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) sum += (double)g[u][o][e] * g[u][o][e];
-  return sum;
-}
+};
 // partial[block] = the squares of chunks block, block + grid, ..., added to what launches before left in the first `have`
 template <typename G>
 __global__ __launch_bounds__(256) void norm_many_kernel(NormArgs s, double *__restrict__ partial, int have) {
   double sum = 0.0;
-  for (uint32_t c = blockIdx.x; c < s.chunks; c += gridDim.x) sum += chunk_squares<G, 256>(s, c);
+  for (uint32_t c = blockIdx.x; c < s.chunks; c += gridDim.x) {
+    Squares<G, 256> q;
+    q.load(s, c);
+    sum += q.sum();
+  }
   sum = workgroup_sum<256>(sum);
   if (threadIdx.x == 0) partial[blockIdx.x] = (int)blockIdx.x < have ? partial[blockIdx.x] + sum : sum;
 }
@@ -335,7 +342,11 @@ __global__ __launch_bounds__(256) void norm_many_sum(int blocks, const double *_
 template <typename G>
 __global__ __launch_bounds__(1024) void norm_many_once(NormArgs s, float *__restrict__ out, int accumulate) {
   double sum = 0.0;
-  for (uint32_t c = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); c < s.chunks; c += 16) sum += chunk_squares<G, 64>(s, c);
+  for (uint32_t c = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); c < s.chunks; c += 16) {
+    Squares<G, 64> q;
+    q.load(s, c);
+    sum += q.sum();
+  }
   sum = workgroup_sum<1024>(sum);
   if (threadIdx.x == 0) out[0] = (float)(accumulate ? (double)out[0] + sum : sum);
 }
@@ -345,9 +356,22 @@ struct Span {
   uintptr_t from, to;
   bool written;
 };
-// Whether no byte that is written is of two spans
-bool spans_apart(Span *s, int64_t n) {
-  std::sort(s, s + n, [](const Span &a, const Span &b) { return a.from < b.from; });
+// Whether no byte that is written is of two spans.  Sorted by merging the runs that are there already: tensors of a kind mostly lie in the order in
+// which the call names them (112 tensors, seven spans each: 30 us with std::sort).  other: room for n more.
+bool spans_apart(Span *s, Span *other, int64_t n) {
+  auto run_end = [&](int64_t i) {
+    for (++i; i < n && s[i - 1].from <= s[i].from; ++i) {}
+    return i;
+  };
+  auto before = [](const Span &a, const Span &b) { return a.from < b.from; };
+  while (run_end(0) < n) {
+    for (int64_t i = 0; i < n;) {
+      const int64_t mid = run_end(i), end = mid < n ? run_end(mid) : n;
+      std::merge(s + i, s + mid, s + mid, s + end, other + i, before);
+      i = end;
+    }
+    std::swap(s, other);
+  }
   uintptr_t any = 0, written = 0;   // ends of the spans so far, of the written ones
   for (int64_t i = 0; i < n; ++i) {
     if (s[i].from < (s[i].written ? any : written)) return false;
@@ -444,26 +468,27 @@ int mtnlg_adam_step_many(const mtnlg_adam_many_desc *desc, const mtnlg_adam_tens
   }
   if (blocks > 0xFFFFFFFFull) return MTNLG_UNSUPPORTED_SHAPE;
   {
-    Span *spans = new (std::nothrow) Span[(size_t)desc->tensors * 7 + 1];
+    const size_t most = (size_t)desc->tensors * 7 + 1;
+    Span *spans = new (std::nothrow) Span[2 * most];
     if (!spans) return MTNLG_HIP_ERROR;
     int64_t n = 0;
-    auto add = [&](const void *p, int64_t bytes, bool written) {
-      if (p) spans[n++] = Span{(uintptr_t)p, (uintptr_t)p + (uintptr_t)bytes, written};
+    auto add = [&](auto place, int64_t bytes, bool written, bool scales = false) {   // of every tensor
+      for (int32_t i = 0; i < desc->tensors; ++i)
+        if (const uintptr_t p = (uintptr_t)place(of[i]))
+          spans[n++] = Span{p, p + (uintptr_t)((scales ? blocks_of(of[i].count) : of[i].count) * bytes), written};
     };
-    for (int32_t i = 0; i < desc->tensors; ++i) {
-      const mtnlg_adam_tensor &t = of[i];
-      add(t.master, t.count * 4, true);
-      add(t.m, t.count * (eight ? 1 : 4), true);
-      add(t.v, t.count * (eight ? 1 : 4), true);
-      add(t.weight_bf16, t.count * 2, true);
-      add(t.grad, t.count * (f32 ? 4 : 2), false);
-      if (eight) {
-        add(t.m_scale, blocks_of(t.count) * 4, true);
-        add(t.v_scale, blocks_of(t.count) * 4, true);
-      }
+    using T = const mtnlg_adam_tensor &;
+    add([](T t) { return t.master; }, 4, true);
+    add([](T t) { return t.m; }, eight ? 1 : 4, true);
+    add([](T t) { return t.v; }, eight ? 1 : 4, true);
+    add([](T t) { return t.weight_bf16; }, 2, true);
+    add([](T t) { return t.grad; }, f32 ? 4 : 2, false);
+    if (eight) {
+      add([](T t) { return t.m_scale; }, 4, true, true);
+      add([](T t) { return t.v_scale; }, 4, true, true);
     }
-    add(sqnorm, 4, false);
-    const bool apart = spans_apart(spans, n);
+    if (sqnorm) spans[n++] = Span{(uintptr_t)sqnorm, (uintptr_t)sqnorm + 4, false};
+    const bool apart = spans_apart(spans, spans + most, n);
     delete[] spans;
     if (!apart) return MTNLG_INVALID_ARG;
   }

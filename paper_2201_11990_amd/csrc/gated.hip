@@ -122,7 +122,7 @@ int mtnlg_gated_ffn_bwd(const mtnlg_gated_desc *desc, const void *x, const void 
   if (((uintptr_t)x | (uintptr_t)w_fc1 | (uintptr_t)w_fc2 | (uintptr_t)z | (uintptr_t)g | (uintptr_t)dy | (uintptr_t)dz | (uintptr_t)dx |
        (uintptr_t)dw_fc1 | (uintptr_t)dw_fc2 | (uintptr_t)workspace) & 15)
     return MTNLG_INVALID_ARG;
-  const bool wide = (desc->flags & MTNLG_WGRAD_FP32) != 0;
+  const bool wide = s.dtype == MTNLG_BF16 && (desc->flags & MTNLG_WGRAD_FP32) != 0;
   const size_t th = s.T * s.h * s.es, tf = s.T * s.F * s.es, w = s.h * s.F * s.es, dw = s.h * s.F * (wide ? 4 : s.es);
   const Bytes out[] = {{dz, 2 * tf}, {dx, th}, {dw_fc1, 2 * dw}, {dw_fc2, dw}, {workspace, need}};
   const Bytes in[] = {{x, th}, {w_fc1, 2 * w}, {w_fc2, w}, {z, 2 * tf}, {g, tf}, {dy, th}};

@@ -89,11 +89,10 @@ def codes_of(x, error, u, least):
     return torch.sign(x) * torch.where(x != 0, k.clamp(min=least), 0.0) * step, scale, near
 
 
-def check(before, after, bits, norm, step, seed=0, lr=1e-3, clip=1.0, b1=0.9, b2=0.95, eps=1e-8, wd=0.1):
+def check(before, after, bits, norm, step, seed=0, lr=1e-3, clip=1.0, b1=0.9, b2=0.95, eps=1e-8, wd=0.1, block=0):
     f32 = lambda x: float(torch.tensor(x, dtype=torch.float32))   # noqa: E731
     b1, b2, lr, wd, eps = map(f32, (b1, b2, lr, wd, eps))
     coef = min(1.0, clip / (math.sqrt(norm) + 1e-6)) if norm is not None and clip > 0 else 1.0
-    block = 0
     for old, new in zip(before, after):
         n = old["master"].numel()
         p, g = old["master"].double(), old["grad"].double() * coef
@@ -323,6 +322,37 @@ def test_runs_are_identical_and_replays_too(bits):
         run()
     side.synchronize()
     assert same()
+
+
+@pytest.mark.parametrize("bits,grads", [(32, "fp32"), (8, "bf16")])
+def test_a_tensor_of_more_than_32_bits_of_elements(bits, grads):
+    n = (1 << 31) + 4096 * 3 + 77
+    gdt = torch.bfloat16 if grads == "bf16" else torch.float32
+    g = torch.Generator(device="cuda").manual_seed(5)
+    part = torch.randn(1 << 20, generator=g, device="cuda") * 1e-3
+    whole = lambda x, dt: x.to(dt).repeat(-(-n // x.numel()))[:n].contiguous()   # noqa: E731
+    row = {"master": whole(part * 20, torch.float32), "grad": whole(part, gdt), "weight_bf16": torch.empty(n, dtype=torch.bfloat16, device="cuda")}
+    if bits == 32:
+        row.update(m=whole(part * 0.5, torch.float32), v=whole(part.square(), torch.float32))
+    else:
+        codes = torch.randint(1, 127, (1 << 20,), generator=g, device="cuda", dtype=torch.uint8)
+        row.update(m=whole(codes, torch.uint8).view(E4M3), v=whole(codes.flip(0), torch.uint8).view(E4M3))
+        row.update({k: torch.full((-(-n // BLOCK),), 1e-6, device="cuda") for k in ("m_scale", "v_scale")})
+    other = with_states(model([700], grads, 9), bits)[0]
+    rows = [other, row]
+    want = norm_of([other]) + float(part.to(gdt).double().square().sum()) * (n // part.numel()) + float(part.to(gdt)[:n % part.numel()].double().square().sum())
+    sq, _ = run_norm(rows)
+    assert abs(float(sq) - want) <= 2.0 ** -24 * want * 1.01
+    first = n // BLOCK - 40   # the last blocks, and some in between on either side of 2^31
+    spans = [(first * BLOCK, n), ((1 << 31) - 2048, (1 << 31) + 2048), (0, 5000)]
+    cut = lambda a, b: {k: (v if not isinstance(v, torch.Tensor) else v[a // BLOCK:-(-b // BLOCK)] if k.endswith("scale") else v[a:b]).clone()   # noqa: E731
+                        if isinstance(v, torch.Tensor) else v for k, v in row.items()}
+    before = [cut(a, b) for a, b in spans]
+    M.mtnlg_adam_step_many(rows, sq, lr=1e-3, step=4, max_grad_norm=0.0, seed=6)
+    for old, (a, b) in zip(before, spans):
+        check([old], [cut(a, b)], bits, float(sq), 4, seed=6, clip=0.0, block=3 + a // BLOCK)
+    del rows, row, before
+    torch.cuda.empty_cache()
 
 
 def test_what_lies_beside_the_tensors_is_left_as_it_was():

@@ -153,7 +153,7 @@ def test_gates_far_from_zero(dtype, kind, T):
     check_backward(kind, s)
 
 
-@pytest.mark.parametrize("dtype,wide", [("bf16", False), ("bf16", True), ("fp32", False)])
+@pytest.mark.parametrize("dtype,wide", [("bf16", False), ("bf16", True), ("fp32", False), ("fp32", True)])
 @pytest.mark.parametrize("T,h,ffn", [(7, 72, 40), (130, 264, 136), (512, 512, 1024)])
 def test_weight_gradients_added_up_and_in_fp32(dtype, wide, T, h, ffn):
     s = inputs(T, h, ffn, dtype, 1, wide)
