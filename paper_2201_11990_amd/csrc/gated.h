@@ -4,10 +4,11 @@
 
 namespace mtnlg {
 
-int gated_mfma_fwd(int kind, int64_t T, int64_t h, int64_t F, const void *x, const void *w_fc1, void *z, void *g, void *ws, size_t ws_bytes,
+// split: on tiles cut along K (gated_split_time)
+int gated_mfma_fwd(int kind, int64_t T, int64_t h, int64_t F, const void *x, const void *w_fc1, void *z, void *g, bool split, void *ws, size_t ws_bytes,
                    hipStream_t stream);
-int gated_mfma_bwd(int kind, int64_t T, int64_t h, int64_t F, const void *dy, const void *w_fc2, const void *z, void *dz, void *ws, size_t ws_bytes,
-                   hipStream_t stream);
+int gated_mfma_bwd(int kind, int64_t T, int64_t h, int64_t F, const void *dy, const void *w_fc2, const void *z, void *dz, bool split, void *ws,
+                   size_t ws_bytes, hipStream_t stream);
 
 // mode: GATE_FWD (A x, B w_fc1, C g) or GATE_BWD (A dy, B w_fc2, C dz); tile: 32 or 64
 bool gated_wave_takes(int dtype, int64_t h, int64_t F);

@@ -32,22 +32,11 @@ int sizes_of(const mtnlg_gated_desc *d, Sizes *s) {
   need(MTNLG_GEMM_NN, s->T, s->h, 2 * s->F);
   need(MTNLG_GEMM_TN, 2 * s->F, s->h, s->T);
   need(MTNLG_GEMM_TN, s->h, s->F, s->T);
-  if (s->dtype == MTNLG_BF16) s->gemm_ws = std::max({s->gemm_ws, gated_split_workspace(s->T, s->h, s->F), gated_split_workspace(s->T, s->h, 2 * s->F)});
+  if (s->dtype == MTNLG_BF16)
+    s->gemm_ws = std::max({s->gemm_ws, gated_split_workspace(s->T, s->h, s->F), gated_split_workspace(s->T, s->h, 2 * s->F),
+                           gated_split_workspace(s->T, 2 * s->F, s->h), gated_split_workspace(s->T, s->F, s->h)});
   s->gemm_ws = align_up(s->gemm_ws, 256);
   return MTNLG_OK;
-}
-
-// C = A B^T (NT) or A B (NN) without the activation: mtnlg_gemm, or tiles cut along K where that is estimated to be faster
-int plain_product(const Sizes &s, int layout, int64_t M, int64_t N, int64_t K, const void *A, const void *B, void *C, void *ws, hipStream_t st) {
-  if (s.dtype == MTNLG_BF16) {
-    const double split = gated_split_time(M, N, K, ws ? s.gemm_ws : 0);
-    // (rows that do not begin at whole lines cost the 32 and 64 tiles a third more than their estimate)
-    if (split < gemm_time(s.dtype, layout, M, N, K, s.gemm_ws) && !gemm_wave_pick(s.dtype, layout, M, N, K, split / (K % 64 ? 1.35 : 1.0))) {
-      const int status = gated_split(layout, M, N, K, A, B, C, ws, s.gemm_ws, st);
-      if (status != MTNLG_UNSUPPORTED_SHAPE) return status;
-    }
-  }
-  return mtnlg_gemm(s.dtype, layout, M, N, K, A, B, C, nullptr, nullptr, 0, ws, s.gemm_ws, st);
 }
 
 struct Bytes {
@@ -66,6 +55,19 @@ bool lies_apart(const Bytes *out, int outs, const Bytes *in, int ins) {
   return true;
 }
 
+// Whether a bf16 product is estimated to be fastest on tiles that are cut along K (rows that do not begin at whole lines cost the 32 and 64 tiles of
+// gemm_wave.hip a third more than their estimate)
+bool cut_along_k(const Sizes &s, int layout, int64_t M, int64_t N, int64_t K) {
+  const double split = gated_split_time(M, N, K, s.gemm_ws);
+  return split < gemm_time(s.dtype, layout, M, N, K, s.gemm_ws) && !gemm_wave_pick(s.dtype, layout, M, N, K, split / (K % 64 ? 1.35 : 1.0)) &&
+         (int64_t)128 * (2 * K + N) * 2 < ((int64_t)1 << 31);   // (what 32-bit offsets reach, with room)
+}
+// C = A B^T (NT) or A B (NN) without the activation
+int plain_product(const Sizes &s, int layout, int64_t M, int64_t N, int64_t K, const void *A, const void *B, void *C, void *ws, hipStream_t st) {
+  if (s.dtype == MTNLG_BF16 && cut_along_k(s, layout, M, N, K)) return gated_split(layout, M, N, K, A, B, C, ws, s.gemm_ws, st);
+  return mtnlg_gemm(s.dtype, layout, M, N, K, A, B, C, nullptr, nullptr, 0, ws, s.gemm_ws, st);
+}
+
 // One of the two products that carry the activation, on the kernel that is estimated to be the fastest
 double gated_time(const Sizes &s, int mode) {
   const int layout = mode == GATE_FWD ? MTNLG_GEMM_NT : MTNLG_GEMM_NN;
@@ -76,11 +78,12 @@ int gated_product(const Sizes &s, int mode, const void *A, const void *B, void *
   const int layout = mode == GATE_FWD ? MTNLG_GEMM_NT : MTNLG_GEMM_NN;
   const int64_t N = mode == GATE_FWD ? 2 * s.F : s.F;
   if (s.dtype == MTNLG_BF16 && mode == GATE_FWD && gated_tokens_takes(s.T, N, s.h)) return gated_tokens_fwd(s.gate, s.T, s.h, s.F, A, B, z, C, st);
-  if (const int tile = gemm_wave_pick(s.dtype, layout, s.T, N, s.h, gated_time(s, mode)))
+  const bool split = s.dtype == MTNLG_BF16 && cut_along_k(s, layout, s.T, N, s.h);
+  if (const int tile = split ? 0 : gemm_wave_pick(s.dtype, layout, s.T, N, s.h, gated_time(s, mode)))
     return gated_wave(s.dtype, mode, s.gate, s.T, s.h, s.F, A, B, z, C, tile, st);
   if (s.dtype == MTNLG_F32) return gated_parts(mode, s.gate, s.T, s.h, s.F, A, B, z, C, st);
-  return mode == GATE_FWD ? gated_mfma_fwd(s.gate, s.T, s.h, s.F, A, B, z, C, ws, s.gemm_ws, st)
-                          : gated_mfma_bwd(s.gate, s.T, s.h, s.F, A, B, z, C, ws, s.gemm_ws, st);
+  return mode == GATE_FWD ? gated_mfma_fwd(s.gate, s.T, s.h, s.F, A, B, z, C, split, ws, s.gemm_ws, st)
+                          : gated_mfma_bwd(s.gate, s.T, s.h, s.F, A, B, z, C, split, ws, s.gemm_ws, st);
 }
 
 }  // namespace

@@ -166,10 +166,10 @@ int launch_tokens(const TokenArgs &a, hipStream_t st) {
 
 }  // namespace
 
-// Whether a product by T tokens belongs here: up to 32 always, up to 64 where the weights are many (20480 x 10240 by 48 tokens 88 us, on gemm_wave.hip's
-// tiles 114; 16384 x 2048 18.4 and 17.6).
+// Whether a product by T tokens belongs here: up to 32 always, up to 64 where many rows of weights are long or do not begin at whole lines (us, here / on
+// gemm_wave.hip's tiles: 20480 x 10240 by 48 tokens 81 / 114, 16384 x 2048 17.5 / 17.6, 20160 x 2040 by 57 tokens 29 / 47; 2048 x 8192 by 48 19.3 / 17.2).
 bool gated_tokens_takes(int64_t T, int64_t N, int64_t K) {
-  return (T <= 32 || (T <= 64 && N * K >= (int64_t)1 << 26)) && (96 + N / 2) * K * 2 < (int64_t)RECORDS - 256;
+  return (T <= 32 || (T <= 64 && N >= 4096 && (N * K >= (int64_t)1 << 25 || K % 64))) && (96 + N / 2) * K * 2 < (int64_t)RECORDS - 256;
 }
 
 int gated_tokens_fwd(int kind, int64_t T, int64_t h, int64_t F, const void *x, const void *w_fc1, void *z, void *g, hipStream_t stream) {

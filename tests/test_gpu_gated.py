@@ -16,7 +16,7 @@ F = 2.0 ** -23
 GATES = {"silu": M.GATE_SILU, "gelu_tanh": M.GATE_GELU_TANH, "gelu_erf": M.GATE_GELU_ERF}
 # tokens, hidden, ffn: one token to many, widths that no tile divides, whole tiles of every kernel, and rows on either side of where the kernels change
 SIZES = [(1, 8, 8), (1, 2048, 1024), (2, 64, 40), (5, 1032, 520), (16, 512, 1368), (17, 520, 344), (24, 2560, 1024), (32, 776, 264), (33, 1024, 2048), (61, 520, 344),
-         (64, 2048, 776), (65, 264, 128), (130, 264, 136), (128, 4096, 256), (256, 512, 1024), (300, 2048, 1000), (130, 1032, 5464), (777, 2048, 5464), (200, 4096, 4104), (257, 1024, 776), (512, 640, 1280),
+         (64, 2048, 776), (65, 264, 128), (130, 264, 136), (128, 4096, 256), (256, 512, 1024), (300, 2048, 1000), (130, 1032, 5464), (777, 2048, 5464), (200, 4096, 4104), (106, 5664, 1648), (70, 8192, 520), (257, 1024, 776), (512, 640, 1280),
          (1024, 2048, 2048), (2048, 1280, 2560)]
 
 
@@ -123,7 +123,7 @@ def test_forward_and_backward(dtype, T, h, ffn):
 # several with a tail; token counts around whole groups; more tokens where the weights are many
 @pytest.mark.parametrize("T,h,ffn", [(1, 8, 16), (1, 136, 10240), (3, 1032, 10248), (8, 20480, 328), (9, 72, 5120), (9, 1032, 10240), (15, 4096, 2048), (16, 2048, 8192),
                                      (17, 520, 12288), (20, 2048, 10240), (24, 4104, 7168), (31, 1544, 4096), (32, 20480, 640), (32, 600, 1304), (40, 2048, 16384),
-                                     (48, 4096, 10240), (49, 8200, 4600), (64, 2048, 16392), (64, 5120, 14336), (41, 10240, 3584)])
+                                     (48, 4096, 10240), (49, 8200, 4600), (64, 2048, 16392), (64, 5120, 14336), (41, 10240, 3584), (57, 2040, 1008), (33, 264, 520)])
 def test_few_tokens(T, h, ffn):
     kind = ("silu", "gelu_tanh", "gelu_erf")[T % 3]
     s = inputs(T, h, ffn, "bf16", T)
