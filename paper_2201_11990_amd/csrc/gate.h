@@ -30,6 +30,19 @@ __device__ __forceinline__ void gate_one(float x, float &a, float &slope) {
       a = gelu_f(x, false);
       slope = gelu_grad_f(x, false);
     }
+  } else if constexpr (FAST) {
+    // The normal distribution's tail below -|x| as exp(-x^2 / 2) t P(t), t = 1 / (1 + 0.44 |x| / sqrt 2): P of degree 7 fitted here to the least relative error
+    // over |x| <= 14 (1.8e-7), so nothing cancels for negative x.  16 instructions, where the library's erf made the product that carries it take 140 us longer
+    // forward and backward (6331 tokens, F 5456).
+    constexpr float C[8] = {0.124110477f, 0.12443559f, 0.108656778f, 0.107906111f, -0.0100903258f, 0.148343735f, -0.13897401f, 0.0356117356f};
+    const float t = __builtin_amdgcn_rcpf(1.0f + 0.311126984f * fabsf(x)), e = __builtin_amdgcn_exp2f(x * x * -0.72134752f);
+    float tail = C[7];
+#pragma unroll
+    for (int i = 6; i >= 0; --i) tail = tail * t + C[i];
+    tail *= t * e;
+    const float cdf = x < 0.0f ? tail : 1.0f - tail;
+    a = x * cdf;
+    slope = cdf + x * (e * 0.39894228f);
   } else {
     a = gelu_f(x, true);
     slope = gelu_grad_f(x, true);

@@ -136,9 +136,15 @@ int mtnlg_gated_ffn_bwd(const mtnlg_gated_desc *desc, const void *x, const void 
   auto gemm = [&](int layout, const GemmCall &c) {
     return mtnlg_gemm(s.dtype, layout, c.M, c.N, c.K, c.A, c.B, c.C, nullptr, nullptr, c.epi, workspace, s.gemm_ws, stream);
   };
-  auto time = [&](int layout, const GemmCall &c) { return gemm_time(s.dtype, layout, c.M, c.N, c.K, s.gemm_ws); };
+  // Both products of a weight in one launch, if that is estimated to be faster; the estimate does not know of rows that begin amid lines, which cost long
+  // launches a third (7473 tokens, h 2680, F 560: 144 us for what two launches take 112 for)
+  auto one_launch = [&](const GemmCall &nn, double nn_time, const GemmCall &tn) {
+    const double tn_time = gemm_time(s.dtype, MTNLG_GEMM_TN, tn.M, tn.N, tn.K, s.gemm_ws);
+    const double less = s.dtype == MTNLG_BF16 && (s.h % 64 || s.F % 64) && nn_time + tn_time > 50.0 ? 1.0 / 1.35 : 1.0;
+    return gemm_wave_group_tile(s.dtype, nn, tn, 0, 0, 0, nn_time * less, tn_time * less);
+  };
   const GemmCall to_dz{s.T, s.F, s.h, dy, w_fc2, dz, const_cast<void *>(z), (uint32_t)s.gate}, to_dw2{s.h, s.F, s.T, dy, g, dw_fc2, nullptr, epi};
-  const int tile2 = dw_fc2 ? gemm_wave_group_tile(s.dtype, to_dz, to_dw2, 0, 0, 0, gated_time(s, GATE_BWD), time(MTNLG_GEMM_TN, to_dw2)) : 0;
+  const int tile2 = dw_fc2 ? one_launch(to_dz, gated_time(s, GATE_BWD), to_dw2) : 0;
   if (tile2) {
     MTNLG_TRY(gated_wave_group(s.dtype, to_dz, to_dw2, tile2, st));
   } else {
@@ -147,7 +153,7 @@ int mtnlg_gated_ffn_bwd(const mtnlg_gated_desc *desc, const void *x, const void 
   }
   const GemmCall to_dx{s.T, s.h, 2 * s.F, dz, w_fc1, dx, nullptr, 0}, to_dw1{2 * s.F, s.h, s.T, dz, x, dw_fc1, nullptr, epi};
   if (dx && dw_fc1)
-    if (const int tile = gemm_wave_group_tile(s.dtype, to_dx, to_dw1, 0, 0, 0, time(MTNLG_GEMM_NN, to_dx), time(MTNLG_GEMM_TN, to_dw1)))
+    if (const int tile = one_launch(to_dx, gemm_time(s.dtype, MTNLG_GEMM_NN, to_dx.M, to_dx.N, to_dx.K, s.gemm_ws), to_dw1))
       return gemm_wave_group(s.dtype, to_dx, to_dw1, ColumnSums{}, tile, st);
   if (dx) MTNLG_TRY(plain_product(s, MTNLG_GEMM_NN, s.T, s.h, 2 * s.F, dz, w_fc1, dx, workspace, st));
   if (dw_fc1) MTNLG_TRY(gemm(MTNLG_GEMM_TN, to_dw1));
