@@ -57,6 +57,16 @@ struct NormArgs {
 };
 static_assert(sizeof(NormArgs) + 32 <= 4096, "arguments of a launch");
 
+// Few chunks, each named on the host: a wave's first wait is for its own entry
+struct NormChunk {
+  const void *g;
+  int64_t count;   // elements from g on, at most kChunk
+};
+struct NormOnceArgs {
+  uint32_t chunks;
+  NormChunk of[kOnce];
+};
+
 // the tensor that chunk c is of: the last one that begins at it or before.  Every lane looks at some of the tensors: one load's latency, where a
 // binary search through 64 of them waits for six
 template <int MOST, typename A>
@@ -277,53 +287,43 @@ __global__ __launch_bounds__(256) void adam_many_kernel(StepArgs s) {
   }
 }
 
-// A chunk's elements, this thread's share of THREADS, 16 bytes a load (of bf16 whose alignment is 8: a load of four dwords needs no more than a dword's)
+// The squares of `left` elements of a chunk (p and left the same in all lanes), this thread's share of THREADS: 16 bytes a load, past the caches; vectors
+// that do not lie within the chunk as a whole are outside the descriptor and arrive as zeros, and what is left of the last one is read an element a lane
 template <typename G, int THREADS>
-struct Squares {
-  static constexpr int W = 16 / sizeof(G), TURNS = kChunk / (W * THREADS);
-  f32x4 g[TURNS][W / 4];
-  __device__ __forceinline__ void load(const NormArgs &s, uint32_t c) {
-    const NormTensor &t = s.of[tensor_of<kNormTensors>(s, c)];
-    const G *p = static_cast<const G *>(t.g);
-    const int64_t n = t.count, base = (int64_t)(c - t.first_chunk) * kChunk, first = base + threadIdx.x % THREADS * W;
-    if (base + kChunk <= n) {
+__device__ __forceinline__ double squares(const G *p, int left) {
+  constexpr int W = 16 / sizeof(G), TURNS = kChunk / (W * THREADS), NONTEMPORAL = 2;
+  const int lane = threadIdx.x % THREADS;
+  const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<G *>(p), 0, left / W * 16, 0x00020000);
+  f32x4 raw[TURNS];
 #pragma unroll
-      for (int u = 0; u < TURNS; ++u) {
-        const int64_t i = first + u * W * THREADS;
-        if constexpr (sizeof(G) == 4) {
-          g[u][0] = stream4(p + i);
-        } else {
-          const bf16x8 x = __builtin_bit_cast(bf16x8, __builtin_nontemporal_load(reinterpret_cast<const f32x4 *>(p + i)));
+  for (int u = 0; u < TURNS; ++u)
+    raw[u] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, (u * THREADS + lane) * 16, 0, NONTEMPORAL));
+  const float rest = lane < left % W ? to_f32(p[left / W * W + lane]) : 0.0f;
+  double s = (double)rest * rest;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) g[u][e / 4][e % 4] = (float)x[e];
-        }
+  for (int u = 0; u < TURNS; ++u)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float x = raw[u][e];
+      if constexpr (sizeof(G) == 4) {
+        s += (double)x * x;
+      } else {   // two bf16 values, the upper halves of fp32 ones
+        const uint32_t w = __builtin_bit_cast(uint32_t, x);
+        const float lo = __builtin_bit_cast(float, w << 16), hi = __builtin_bit_cast(float, w & 0xFFFF0000u);
+        s += (double)lo * lo;
+        s += (double)hi * hi;
       }
-    } else {
-#pragma unroll
-      for (int u = 0; u < TURNS; ++u)
-#pragma unroll
-        for (int o = 0; o < W / 4; ++o) g[u][o] = load_some<false>(p, first + u * W * THREADS + 4 * o, n);
     }
-  }
-  __device__ __forceinline__ double sum() const {
-    double s = 0.0;
-#pragma unroll
-    for (int u = 0; u < TURNS; ++u)
-#pragma unroll
-      for (int o = 0; o < W / 4; ++o)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) s += (double)g[u][o][e] * g[u][o][e];
-    return s;
-  }
-};
+  return s;
+}
 // partial[block] = the squares of chunks block, block + grid, ..., added to what launches before left in the first `have`
 template <typename G>
 __global__ __launch_bounds__(256) void norm_many_kernel(NormArgs s, double *__restrict__ partial, int have) {
   double sum = 0.0;
   for (uint32_t c = blockIdx.x; c < s.chunks; c += gridDim.x) {
-    Squares<G, 256> q;
-    q.load(s, c);
-    sum += q.sum();
+    const NormTensor &t = s.of[tensor_of<kNormTensors>(s, c)];
+    const int64_t base = (int64_t)(c - t.first_chunk) * kChunk, left = t.count - base;
+    sum += squares<G, 256>(static_cast<const G *>(t.g) + base, left < kChunk ? (int)left : kChunk);
   }
   sum = workgroup_sum<256>(sum);
   if (threadIdx.x == 0) partial[blockIdx.x] = (int)blockIdx.x < have ? partial[blockIdx.x] + sum : sum;
@@ -340,13 +340,11 @@ __global__ __launch_bounds__(256) void norm_many_sum(int blocks, const double *_
 }
 // Few elements: the launches are the time, so there is one
 template <typename G>
-__global__ __launch_bounds__(1024) void norm_many_once(NormArgs s, float *__restrict__ out, int accumulate) {
+__global__ __launch_bounds__(1024) void norm_many_once(NormOnceArgs s, float *__restrict__ out, int accumulate) {
   double sum = 0.0;
-  for (uint32_t c = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); c < s.chunks; c += 16) {
-    Squares<G, 64> q;
-    q.load(s, c);
-    sum += q.sum();
-  }
+#pragma unroll 1
+  for (uint32_t c = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); c < s.chunks; c += 16)
+    sum += squares<G, 64>(static_cast<const G *>(s.of[c].g), (int)s.of[c].count);
   sum = workgroup_sum<1024>(sum);
   if (threadIdx.x == 0) out[0] = (float)(accumulate ? (double)out[0] + sum : sum);
 }
@@ -421,6 +419,17 @@ int mtnlg_grad_sqnorm_many(int32_t tensors, const mtnlg_adam_tensor *of, int gra
   }
   hipStream_t st = (hipStream_t)stream;
   LaunchScope scope(MTNLG_K_ELEMENTWISE, st);
+  NormOnceArgs once;
+  once.chunks = 0;
+  int32_t named = 0;
+  for (; named < tensors && once.chunks + (of[named].count + kChunk - 1) / kChunk <= kOnce; ++named)
+    for (int64_t at = 0; at < of[named].count; at += kChunk)
+      once.of[once.chunks++] = NormChunk{(const char *)of[named].grad + at * (f32 ? 4 : 2), std::min<int64_t>(of[named].count - at, kChunk)};
+  if (named == tensors) {
+    if (f32) norm_many_once<float><<<1, 1024, 0, st>>>(once, sqnorm, accumulate ? 1 : 0);
+    else norm_many_once<bf16><<<1, 1024, 0, st>>>(once, sqnorm, accumulate ? 1 : 0);
+    return check_launch();
+  }
   int have = 0;
   for (int32_t i = 0; i < tensors;) {
     NormArgs s;
@@ -432,11 +441,6 @@ int mtnlg_grad_sqnorm_many(int32_t tensors, const mtnlg_adam_tensor *of, int gra
     }
     s.chunks = (uint32_t)chunks;   // (a tensor has up to 2^27)
     s.tensors = k;
-    if (i == 0 && k == tensors && chunks <= kOnce) {
-      if (f32) norm_many_once<float><<<1, 1024, 0, st>>>(s, sqnorm, accumulate ? 1 : 0);
-      else norm_many_once<bf16><<<1, 1024, 0, st>>>(s, sqnorm, accumulate ? 1 : 0);
-      return check_launch();
-    }
     const int grid = chunks < kNormBlocks ? (int)chunks : kNormBlocks;
     if (f32) norm_many_kernel<float><<<grid, 256, 0, st>>>(s, (double *)workspace, have);
     else norm_many_kernel<bf16><<<grid, 256, 0, st>>>(s, (double *)workspace, have);
