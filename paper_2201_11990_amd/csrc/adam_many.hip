@@ -500,6 +500,7 @@ int mtnlg_adam_step_many(const mtnlg_adam_many_desc *desc, const mtnlg_adam_tens
   LaunchScope scope(MTNLG_K_ELEMENTWISE, st);
   StepArgs s;
   s.a = adam_args(desc->adam);
+  if (eight) s.a.eps = fmaxf(s.a.eps, 0x1p-126f);   // what it is added to is multiplied with by its reciprocal: finite
   s.sqnorm = sqnorm;
   step_keys(desc->seed, desc->adam.step, &s.key_lo, &s.key_hi);
   uint32_t block = 0;

@@ -210,6 +210,28 @@ def test_first_step_from_nothing_and_without_a_norm(bits):
     check(before, rows, bits, None, 1, seed=5)
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+def test_nothing_comes_of_nothing_whatever_eps(bits):
+    rows = with_states(model([1000], "fp32"), bits, zero=True)
+    rows[0]["grad"].zero_()
+    before = copies(rows)
+    M.mtnlg_adam_step_many(rows, lr=1e-3, step=1, eps=1e-42, weight_decay=0.0)
+    for k in ("master", "m", "v"):
+        assert torch.equal(rows[0][k].view(torch.uint8), before[0][k].view(torch.uint8)), k
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_gradient_that_two_tensors_share(bits):
+    rows = with_states(model([5000, 5000, 300], "bf16"), bits)
+    rows[1]["grad"] = rows[0]["grad"]
+    before = copies(rows)
+    sq, _ = run_norm(rows)
+    want = norm_of(rows)
+    assert abs(float(sq) - want) <= 2.0 ** -24 * want * 1.01
+    M.mtnlg_adam_step_many(rows, sq, lr=1e-3, step=2, seed=9)
+    check(before, rows, bits, float(sq), 2, seed=9)
+
+
 def test_states_of_32_bits_as_the_step_on_one_tensor():
     rows = with_states(model(COUNTS["mixed"], "fp32"), 32)
     one = copies(rows)
