@@ -2,12 +2,15 @@
 //
 // A model's parameters are a few large tensors and many small ones (gains, biases), and a launch for each is what the small ones cost.
 // Here the addresses and sizes of up to kStepTensors tensors travel in the launch's arguments (no table in device memory, nothing to copy before the
-// call), every tensor is cut into chunks of 4096 elements, and a workgroup finds its chunk's tensor by a binary search through uniform values.
+// call), every tensor is cut into chunks of 4096 elements, and a workgroup finds its chunk's tensor with a ballot over where they begin.
 //
 // States in 8 bits: e4m3 codes of m and of r = sqrt(v), with one fp32 scale each to a block of 256 elements, which is what a wave takes at 4
 // elements a lane, so that a block's largest magnitude is one reduction over the wave.  r and not v: a code's range (2^-9 .. 448 times the scale) then spans
 // 10 decades of v, and a step is at most 1/8 of r as it is of m.  Codes are rounded up with the probability of the part of a step that is left: rounded to
 // nearest, a moment whose change in a step is below half a code (beta2 = 0.95 takes 5 % of v, 2.5 % of r; a code is 6 to 12 % wide) would never move.
+//
+// Both are bound by HBM: 122 M parameters in fp32 (30 bytes each) 620 us, 5.9 TB/s; 243 M in 8 bits with bf16 gradients (16 bytes) 660 us, 5.9 TB/s; their norms 75 and 77 us,
+// 6.4 and 6.3 TB/s (a copy of 2 GiB: 4.7 to 4.9 TB/s without the hint that goes past the caches).
 #include <algorithm>
 #include <new>
 #include <type_traits>

@@ -1,12 +1,12 @@
 // The gated feed-forward block's products for few tokens (a model in use: the next token of some sequences), bf16: x [T, K] by weights [N, K].
 //
-// Every weight is used for at most 64 tokens, so its way from memory is all (h 20480, F 10240: 1.26 GB, 219 us at the 5.75 TB/s that the weights
-// of one token have been read at).  A workgroup has TN rows of weights and all tokens; its eight waves take every eighth slab of 64 k each, through stages
-// of their own that DMA fills with whole 128-byte lines, so nothing waits for another wave before the sums meet in LDS, where they are added in wave
-// order.  (Fragments straight from memory to registers, 16 rows x 64 bytes an instruction, reached 3.2 to 4.7 TB/s where this reaches 5 to 6.1.)
+// Every weight is used for at most 64 tokens, so its way from memory is all (h 20480, F 10240: 1.26 GB).  A workgroup has TN rows of weights and all
+// tokens; its eight waves take every eighth slab of 64 k each, through stages of their own that DMA fills with whole 128-byte lines past the caches, so nothing
+// waits for another wave before the sums meet in LDS, where they are added in wave order.  One token takes 122 us by 20480 x 20480 (6.9 TB/s) and 62 by
+// 20480 x 10240; without the hint that goes past the caches 139 and 71, with fragments straight from memory to registers, 16 rows x 64 bytes an instruction, 180 and 87.
 // The tokens come from the caches, once for every TN rows: what that costs beside the weights (28 % of their time times T / TN), and compute units that
-// others wait for, is what the choice of TN goes by.  us for 20480 x 20480 / 20480 x 10240, TN 16 / 32 / 48 / 64 / 80: 1 token 139 / 148 / 144 / 173 / 143, 71 / 78
-// / 77 / 92 / -; 24 tokens 197 / 172 / 160 / 192 / 146, 104 / 91 / 85 / 102 / 82 (80: 256 workgroups, 64: 320); on the 32 x 32 tiles of gemm_wave.hip 169 and 94.
+// others wait for, is what the choice of TN goes by.  us by 20480 x 20480 / 20480 x 10240, 24 tokens, TN 32 / 48 / 80 / 96: 163 / 150 / 136 / 143, 84 / 78 / 75 / 79 (80: 256
+// workgroups); on the 32 x 32 tiles of gemm_wave.hip 169 and 94.
 #include <algorithm>
 
 #include "gated.h"
@@ -123,7 +123,7 @@ int launch(const TokenArgs &a, hipStream_t st) {
 int token_groups(int64_t T) { return T <= 8 ? 1 : T <= 16 ? 2 : T <= 32 ? 4 : T <= 48 ? 6 : 8; }
 
 // Rows of weights to a workgroup, of 16 times 1 .. 6 the one with the least of: the tokens' share; stages that few slabs a wave leave waiting for memory
-// (64 rows in four slabs: 16.7 us for 16384 x 2048 by 16 tokens, 16 rows 15.5, 32 rows 15.6); compute units that have more workgroups than others, half of
+// (16384 x 2048 by 16 tokens, four slabs a wave: 64 rows 15.4 us, 16 rows 15.1, 32 rows 14.6); compute units that have more workgroups than others, half of
 // which the memory's time hides where all workgroups are on the chip at once.
 int rows_of(int64_t T, int64_t N, int64_t K) {
   const int nx = token_groups(T);
@@ -144,7 +144,7 @@ int rows_of(int64_t T, int64_t N, int64_t K) {
 template <int NX, int GATE>
 int launch_rows(const TokenArgs &a, hipStream_t st) {
   switch (rows_of(a.T, a.N, a.K)) {
-    // a second stage pays where a wave has many slabs, or the tokens are next to nothing (2048 x 8192: 13.3 / 10.9 us; 16384 x 2048, 16 tokens: 15.5 / 16.3)
+    // a second stage pays where a wave has many slabs, or the tokens are next to nothing (one and two stages: 2048 x 8192, one token 12.7 / 10.2 us; 16384 x 2048, 16 tokens 15.1 / 15.6)
     case 16: return a.T <= 8 || a.K >= 8 * 64 * WAVES ? launch<NX, 16, 2, GATE>(a, st) : launch<NX, 16, 1, GATE>(a, st);
     case 32: return launch<NX, 32, 1, GATE>(a, st);
     case 48: return launch<NX, 48, 1, GATE>(a, st);
