@@ -499,7 +499,8 @@ typedef struct {
 } mtnlg_adam_many_desc;
 
 /* mtnlg_grad_sqnorm over the gradients of all tensors (of `tensors` entries the fields count and grad): one launch up to 32 chunks of 4096
- * elements, else one per 160 tensors and one more.  Elements are added in a fixed order, in 64 bits.  grad 16-byte aligned (bf16: 8). */
+ * elements, else one per 160 tensors and one more.  Elements are added in a fixed order, in 64 bits.  grad 16-byte aligned (bf16: 8); sqnorm and
+ * workspace lie on no gradient and not on each other. */
 size_t mtnlg_grad_sqnorm_many_workspace(void);
 int mtnlg_grad_sqnorm_many(int32_t tensors, const mtnlg_adam_tensor *of, int grad_dtype, void *workspace, size_t workspace_bytes, float *sqnorm,
                            int accumulate, void *stream);
@@ -512,6 +513,7 @@ int mtnlg_grad_sqnorm_many(int32_t tensors, const mtnlg_adam_tensor *of, int gra
  * in its block.  So rounding has no bias, which moments need that change by less than a code in a step, and the same call gives the same codes.  A root that is not zero is one step at
  * least, so that no update divides by a lost one.  NaN gives the code of NaN; squares of gradients have to be finite.  Codes of zero are zero with any
  * finite scale: a program begins with codes and scales of 0.
+ * The descriptor's values are arguments of the launches: a captured call repeats its step, rate and seed.
  * Alignment: master 16 bytes, m and v 16 (codes: 4), grad 16 (bf16: 8), weight_bf16 8.  What is written lies on nothing else of the call (the same tensor twice is
  * MTNLG_INVALID_ARG). */
 int mtnlg_adam_step_many(const mtnlg_adam_many_desc *desc, const mtnlg_adam_tensor *of, const float *sqnorm, void *stream);

@@ -419,7 +419,12 @@ int mtnlg_grad_sqnorm_many(int32_t tensors, const mtnlg_adam_tensor *of, int gra
     if (!of[i].grad) return MTNLG_NULL_POINTER;
     if (of[i].count <= 0 || ((uintptr_t)of[i].grad & (f32 ? 15 : 7))) return MTNLG_INVALID_ARG;
     if (!count_ok(of[i].count)) return MTNLG_UNSUPPORTED_SHAPE;
+    // what is written lies on no gradient
+    const uintptr_t from = (uintptr_t)of[i].grad, to = from + (uintptr_t)(of[i].count * (f32 ? 4 : 2));
+    if (((uintptr_t)sqnorm < to && from < (uintptr_t)sqnorm + 4) || ((uintptr_t)workspace < to && from < (uintptr_t)workspace + kNormBlocks * sizeof(double)))
+      return MTNLG_INVALID_ARG;
   }
+  if ((uintptr_t)sqnorm < (uintptr_t)workspace + kNormBlocks * sizeof(double) && (uintptr_t)workspace < (uintptr_t)sqnorm + 4) return MTNLG_INVALID_ARG;
   hipStream_t st = (hipStream_t)stream;
   LaunchScope scope(MTNLG_K_ELEMENTWISE, st);
   NormOnceArgs once;

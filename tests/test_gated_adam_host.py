@@ -171,6 +171,11 @@ def test_norm_arguments_that_are_refused():
     assert call([tensor(), tensor(1, grad=None)]) == NULL
     assert call([tensor(grad=(1 << 45) + 8)]) == INVALID and call([tensor(grad=(1 << 45) + 4)], dtype=B.BF16) == INVALID
     assert call([tensor(count=0)]) == INVALID and call([tensor(count=(1 << 39) + 1)]) == SHAPE
+    size, at = M.mtnlg_grad_sqnorm_many_workspace(), 1 << 45
+    for kw in (dict(sqnorm=at), dict(sqnorm=at + 3996), dict(workspace=at), dict(workspace=at + 3984), dict(workspace=at - size + 16)):
+        assert call([tensor(), tensor(1, grad=at)], **kw) == INVALID, kw
+    for sqnorm in (1 << 50, (1 << 50) + size - 4):
+        assert call(one, sqnorm=sqnorm) == INVALID
 
 
 def test_tables_refuse_what_does_not_fit():

@@ -232,6 +232,24 @@ def test_a_gradient_that_two_tensors_share(bits):
     check(before, rows, bits, float(sq), 2, seed=9)
 
 
+def test_many_launches_of_small_tensors():
+    # 1500 tensors side by side in one buffer: 27 launches, and norms of 10
+    sizes = [(i * 37) % 61 * 4 + 4 for i in range(1500)]
+    flat = with_states(model([sum(sizes)], "fp32"), 32)[0]
+    one = copies([flat])[0]
+    rows, at = [], 0
+    for n in sizes:
+        rows.append({k: (v[at:at + n] if isinstance(v, torch.Tensor) else v) for k, v in flat.items()})
+        at += n
+    sq, _ = run_norm(rows)
+    want = norm_of([flat])
+    assert abs(float(sq) - want) <= 2.0 ** -24 * want * 1.01
+    M.mtnlg_adam_step_many(rows, sq, lr=1e-3, step=3)
+    M.mtnlg_adam_step_many([one], sq, lr=1e-3, step=3)
+    for k in ("master", "m", "v", "weight_bf16"):
+        assert torch.equal(flat[k], one[k]), k
+
+
 def test_states_of_32_bits_as_the_step_on_one_tensor():
     rows = with_states(model(COUNTS["mixed"], "fp32"), 32)
     one = copies(rows)

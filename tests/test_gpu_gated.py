@@ -305,3 +305,13 @@ def test_rows_behind_the_outputs_are_left_as_they_were():
             backward(desc, s, ws)
             forward(desc, s, ws, z=False)
             assert all((t[s[k].shape[0]:] == 7).all() for k, t in whole.items())
+
+
+def test_matrices_that_are_not_dense_or_elsewhere_are_refused():
+    s = inputs(6, 64, 128, "bf16")
+    desc = M.gated_desc(s["x"], s["w_fc1"])
+    for k, bad in (("x", torch.empty(64, 6, dtype=torch.bfloat16, device="cuda").T), ("w_fc2", torch.empty(128, 64, dtype=torch.bfloat16, device="cuda").T),
+                   ("g", torch.empty(6, 256, dtype=torch.bfloat16, device="cuda")[:, :128]), ("y", torch.empty(6, 64, dtype=torch.bfloat16)),
+                   ("z", torch.empty(6, 128, dtype=torch.bfloat16, device="cuda"))):
+        with pytest.raises(ValueError):
+            forward(desc, {**s, k: bad}, None)
