@@ -307,6 +307,32 @@ def test_rows_behind_the_outputs_are_left_as_they_were():
             assert all((t[s[k].shape[0]:] == 7).all() for k, t in whole.items())
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("kind", list(GATES))
+@pytest.mark.parametrize("T", [16, 300])
+def test_gates_far_from_zero(dtype, kind, T):
+    h, ffn = 64, 128
+    s = inputs(T, h, ffn, dtype)
+    # z = [+- x0, x1] by weights of one value a row
+    s["w_fc1"].zero_()
+    s["w_fc1"][:ffn, 0] = torch.tensor([1.0, -1.0], device="cuda").repeat(ffn // 2)
+    s["w_fc1"][ffn:, 1] = 1.0
+    s["x"][:, 0] = torch.tensor([9.0, 12.0, 79.0, 81.0, 90.0, 1e4, 1e10, 1e12, 1e14, 1e20, 1e30, 1e36], device="cuda").repeat(T // 12 + 1)[:T]
+    desc = M.gated_desc(s["x"], s["w_fc1"], GATES[kind])
+    ws = room(desc)
+    forward(desc, s, ws)
+    check_forward(kind, s)
+    backward(desc, s, ws)
+    check_backward(kind, s)
+    negative = s["z"][:, 1:ffn:2].double()
+    assert (s["g"][:, 1::2].double().abs() <= 80 * torch.exp(-negative.abs().clamp(max=70))).all()   # act(-r) < r exp(-r)
+    far = s["z"][:, :ffn].double().abs() >= 1e4   # slopes of 0 and 1
+    dg, e = product(s["dy"], s["w_fc2"].T)
+    one = (s["z"][:, :ffn] > 0).double() * dg * s["z"][:, ffn:].double()
+    error = (e + 2 * F * dg.abs()) * s["z"][:, ffn:].double().abs() + 1e-20
+    within(s["dz"][:, :ffn][far], one[far], (error + HALF_STEP[s["x"].dtype] * (one.abs() + error))[far], "dz far from zero")
+
+
 def test_matrices_that_are_not_dense_or_elsewhere_are_refused():
     s = inputs(6, 64, 128, "bf16")
     desc = M.gated_desc(s["x"], s["w_fc1"])
