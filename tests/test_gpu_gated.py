@@ -310,7 +310,7 @@ def test_rows_behind_the_outputs_are_left_as_they_were():
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("kind", list(GATES))
 @pytest.mark.parametrize("T", [16, 300])
-def test_gates_far_from_zero(dtype, kind, T):
+def test_gates_at_their_limits(dtype, kind, T):
     h, ffn = 64, 128
     s = inputs(T, h, ffn, dtype)
     # z = [+- x0, x1] by weights of one value a row
