@@ -395,6 +395,8 @@ typedef struct {
 /* z = x w_fc1^T [T,2F];  g = act(z[:, :F]) * z[:, F:] [T,F];  y = g w_fc2^T [T,h], under tensor slicing a row-parallel partial sum as that of
  * FC2 above.  w_fc1 [2F,h]: the F rows of the gate, then the other projection's; w_fc2 [h,F].  All matrices dense, in the storage type.
  * z is what backward reads, stored rounded; NULL: it is not kept (a model in use).  g is of z before its rounding; y of g as stored.
+ * Where the gate's column of z is infinite, act and act' are what their formulas give in floating point: act(inf) = inf, act(-inf) = -inf times 0 = NaN,
+ * act' NaN at both, for every gate and type: sums that overflow are not hidden by the activation's limit of 0.
  * workspace (16-byte aligned; nullable where its size is 0): mtnlg_gated_ffn_workspace() bytes for either pass, contents destroyed.  Outputs and workspace lie on no other argument. */
 size_t mtnlg_gated_ffn_workspace(const mtnlg_gated_desc *desc);
 int mtnlg_gated_ffn_fwd(const mtnlg_gated_desc *desc, const void *x, const void *w_fc1, const void *w_fc2, void *z, void *g, void *y,

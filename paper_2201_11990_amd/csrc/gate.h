@@ -4,14 +4,17 @@
 
 namespace mtnlg {
 
+__device__ __forceinline__ float nan_of_inf(float x, float y) { return __builtin_fmaf(x, 0.0f, y); }   // y, or NaN where x is not finite
 // FAST: hardware exp2 and reciprocal (1 ulp each), a few 1e-7 of relative error, for results that round to bf16: silu(x) = x s, s = 1 / (1 + exp(-x)), silu' = s + x s (1 - s) with 1 - s =
 // exp(-x) s; GeLU's tanh form likewise (gelu_sigmoid_f).  x is clamped where both have reached their limits to 1e-32, so that exp(-x) s and powers of x
-// stay finite and large negative values give no multiple of themselves; comparisons, which let NaN through.
+// stay finite and large negative values give no multiple of themselves; by comparisons, which let NaN through, and to a value that an infinity makes NaN:
+// an infinite x (sums that pass the largest value) gives what the formulas give in floating point, so that it is seen in the results: inf act(inf), NaN
+// at -inf (-inf times 0) and in the slope at either, whose second term is infinity times 0.
 template <bool FAST, int KIND>
 __device__ __forceinline__ void gate_one(float x, float &a, float &slope) {
   if constexpr (KIND == MTNLG_GATE_SILU) {
     if constexpr (FAST) {
-      const float c = x < -80.0f ? -80.0f : x, e = __builtin_amdgcn_exp2f(c * -1.4426950408889634f), s = __builtin_amdgcn_rcpf(1.0f + e);
+      const float c = x < -80.0f ? nan_of_inf(x, -80.0f) : x, e = __builtin_amdgcn_exp2f(c * -1.4426950408889634f), s = __builtin_amdgcn_rcpf(1.0f + e);
       a = c * s;
       slope = s + a * (e * s);
     } else {
@@ -20,17 +23,17 @@ __device__ __forceinline__ void gate_one(float x, float &a, float &slope) {
       slope = s + a * (1.0f - s);
     }
   } else if constexpr (KIND == MTNLG_GATE_GELU_TANH) {
-    const float lo = x < -10.0f ? -10.0f : x, c = lo > 10.0f ? 10.0f : lo;
+    const float lo = x < -10.0f ? nan_of_inf(x, -10.0f) : x, c = lo > 10.0f ? 10.0f : lo;
     if constexpr (FAST) {
       constexpr float D1 = 2.0f * 0.79788456080286536f, D3 = D1 * 3.0f * 0.044715f;
       const float c2 = c * c;
       float e;
       const float s = gelu_sigmoid_f(c, c2, e);
       a = lo * s;
-      slope = s + (c * (D1 + D3 * c2)) * (e * s) * s;
+      slope = nan_of_inf(x, s) + (c * (D1 + D3 * c2)) * (e * s) * s;
     } else {
       a = gelu_f(x, false);
-      slope = gelu_grad_f(c, false);
+      slope = nan_of_inf(x, gelu_grad_f(c, false));
     }
   } else if constexpr (FAST) {
     // The normal distribution's tail below -|x| as exp(-x^2 / 2) t P(t), t = 1 / (1 + 0.44 |x| / sqrt 2): P of degree 7 fitted here to the least relative error
