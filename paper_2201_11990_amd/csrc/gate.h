@@ -23,17 +23,19 @@ __device__ __forceinline__ void gate_one(float x, float &a, float &slope) {
       slope = s + a * (1.0f - s);
     }
   } else if constexpr (KIND == MTNLG_GATE_GELU_TANH) {
-    const float lo = x < -10.0f ? nan_of_inf(x, -10.0f) : x, c = lo > 10.0f ? 10.0f : lo;
+    constexpr float K = 2.0f * 0.79788456080286536f, D3 = K * 3.0f * 0.044715f;   // 2 u' = K + D3 x^2
     if constexpr (FAST) {
-      constexpr float D1 = 2.0f * 0.79788456080286536f, D3 = D1 * 3.0f * 0.044715f;
-      const float c2 = c * c;
+      const float lo = x < -10.0f ? nan_of_inf(x, -10.0f) : x, c = lo > 10.0f ? 10.0f : lo, c2 = c * c;
       float e;
       const float s = gelu_sigmoid_f(c, c2, e);
       a = lo * s;
-      slope = nan_of_inf(x, s) + (c * (D1 + D3 * c2)) * (e * s) * s;
+      slope = nan_of_inf(x, s) + (c * (K + D3 * c2)) * (e * s) * s;
     } else {
-      a = gelu_f(x, false);
-      slope = nan_of_inf(x, gelu_grad_f(c, false));
+      // s and 1 - s from exp(-|2 u|), which is at most 1: neither is a difference.  (1 + tanh u) / 2 has 24 bits below 1 and not below s: at -5 the value had two of its own left
+      const float w = K * (x + 0.044715f * x * x * x), t = expf(-fabsf(w)), d = 1.0f / (1.0f + t), td = t * d, s = w < 0.0f ? td : d;
+      const float lo = x < -12.0f ? -12.0f : x, c = lo > 12.0f ? 12.0f : lo;   // (beyond, t is 0)
+      a = x * s;
+      slope = nan_of_inf(x, s) + (c * (K + D3 * c * c)) * (td * d);
     }
   } else if constexpr (FAST) {
     // The normal distribution's tail below -|x| as exp(-x^2 / 2) t P(t), t = 1 / (1 + 0.44 |x| / sqrt 2): P of degree 7 fitted here to the least relative error
@@ -49,8 +51,10 @@ __device__ __forceinline__ void gate_one(float x, float &a, float &slope) {
     a = x * cdf;
     slope = cdf + x * (e * 0.39894228f);
   } else {
-    a = gelu_f(x, true);
-    slope = gelu_grad_f(x, true);
+    // the tail by erfc: (1 + erf) / 2 cancels for negative x as 1 + tanh does
+    const float tail = 0.5f * erfcf(fabsf(x) * 0.70710678118654752f), cdf = x < 0.0f ? tail : 1.0f - tail;
+    a = x * cdf;
+    slope = cdf + x * (expf(-0.5f * x * x) * 0.39894228f);
   }
 }
 // a[i] = act(x[i]), slope[i] = act'(x[i]); the kind is the same in all lanes and is looked at once for the N values
