@@ -4,10 +4,18 @@
 
 namespace mtnlg {
 
-// split: on tiles cut along K (gated_split_time)
-int gated_mfma_fwd(int kind, int64_t T, int64_t h, int64_t F, const void *x, const void *w_fc1, void *z, void *g, bool split, void *ws, size_t ws_bytes,
+// Kernels that the block's products go to; of GATED_STREAM on with a gemm_tile, or GATED_SPLIT, added: 128 x 128, each cut along K (gated_split_time)
+enum gated_kernel { GATED_PLAIN = 0, GATED_TOKENS, GATED_WAVE_32, GATED_WAVE_64, GATED_PARTS, GATED_GROUP_32, GATED_GROUP_64, GATED_STREAM = 16 };
+constexpr int GATED_SPLIT = 8;
+
+// The kernel that one of the block's products goes to: 0 z and g, 1 y, 2 dz, 3 dx (GATED_PLAIN: one of mtnlg_gemm's); with_dw: the gradient of the weight that dz or dx is
+// worked out with is wanted too.  Negative: a status
+int gated_path(const mtnlg_gated_desc *desc, int product, int with_dw);
+
+// tile: a gemm_tile, or GATED_SPLIT
+int gated_mfma_fwd(int kind, int64_t T, int64_t h, int64_t F, const void *x, const void *w_fc1, void *z, void *g, int tile, void *ws, size_t ws_bytes,
                    hipStream_t stream);
-int gated_mfma_bwd(int kind, int64_t T, int64_t h, int64_t F, const void *dy, const void *w_fc2, const void *z, void *dz, bool split, void *ws,
+int gated_mfma_bwd(int kind, int64_t T, int64_t h, int64_t F, const void *dy, const void *w_fc2, const void *z, void *dz, int tile, void *ws,
                    size_t ws_bytes, hipStream_t stream);
 
 // mode: GATE_FWD (A x, B w_fc1, C g) or GATE_BWD (A dy, B w_fc2, C dz); tile: 32 or 64

@@ -62,31 +62,60 @@ bool cut_along_k(const Sizes &s, int layout, int64_t M, int64_t N, int64_t K) {
   return split < gemm_time(s.dtype, layout, M, N, K, s.gemm_ws) && !gemm_wave_pick(s.dtype, layout, M, N, K, split / (K % 64 ? 1.35 : 1.0)) &&
          (int64_t)128 * (2 * K + N) * 2 < ((int64_t)1 << 31);   // (what 32-bit offsets reach, with room)
 }
-// C = A B^T (NT) or A B (NN) without the activation
-int plain_product(const Sizes &s, int layout, int64_t M, int64_t N, int64_t K, const void *A, const void *B, void *C, void *ws, hipStream_t st) {
-  if (s.dtype == MTNLG_BF16 && cut_along_k(s, layout, M, N, K)) return gated_split(layout, M, N, K, A, B, C, ws, s.gemm_ws, st);
-  return mtnlg_gemm(s.dtype, layout, M, N, K, A, B, C, nullptr, nullptr, 0, ws, s.gemm_ws, st);
-}
-
 // One of the two products that carry the activation, on the kernel that is estimated to be the fastest
 double gated_time(const Sizes &s, int mode) {
   const int layout = mode == GATE_FWD ? MTNLG_GEMM_NT : MTNLG_GEMM_NN;
   const int64_t N = mode == GATE_FWD ? 2 * s.F : s.F;
   return s.dtype == MTNLG_F32 ? gemm_parts_time(s.T, N, s.h) : gemm_mfma_time(layout, s.T, N, s.h, s.gemm_ws);
 }
-int gated_product(const Sizes &s, int mode, const void *A, const void *B, void *z, void *C, void *ws, hipStream_t st) {
+int gated_pick(const Sizes &s, int mode) {
   const int layout = mode == GATE_FWD ? MTNLG_GEMM_NT : MTNLG_GEMM_NN;
   const int64_t N = mode == GATE_FWD ? 2 * s.F : s.F;
-  if (s.dtype == MTNLG_BF16 && mode == GATE_FWD && gated_tokens_takes(s.T, N, s.h)) return gated_tokens_fwd(s.gate, s.T, s.h, s.F, A, B, z, C, st);
-  const bool split = s.dtype == MTNLG_BF16 && cut_along_k(s, layout, s.T, N, s.h);
-  if (const int tile = split ? 0 : gemm_wave_pick(s.dtype, layout, s.T, N, s.h, gated_time(s, mode)))
-    return gated_wave(s.dtype, mode, s.gate, s.T, s.h, s.F, A, B, z, C, tile, st);
-  if (s.dtype == MTNLG_F32) return gated_parts(mode, s.gate, s.T, s.h, s.F, A, B, z, C, st);
-  return mode == GATE_FWD ? gated_mfma_fwd(s.gate, s.T, s.h, s.F, A, B, z, C, split, ws, s.gemm_ws, st)
-                          : gated_mfma_bwd(s.gate, s.T, s.h, s.F, A, B, z, C, split, ws, s.gemm_ws, st);
+  if (s.dtype == MTNLG_BF16 && mode == GATE_FWD && gated_tokens_takes(s.T, N, s.h)) return GATED_TOKENS;
+  if (s.dtype == MTNLG_BF16 && cut_along_k(s, layout, s.T, N, s.h)) return GATED_STREAM + GATED_SPLIT;
+  if (const int tile = gemm_wave_pick(s.dtype, layout, s.T, N, s.h, gated_time(s, mode))) return tile == 32 ? GATED_WAVE_32 : GATED_WAVE_64;
+  return s.dtype == MTNLG_F32 ? (int)GATED_PARTS : GATED_STREAM + gemm_mfma_pick_tile(layout, s.T, N, s.h, s.gemm_ws);
+}
+int gated_product(const Sizes &s, int mode, int kernel, const void *A, const void *B, void *z, void *C, void *ws, hipStream_t st) {
+  if (kernel == GATED_TOKENS) return gated_tokens_fwd(s.gate, s.T, s.h, s.F, A, B, z, C, st);
+  if (kernel == GATED_WAVE_32 || kernel == GATED_WAVE_64)
+    return gated_wave(s.dtype, mode, s.gate, s.T, s.h, s.F, A, B, z, C, kernel == GATED_WAVE_32 ? 32 : 64, st);
+  if (kernel == GATED_PARTS) return gated_parts(mode, s.gate, s.T, s.h, s.F, A, B, z, C, st);
+  return mode == GATE_FWD ? gated_mfma_fwd(s.gate, s.T, s.h, s.F, A, B, z, C, kernel - GATED_STREAM, ws, s.gemm_ws, st)
+                          : gated_mfma_bwd(s.gate, s.T, s.h, s.F, A, B, z, C, kernel - GATED_STREAM, ws, s.gemm_ws, st);
+}
+
+// The tile of a launch of both products of a weight's backward (of sizes [M, N, K]), 0 where launches of their own are estimated to be faster; the estimate does not
+// know of rows that begin amid lines, which cost long launches a third (7473 tokens, h 2680, F 560: 144 us for what two launches take 112 for)
+int one_launch(const Sizes &s, double nn_time, const int64_t (&nn)[3], const int64_t (&tn)[3]) {
+  auto call = [](const int64_t (&n)[3]) { return GemmCall{n[0], n[1], n[2], nullptr, nullptr, nullptr, nullptr, 0}; };   // (all matrices are aligned)
+  const double tn_time = gemm_time(s.dtype, MTNLG_GEMM_TN, tn[0], tn[1], tn[2], s.gemm_ws);
+  const double less = s.dtype == MTNLG_BF16 && (s.h % 64 || s.F % 64) && nn_time + tn_time > 50.0 ? 1.0 / 1.35 : 1.0;
+  return gemm_wave_group_tile(s.dtype, call(nn), call(tn), 0, 0, 0, nn_time * less, tn_time * less);
+}
+
+// The kernel of a product: z and g, y, dz, dx; with_dw: of a backward one whose weight's gradient is wanted too
+enum Product { TO_G = 0, TO_Y, TO_DZ, TO_DX };
+int path_of(const Sizes &s, int product, bool with_dw) {
+  if (with_dw && product >= TO_DZ) {
+    const int tile = product == TO_DZ ? one_launch(s, gated_time(s, GATE_BWD), {s.T, s.F, s.h}, {s.h, s.F, s.T})
+                                      : one_launch(s, gemm_time(s.dtype, MTNLG_GEMM_NN, s.T, s.h, 2 * s.F, s.gemm_ws), {s.T, s.h, 2 * s.F}, {2 * s.F, s.h, s.T});
+    if (tile) return tile == 32 ? GATED_GROUP_32 : GATED_GROUP_64;
+  }
+  if (product == TO_G || product == TO_DZ) return gated_pick(s, product == TO_G ? GATE_FWD : GATE_BWD);
+  if (s.dtype == MTNLG_F32) return GATED_PLAIN;
+  if (product == TO_Y && gated_tokens_takes(s.T, s.h, s.F)) return GATED_TOKENS;
+  const bool cut = product == TO_Y ? cut_along_k(s, MTNLG_GEMM_NT, s.T, s.h, s.F) : cut_along_k(s, MTNLG_GEMM_NN, s.T, s.h, 2 * s.F);
+  return cut ? GATED_STREAM + GATED_SPLIT : (int)GATED_PLAIN;
 }
 
 }  // namespace
+
+int gated_path(const mtnlg_gated_desc *desc, int product, int with_dw) {
+  Sizes s;
+  MTNLG_TRY(sizes_of(desc, &s));
+  return path_of(s, product, with_dw != 0);
+}
 
 }  // namespace mtnlg
 
@@ -111,9 +140,11 @@ int mtnlg_gated_ffn_fwd(const mtnlg_gated_desc *desc, const void *x, const void 
   if (!lies_apart(out, 4, in, 3)) return MTNLG_INVALID_ARG;
   if (workspace_bytes < need) return MTNLG_WORKSPACE_TOO_SMALL;
   hipStream_t st = (hipStream_t)stream;
-  MTNLG_TRY(gated_product(s, GATE_FWD, x, w_fc1, z, g, workspace, st));
-  if (s.dtype == MTNLG_BF16 && gated_tokens_takes(s.T, s.h, s.F)) return gated_tokens_out(s.T, s.h, s.F, g, w_fc2, y, st);
-  return plain_product(s, MTNLG_GEMM_NT, s.T, s.h, s.F, g, w_fc2, y, workspace, st);
+  MTNLG_TRY(gated_product(s, GATE_FWD, path_of(s, TO_G, false), x, w_fc1, z, g, workspace, st));
+  const int to_y = path_of(s, TO_Y, false);
+  if (to_y == GATED_TOKENS) return gated_tokens_out(s.T, s.h, s.F, g, w_fc2, y, st);
+  if (to_y != GATED_PLAIN) return gated_split(MTNLG_GEMM_NT, s.T, s.h, s.F, g, w_fc2, y, workspace, s.gemm_ws, st);
+  return mtnlg_gemm(s.dtype, MTNLG_GEMM_NT, s.T, s.h, s.F, g, w_fc2, y, nullptr, nullptr, 0, workspace, s.gemm_ws, stream);
 }
 
 int mtnlg_gated_ffn_bwd(const mtnlg_gated_desc *desc, const void *x, const void *w_fc1, const void *w_fc2, const void *z, const void *g,
@@ -136,26 +167,22 @@ int mtnlg_gated_ffn_bwd(const mtnlg_gated_desc *desc, const void *x, const void 
   auto gemm = [&](int layout, const GemmCall &c) {
     return mtnlg_gemm(s.dtype, layout, c.M, c.N, c.K, c.A, c.B, c.C, nullptr, nullptr, c.epi, workspace, s.gemm_ws, stream);
   };
-  // Both products of a weight in one launch, if that is estimated to be faster; the estimate does not know of rows that begin amid lines, which cost long
-  // launches a third (7473 tokens, h 2680, F 560: 144 us for what two launches take 112 for)
-  auto one_launch = [&](const GemmCall &nn, double nn_time, const GemmCall &tn) {
-    const double tn_time = gemm_time(s.dtype, MTNLG_GEMM_TN, tn.M, tn.N, tn.K, s.gemm_ws);
-    const double less = s.dtype == MTNLG_BF16 && (s.h % 64 || s.F % 64) && nn_time + tn_time > 50.0 ? 1.0 / 1.35 : 1.0;
-    return gemm_wave_group_tile(s.dtype, nn, tn, 0, 0, 0, nn_time * less, tn_time * less);
-  };
   const GemmCall to_dz{s.T, s.F, s.h, dy, w_fc2, dz, const_cast<void *>(z), (uint32_t)s.gate}, to_dw2{s.h, s.F, s.T, dy, g, dw_fc2, nullptr, epi};
-  const int tile2 = dw_fc2 ? one_launch(to_dz, gated_time(s, GATE_BWD), to_dw2) : 0;
-  if (tile2) {
-    MTNLG_TRY(gated_wave_group(s.dtype, to_dz, to_dw2, tile2, st));
+  const int dz_path = path_of(s, TO_DZ, dw_fc2 != nullptr);
+  if (dz_path == GATED_GROUP_32 || dz_path == GATED_GROUP_64) {
+    MTNLG_TRY(gated_wave_group(s.dtype, to_dz, to_dw2, dz_path == GATED_GROUP_32 ? 32 : 64, st));
   } else {
     if (dw_fc2) MTNLG_TRY(gemm(MTNLG_GEMM_TN, to_dw2));
-    MTNLG_TRY(gated_product(s, GATE_BWD, dy, w_fc2, const_cast<void *>(z), dz, workspace, st));
+    MTNLG_TRY(gated_product(s, GATE_BWD, dz_path, dy, w_fc2, const_cast<void *>(z), dz, workspace, st));
   }
   const GemmCall to_dx{s.T, s.h, 2 * s.F, dz, w_fc1, dx, nullptr, 0}, to_dw1{2 * s.F, s.h, s.T, dz, x, dw_fc1, nullptr, epi};
-  if (dx && dw_fc1)
-    if (const int tile = one_launch(to_dx, gemm_time(s.dtype, MTNLG_GEMM_NN, to_dx.M, to_dx.N, to_dx.K, s.gemm_ws), to_dw1))
-      return gemm_wave_group(s.dtype, to_dx, to_dw1, ColumnSums{}, tile, st);
-  if (dx) MTNLG_TRY(plain_product(s, MTNLG_GEMM_NN, s.T, s.h, 2 * s.F, dz, w_fc1, dx, workspace, st));
+  if (dx) {
+    const int dx_path = path_of(s, TO_DX, dw_fc1 != nullptr);
+    if (dx_path == GATED_GROUP_32 || dx_path == GATED_GROUP_64)
+      return gemm_wave_group(s.dtype, to_dx, to_dw1, ColumnSums{}, dx_path == GATED_GROUP_32 ? 32 : 64, st);
+    if (dx_path != GATED_PLAIN) MTNLG_TRY(gated_split(MTNLG_GEMM_NN, s.T, s.h, 2 * s.F, dz, w_fc1, dx, workspace, s.gemm_ws, st));
+    else MTNLG_TRY(gemm(MTNLG_GEMM_NN, to_dx));
+  }
   if (dw_fc1) MTNLG_TRY(gemm(MTNLG_GEMM_TN, to_dw1));
   return MTNLG_OK;
 }

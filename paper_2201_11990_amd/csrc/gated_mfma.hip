@@ -12,8 +12,6 @@ namespace mtnlg {
 
 namespace {
 
-constexpr int SPLIT_128 = -2;   // 128 x 128, cut along K
-
 template <bool BT, int EPI>
 int launch_tile(int tile, const GemmArgs &g, void *ws, size_t ws_bytes, hipStream_t st) {
   switch (tile) {
@@ -22,26 +20,26 @@ int launch_tile(int tile, const GemmArgs &g, void *ws, size_t ws_bytes, hipStrea
     case GEMM_TILE_RAGGED_256: return launch_stream<256, 256, 2, 4, 0, false, BT, true, EPI>(g, ws, ws_bytes, st);
     case GEMM_TILE_RAGGED_128: return launch_stream<128, 128, 2, 2, 0, false, BT, true, EPI>(g, ws, ws_bytes, st);
     case GEMM_TILE_RAGGED_128_DEEP: return launch_stream<128, 128, 2, 2, 4, false, BT, true, EPI>(g, ws, ws_bytes, st);
-    case SPLIT_128: return launch_stream<128, 128, 2, 2, 4, false, BT, true, EPI, true>(g, ws, ws_bytes, st);
+    case GATED_SPLIT: return launch_stream<128, 128, 2, 2, 4, false, BT, true, EPI, true>(g, ws, ws_bytes, st);
     default: return MTNLG_UNSUPPORTED_SHAPE;
   }
 }
 
 }  // namespace
 
-int gated_mfma_fwd(int kind, int64_t T, int64_t h, int64_t F, const void *x, const void *w_fc1, void *z, void *g, bool split, void *ws, size_t ws_bytes,
+int gated_mfma_fwd(int kind, int64_t T, int64_t h, int64_t F, const void *x, const void *w_fc1, void *z, void *g, int tile, void *ws, size_t ws_bytes,
                    hipStream_t stream) {
   const GemmArgs a{T, 2 * F, h, (const bf16 *)x, (const bf16 *)w_fc1, h, h, g, F, EpiArgs{nullptr, z, (uint32_t)kind}, 0, 0, 0, 0, 1, 0, nullptr};
   LaunchScope scope(MTNLG_K_GEMM_NT, stream);
-  return launch_tile<false, EPI_GATE_FWD>(split ? SPLIT_128 : gemm_mfma_pick_tile(MTNLG_GEMM_NT, T, 2 * F, h, ws ? ws_bytes : 0), a, ws, ws_bytes, stream);
+  return launch_tile<false, EPI_GATE_FWD>(tile, a, ws, ws_bytes, stream);
 }
 
-int gated_mfma_bwd(int kind, int64_t T, int64_t h, int64_t F, const void *dy, const void *w_fc2, const void *z, void *dz, bool split, void *ws,
+int gated_mfma_bwd(int kind, int64_t T, int64_t h, int64_t F, const void *dy, const void *w_fc2, const void *z, void *dz, int tile, void *ws,
                    size_t ws_bytes, hipStream_t stream) {
   const GemmArgs a{T, F, h, (const bf16 *)dy, (const bf16 *)w_fc2, h, F, dz, 2 * F, EpiArgs{nullptr, const_cast<void *>(z), (uint32_t)kind}, 0, 0, 0, 0, 1, 0,
                    nullptr};
   LaunchScope scope(MTNLG_K_GEMM_NN, stream);
-  return launch_tile<true, EPI_GATE_BWD>(split ? SPLIT_128 : gemm_mfma_pick_tile(MTNLG_GEMM_NN, T, F, h, ws ? ws_bytes : 0), a, ws, ws_bytes, stream);
+  return launch_tile<true, EPI_GATE_BWD>(tile, a, ws, ws_bytes, stream);
 }
 
 // Products of few row and column tiles with long sums (of some hundred tokens, w_fc2's and dx from both halves of dz above all): on 128 x 128 tiles of which
