@@ -5,13 +5,13 @@ import torch
 
 import paper_2201_11990_amd as M
 from gated_paths import path
-from test_gpu_gated import DT, GATES, HALF_STEP, act, backward, forward, product, room, within
+from test_gpu_gated import DT, GATES, HALF_STEP, act, backward, check_backward, check_forward, check_weights, forward, product, room, within
 from test_gpu_gated import F as STEP
 
 # tokens, hidden, ffn, kernel of g
 LIMITS = [("bf16", 5, 32768, 65280, "tokens"), ("bf16", 3, 2048, 1044480, "tokens"), ("bf16", 65, 32768, 65280, "ragged 128"), ("bf16", 100, 20480, 104448, "ragged 128 deep"),
           ("bf16", 130, 32768, 65280, "ragged 256"), ("bf16", 256, 32768, 65280, "256x256"), ("bf16", 256, 20480, 104448, "256x256, cut"),
-          ("bf16", 256, 2048, 1044480, "256x320"), ("fp32", 5, 32768, 32640, "wave 32"), ("fp32", 40, 32768, 32640, "wave 64"), ("fp32", 70, 32768, 32640, "parts")]
+          ("bf16", 256, 2048, 1044480, "256x320"), ("bf16", 33, 2040, 1048576, "tokens"), ("fp32", 5, 32768, 32640, "wave 32"), ("fp32", 40, 32768, 32640, "wave 64"), ("fp32", 70, 32768, 32640, "parts")]
 
 
 @pytest.mark.parametrize("dtype,T,h,ffn,kernel", LIMITS)
@@ -57,3 +57,30 @@ def test_weights_at_the_limit(dtype, T, h, ffn, kernel):
         assert not torch.isnan(s[k]).any(), k
     del s, ws, a, za, zb, ea, eb, dg, e, slope, error
     torch.cuda.empty_cache()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,h,ffn", [("bf16", 8, 8), ("bf16", 16, 8), ("fp32", 8, 8), ("fp32", 8, 16)])
+def test_as_many_tokens_as_may_be(dtype, h, ffn):
+    # a thousand of 2^22 - 64 tokens are not zero, the first and the last among them: sums over tokens are sums of a thousand
+    T, n = 2 ** 22 - 64, 1000
+    gen, dt = torch.Generator(device="cuda").manual_seed(h + ffn), DT[dtype]
+    at = torch.randint(0, T, (n,), generator=gen, device="cuda").index_fill_(0, torch.tensor([0], device="cuda"), T - 1).unique()
+    s = {k: torch.zeros(shape, dtype=dt, device="cuda") for k, shape in (("x", (T, h)), ("dy", (T, h)))}
+    for k in s:
+        s[k][at] = torch.randn((len(at), h), generator=gen, device="cuda").to(dt)
+    r = lambda *shape: torch.randn(shape, generator=gen, device="cuda").to(dt)   # noqa: E731
+    nan = lambda *shape: torch.full(shape, float("nan"), dtype=dt, device="cuda")   # noqa: E731
+    s.update(w_fc1=r(2 * ffn, h), w_fc2=r(h, ffn), z=nan(T, 2 * ffn), g=nan(T, ffn), y=nan(T, h), dz=nan(T, 2 * ffn), dx=nan(T, h), dw_fc1=nan(2 * ffn, h),
+             dw_fc2=nan(h, ffn))
+    desc = M.gated_desc(s["x"], s["w_fc1"], GATES["gelu_tanh"])
+    ws = room(desc)
+    forward(desc, s, ws)
+    backward(desc, s, ws)
+    some = {k: (t[at] if t.shape[0] == T else t) for k, t in s.items()}
+    check_forward("gelu_tanh", some)
+    check_backward("gelu_tanh", some)
+    check_weights(some, s["dw_fc1"], s["dw_fc2"])
+    rest = torch.ones(T, dtype=torch.bool, device="cuda").index_fill_(0, at, False)
+    for k in ("z", "g", "y", "dz", "dx"):
+        assert (s[k][rest] == 0).all(), k
