@@ -386,7 +386,7 @@ enum mtnlg_gate { MTNLG_GATE_SILU = 0, MTNLG_GATE_GELU_TANH = 1, MTNLG_GATE_GELU
 typedef struct {
   int32_t dtype;    /* MTNLG_F32 or MTNLG_BF16                                                    */
   int32_t gate;     /* mtnlg_gate                                                               */
-  int64_t tokens;   /* T, <= 2^22 - 64                                                            */
+  int64_t tokens;   /* T, <= 2^22 - 64; float: T by 2 F in less than 2^23 tiles of 128 x 128       */
   int32_t hidden;   /* h, a multiple of 8, <= 32768                                               */
   int32_t ffn;      /* F, a multiple of 8, <= 2^20; h F <= 2^31 - 2^23, float 2^30 - 2^22          */
   uint32_t flags;   /* backward: MTNLG_ACCUMULATE_WGRAD, MTNLG_WGRAD_FP32                         */

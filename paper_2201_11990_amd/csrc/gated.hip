@@ -24,6 +24,8 @@ int sizes_of(const mtnlg_gated_desc *d, Sizes *s) {
   if (d->tokens > GEMM_GENERIC_MAX_ROWS || d->hidden % 8 || d->hidden > 32768 || d->ffn % 8 || d->ffn > (1 << 20)) return MTNLG_UNSUPPORTED_SHAPE;
   // 32-bit offsets reach both halves of w_fc1 from a tile's first row
   if ((int64_t)d->hidden * d->ffn > (d->dtype == MTNLG_F32 ? ((int64_t)1 << 30) - (1 << 22) : ((int64_t)1 << 31) - (1 << 23))) return MTNLG_UNSUPPORTED_SHAPE;
+  // a launch is of less than 2^32 work items: in parts, 512 to a tile of 128 x 128 (what bf16 takes for so many columns has fewer, and memory ends before)
+  if (d->dtype == MTNLG_F32 && ((d->tokens + 127) / 128) * ((2 * (int64_t)d->ffn + 127) / 128) >= (int64_t)1 << 23) return MTNLG_UNSUPPORTED_SHAPE;
   *s = Sizes{d->tokens, d->hidden, d->ffn, d->dtype, d->gate, d->dtype == MTNLG_F32 ? (size_t)4 : 2, 0};
   auto need = [&](int layout, int64_t M, int64_t N, int64_t K) { s->gemm_ws = std::max(s->gemm_ws, mtnlg_gemm_workspace(s->dtype, layout, M, N, K)); };
   need(MTNLG_GEMM_NT, s->T, 2 * s->F, s->h);

@@ -1,7 +1,10 @@
 """Which kernels the gated feed-forward block's tests reach: every size goes to the kernels that its entry names, and together they are all that there are."""
+import ctypes
+
 import pytest
 
-from gated_paths import PATHS, PRODUCTS, path
+from gated_paths import NAMES, PATHS, PRODUCTS, path
+from paper_2201_11990_amd import binding as B
 from test_gpu_gated import SIZES
 
 
@@ -19,3 +22,18 @@ def test_every_kernel_is_reached():
     sizes = [(dtype, *s) for s in SIZES for dtype in ("bf16", "fp32")] + list(PATHS)
     for (dtype, product), want in every.items():
         assert {path(*s, product) for s in sizes if s[0] == dtype} == want, (dtype, product)
+
+
+def test_more_work_items_than_a_launch_has_are_refused():
+    # fp32 in parts: 512 to a tile of 128 x 128, less than 2^32 in all
+    fn = B.lib()._ZN5mtnlg10gated_pathEPK16mtnlg_gated_descii
+    fn.argtypes, fn.restype = [ctypes.c_void_p, ctypes.c_int, ctypes.c_int], ctypes.c_int
+
+    def ask(dtype, ffn):
+        desc = B.GatedDesc(dtype, 0, 2 ** 22 - 64, 8, ffn, 0)
+        return fn(ctypes.addressof(desc), 0, 0)
+
+    assert NAMES[ask(B.F32, 255 * 64)] == "parts" and ask(B.F32, 255 * 64 + 8) == -3 and ask(B.BF16, 255 * 64 + 8) > 0
+    desc = B.GatedDesc(B.F32, 0, 2 ** 22 - 64, 8, 255 * 64 + 8, 0)
+    assert B.lib().mtnlg_gated_ffn_workspace(ctypes.byref(desc)) == 0
+    assert B.lib().mtnlg_gated_ffn_fwd(ctypes.byref(desc), *((i + 1) << 46 for i in range(7)), 1 << 40, None) == -3
