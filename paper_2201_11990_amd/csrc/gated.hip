@@ -2,7 +2,7 @@
 //   forward   x w_fc1^T (act(gate) * other in the epilogue), g w_fc2^T
 //   backward  dw_fc2 = dy^T g, dy w_fc2 (the activation's backward in the epilogue: dz), dx = dz w_fc1, dw_fc1 = dz^T x
 // Bound by the matrix pipes from some hundred tokens on: 6 T h F operations forward and 12 backward, with z written and read once.  In small calls
-// the products of one weight matrix's backward are one launch (gemm_wave.hip), so a step of 61 tokens is four: 26 us in fp32 (h 520, F 344), 39 in the seven that it was.
+// the products of one weight matrix's backward are one launch (gemm_wave.hip), so a step of 61 tokens is four: 25 us in fp32 (h 520, F 344), 39 in the seven that it was.
 #include <algorithm>
 
 #include "gated.h"
